@@ -1,0 +1,434 @@
+// Attention of new tokens over the 8-bit cache (include/eas_attention.h).
+//
+// A row is one query of one head; the rows of a sequence that share a key / value head
+// (its queries times the group's heads) are taken 16 at a time, as the columns of MFMA
+// products whose rows are the cache's tokens and dimensions:
+//   S^T = K Q^T,  O^T += V^T P^T   (v_mfma_f32_16x16x32_f16).
+// A wave walks tiles of 64 tokens.  Which token sits in which MFMA row is free, and is
+// chosen so that a lane ends with the 16 scores of 16 consecutive tokens of one query and
+// needs the values of the same 16 tokens of one dimension: one 16-byte load from the value
+// codes, which are stored dimension by dimension for that.  Nothing goes through LDS but
+// the waves' final sums.  The 16 tokens lie in one page, whatever its size, so a lane
+// looks up one scale of each kind.
+//
+// Codes are exact in fp16 (both formats), and so are the queries after a multiplication by
+// a power of two for each row, so the scores are exact products summed in fp32.  With
+// block scales 2^f of the values, x = scale * q . k in log2 units and running maxima m of
+// x and m' of x + f, a lane sums l += 2^(x - m) and O += 2^(x + f - m') * code: whatever
+// the scales, the largest weight of a code is within [2^-8, 2^8], so rounding the weights
+// to fp16 costs 2^-12 of the result.
+//
+// A sequence's tokens are split into runs by a rule on its own length and queries only,
+// so its result does not depend on the batch; each run's result goes to the workspace
+// and a second kernel joins them in order.
+#include "attention_ops.h"
+
+namespace eas {
+namespace {
+
+constexpr int TILE = 64;         // tokens per wave and step
+constexpr int NW = 4;            // waves per workgroup
+constexpr int RUN = NW * TILE;   // smallest run: a tile for each wave
+constexpr int MAX_RUNS = 64;     // runs per sequence
+constexpr int RUN_ROWS = 256;    // runs * queries of a sequence that is split
+
+// Runs that `len` tokens are split into for nq queries, and a run's tokens.
+__host__ __device__ inline int n_runs(int len, int nq) {
+  const int by_len = (int)(((int64_t)len + RUN - 1) / RUN);
+  int most = nq > 0 ? RUN_ROWS / nq : 1;
+  most = most < 1 ? 1 : most > MAX_RUNS ? MAX_RUNS : most;
+  return by_len < 1 ? 1 : by_len < most ? by_len : most;
+}
+__host__ __device__ inline int run_tokens(int len, int runs) {
+  return (int)(((int64_t)len + (int64_t)runs * RUN - 1) / ((int64_t)runs * RUN)) * RUN;
+}
+// Workspace slots per sequence and head: at least n_runs * nq for every nq <= max_q, len <= max_len
+// of a sequence that is split
+inline int64_t slots(int max_q, int max_len) {
+  const int64_t by_len = ((int64_t)max_len + RUN - 1) / RUN;
+  const int64_t runs = by_len < 1 ? 1 : by_len < MAX_RUNS ? by_len : MAX_RUNS;
+  return runs * max_q < RUN_ROWS ? runs * max_q : RUN_ROWS;
+}
+
+struct Kv8AttnArgs {
+  Kv8Args c;
+  const void* q;
+  void* out;
+  float* lse;
+  eas_strides qs, os;
+  const int* cu_q;
+  const int* lens;
+  const int* pages;
+  float* part;          // [n_seqs, heads, slots, D] results of runs, then [n_seqs, heads, slots] their log2 sums
+  float* part_lse;
+  float scale_log2;     // scale * log2(e)
+  int heads, causal, n_rows, max_q, max_len, max_pages, n_seqs, slots, row_tiles, runs;
+};
+
+struct Seq {
+  long row0;   // first query's row
+  int nq, len;
+};
+
+__device__ __forceinline__ Seq find_seq(const Kv8AttnArgs& a, int r) {
+  Seq s;
+  long n;
+  if (a.cu_q) {
+    s.row0 = a.cu_q[r];
+    n = (long)a.cu_q[r + 1] - s.row0;
+  } else {
+    s.row0 = (long)r * a.max_q;
+    n = a.max_q;
+  }
+  n = min(n, (long)a.max_q);
+  if (s.row0 < 0 || s.row0 + n > a.n_rows) n = s.row0 < 0 ? 0 : a.n_rows - s.row0;
+  s.nq = (int)max(n, 0l);
+  s.len = max(0, min(a.lens[r], min(a.max_len, a.max_pages << a.c.page_shift)));
+  return s;
+}
+
+// 16 codes to fp16, exactly: int8 by building 1024 + (code + 128) and taking 1152 off
+template <int FORMAT>
+__device__ __forceinline__ void codes_to_f16(const uint4& w, f16x8* lo, f16x8* hi) {
+  union { f16x2 h[8]; f16x8 v[2]; } u;
+  const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (FORMAT == EAS_KV_INT8) {
+      const uint32_t b = x[i] ^ 0x80808080u;
+      union { uint32_t u; f16x2 h; } p0, p1;
+      p0.u = __builtin_amdgcn_perm(0x64646464u, b, 0x04010400u);
+      p1.u = __builtin_amdgcn_perm(0x64646464u, b, 0x04030402u);
+      u.h[2 * i] = p0.h - (f16)1152.0f;
+      u.h[2 * i + 1] = p1.h - (f16)1152.0f;
+    } else {
+      u.h[2 * i] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x[i], 1.0f, false);
+      u.h[2 * i + 1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x[i], 1.0f, true);
+    }
+  }
+  *lo = u.v[0];
+  *hi = u.v[1];
+}
+
+// the first n of 16 bytes, the others 0
+__device__ __forceinline__ uint4 first_bytes(uint4 w, int n) {
+  uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int k = min(max(n - 4 * i, 0), 4);
+    x[i] &= k == 4 ? 0xffffffffu : (1u << 8 * k) - 1;
+  }
+  return make_uint4(x[0], x[1], x[2], x[3]);
+}
+
+// maximum over the four lanes that hold one query (lane, lane ^ 16, ^ 32, ^ 48)
+__device__ __forceinline__ float column_max(float v) {
+  v = fmaxf(v, __shfl_xor(v, 16, 64));
+  return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+
+template <class T, int FORMAT, int D>
+__global__ __launch_bounds__(64 * NW) void kv8_attention_kernel(Kv8AttnArgs a) {
+  typedef T Tx8 __attribute__((ext_vector_type(8)));
+  constexpr int DX = D / 64;   // 64-dimension parts of a key
+  constexpr int DB = D / 16;   // 16-dimension blocks of the output
+  __shared__ float o_part[NW][16][D];
+  __shared__ float m_part[NW][16], mv_part[NW][16], l_part[NW][16];
+
+  int b = blockIdx.x;
+  const int run = b % a.runs;
+  b /= a.runs;
+  const int rt = b % a.row_tiles;
+  b /= a.row_tiles;
+  const int kvh = b % a.c.kv_heads, r = b / a.c.kv_heads;
+  const Seq s = find_seq(a, r);
+  const int group = a.heads / a.c.kv_heads;
+  if ((long)rt * 16 >= (long)s.nq * group) return;
+  const int runs = n_runs(s.len, s.nq);
+  if (run >= runs) return;
+  const int each = run_tokens(s.len, runs);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+
+  // this lane's query, and how many tokens it sees
+  const int rho = rt * 16 + c;
+  const bool real = rho < s.nq * group;
+  const int qi = real ? rho / group : 0, h = kvh * group + (real ? rho % group : 0);
+  const int sees = !real ? 0 : a.causal ? max(0, min(s.len, s.len - s.nq + qi + 1)) : s.len;
+  // the tile's last query sees most
+  const int last = min(rt * 16 + 15, s.nq * group - 1) / group;
+  const int most = a.causal ? max(0, min(s.len, s.len - s.nq + last + 1)) : s.len;
+  const long t_begin = (long)run * each;
+  const int t_end = (int)min((long)most, t_begin + each);
+
+  // queries times a power of two that brings the row's largest to [2^14, 2^15)
+  f16x8 qf[2 * DX];
+  float q_scale;
+  {
+    const T* q = static_cast<const T*>(a.q) + (s.row0 + qi) * a.qs.row + h * a.qs.head;
+    Tx8 v[2 * DX];
+    float top = 0.0f;
+#pragma unroll
+    for (int x = 0; x < DX; ++x)
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        v[2 * x + y] = *reinterpret_cast<const Tx8*>(q + 64 * x + 16 * g + 8 * y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)v[2 * x + y][e]));
+      }
+    top = column_max(top);
+    // 2^(14 - floor(log2 top)), kept in the normal range
+    const int e = min(max((int)(__float_as_uint(top) >> 23), 15), 254);
+    const float up = __uint_as_float((uint32_t)min(268 - e, 254) << 23);
+    q_scale = a.scale_log2 * __uint_as_float((uint32_t)max(e - 14, 0) << 23);
+#pragma unroll
+    for (int i = 0; i < 2 * DX; ++i)
+#pragma unroll
+      for (int e8 = 0; e8 < 8; ++e8) qf[i][e8] = (f16)((float)v[i][e8] * up);
+  }
+
+  f32x4 o[DB];
+#pragma unroll
+  for (int i = 0; i < DB; ++i) o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  float m = -INFINITY, mv = -INFINITY, l = 0.0f;
+
+  const int page_mask = (1 << a.c.page_shift) - 1;
+  const int* table = a.pages + (long)r * a.max_pages;
+  for (long t0 = t_begin + wave * TILE; t0 < t_end; t0 += NW * TILE) {
+    // pages of the 16 tokens whose scores and values this lane holds, and of those whose keys it loads
+    const int tv = (int)t0 + 16 * g, tk = (int)t0 + 16 * (c >> 2);
+    int pv = tv < s.len ? table[tv >> a.c.page_shift] : -1;
+    int pk = tk < s.len ? table[tk >> a.c.page_shift] : -1;
+    const bool there = pv >= 0 && pv < a.c.n_pages;
+    pv = there ? pv : 0;
+    pk = pk >= 0 && pk < a.c.n_pages ? pk : 0;
+    const long bv = (long)pv * a.c.kv_heads + kvh, bk = (long)pk * a.c.kv_heads + kvh;
+    const uint8_t* kp = a.c.k + ((bk << a.c.page_shift) + (tk & page_mask) + (c & 3)) * D + 16 * g;
+    const uint8_t* vp = a.c.v + (((bv * D) + c) << a.c.page_shift) + (tv & page_mask);
+    const float ks = a.c.k_scale[bv], vs = a.c.v_scale[bv];
+    uint4 kw[4][DX], vw[DB];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int x = 0; x < DX; ++x) kw[i][x] = *reinterpret_cast<const uint4*>(kp + 4 * i * D + 64 * x);
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+      vw[i] = *reinterpret_cast<const uint4*>(vp + ((long)16 * i << a.c.page_shift));
+
+    // scores of tokens tv + 4 i + e of this lane's query, in log2 units
+    float x[16];
+    const float ck = q_scale * ks;
+    const int left = there ? sees - tv : 0;   // of the lane's 16 tokens, those its query sees
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f32x4 sc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int d = 0; d < DX; ++d) {
+        f16x8 k0, k1;
+        codes_to_f16<FORMAT>(kw[i][d], &k0, &k1);
+        sc = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, qf[2 * d], sc, 0, 0, 0);
+        sc = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, qf[2 * d + 1], sc, 0, 0, 0);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[4 * i + e] = 4 * i + e < left ? sc[e] * ck : -INFINITY;
+    }
+    float top = x[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
+    const float f = vs > 0.0f ? (float)((int)(__float_as_uint(vs) >> 23) - 127) : -INFINITY;
+    const float top_m = column_max(top), top_v = column_max(top + f);
+    if (__any(top_m > m)) {
+      const float up = fmaxf(m, top_m);
+      l *= up == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - up);
+      m = up;
+    }
+    if (__any(top_v > mv)) {
+      const float up = fmaxf(mv, top_v);
+      const float alpha = up == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(mv - up);
+      mv = up;
+#pragma unroll
+      for (int i = 0; i < DB; ++i) o[i] *= alpha;
+    }
+    // p = 2^(x - m); a code's weight is p 2^(m + f - m')
+    const float m0 = m == -INFINITY ? 0.0f : m, mv0 = mv == -INFINITY ? 0.0f : mv;
+    const float w = f == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(fminf(m0 + f - mv0, 126.0f));
+    f16x8 p[2];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float e = __builtin_amdgcn_exp2f(x[i] - m0);
+      l += e;
+      p[i >> 3][i & 7] = (f16)(e * w);
+    }
+    const int held = there ? s.len - tv : 0;   // places behind the last token may hold anything
+    const bool ragged = __any(held < 16);
+#pragma unroll
+    for (int i = 0; i < DB; ++i) {
+      if (ragged) vw[i] = first_bytes(vw[i], held);
+      f16x8 v0, v1;
+      codes_to_f16<FORMAT>(vw[i], &v0, &v1);
+      o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[0], o[i], 0, 0, 0);
+      o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[1], o[i], 0, 0, 0);
+    }
+  }
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+
+  // the four waves' sums: lane (c, g) holds dimensions 16 i + 4 g .. + 4 of query c
+  if (g == 0) {
+    m_part[wave][c] = m;
+    mv_part[wave][c] = mv;
+    l_part[wave][c] = l;
+  }
+#pragma unroll
+  for (int i = 0; i < DB; ++i) *reinterpret_cast<f32x4*>(&o_part[wave][c][16 * i + 4 * g]) = o[i];
+  __syncthreads();
+  for (int i = threadIdx.x; i < 16 * (D / 4); i += 64 * NW) {
+    const int row = i / (D / 4), d = i % (D / 4) * 4, rr = rt * 16 + row;
+    if (rr >= s.nq * group) break;
+    float M = m_part[0][row];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) M = fmaxf(M, m_part[w][row]);
+    const float M0 = M == -INFINITY ? 0.0f : M;
+    float L = 0.0f;
+    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      L += l_part[w][row] * __builtin_amdgcn_exp2f(m_part[w][row] - M0);
+      const float beta = __builtin_amdgcn_exp2f(mv_part[w][row] - M0);
+      sum += *reinterpret_cast<const f32x4*>(&o_part[w][row][d]) * beta;
+    }
+    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+    const float lse2 = L == 0.0f ? -INFINITY : M0 + __log2f(L);
+    const int q = rr / group, head = kvh * group + rr % group;
+    if (runs == 1) {
+      const long orow = s.row0 + q;
+      typedef T Tx4 __attribute__((ext_vector_type(4)));
+      Tx4 y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = (T)(sum[e] * inv);
+      *reinterpret_cast<Tx4*>(static_cast<T*>(a.out) + orow * a.os.row + head * a.os.head + d) = y;
+      if (d == 0 && a.lse) a.lse[orow * a.heads + head] = lse2 * kLn2;
+    } else {
+      const long slot = ((long)r * a.heads + head) * a.slots + q * runs + run;
+      *reinterpret_cast<f32x4*>(a.part + slot * D + d) = sum * inv;
+      if (d == 0) a.part_lse[slot] = lse2;
+    }
+  }
+}
+
+// Joins the runs of the sequences that were split: a wave for each row.
+template <class T, int D>
+__global__ __launch_bounds__(64 * NW) void kv8_join_kernel(Kv8AttnArgs a) {
+  const long row = (long)blockIdx.x * NW + (threadIdx.x >> 6);   // (sequence, query, head)
+  const int lane = threadIdx.x & 63;
+  const int h = (int)(row % a.heads), q = (int)(row / a.heads % a.max_q);
+  const long r = row / a.heads / a.max_q;
+  if (r >= a.n_seqs) return;
+  const Seq s = find_seq(a, (int)r);
+  if (q >= s.nq) return;
+  const int runs = n_runs(s.len, s.nq);
+  if (runs == 1) return;
+  const long slot = (r * a.heads + h) * a.slots + (long)q * runs;
+  const float lse2 = lane < runs ? a.part_lse[slot + lane] : -INFINITY;
+  float M = lse2;
+#pragma unroll
+  for (int o = 32; o; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
+  const float M0 = M == -INFINITY ? 0.0f : M;
+  const float w = __builtin_amdgcn_exp2f(lse2 - M0);
+  const float W = wave_sum(w), inv = W == 0.0f ? 0.0f : 1.0f / W;
+  constexpr int E = D / 64;
+  float sum[E] = {};
+  for (int k = 0; k < runs; ++k) {
+    const float wk = __shfl(w, k, 64);
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum[e] += wk * a.part[(slot + k) * D + lane * E + e];
+  }
+  T* out = static_cast<T*>(a.out) + (s.row0 + q) * a.os.row + h * a.os.head + lane * E;
+#pragma unroll
+  for (int e = 0; e < E; ++e) out[e] = (T)(sum[e] * inv);
+  if (lane == 0 && a.lse) a.lse[(s.row0 + q) * a.heads + h] = W == 0.0f ? -INFINITY : (M0 + __log2f(W)) * kLn2;
+}
+
+template <class T, int FORMAT, int D>
+eas_status launch(const Kv8AttnArgs& a, unsigned blocks, bool join, hipStream_t s) {
+  hipLaunchKernelGGL((kv8_attention_kernel<T, FORMAT, D>), dim3(blocks), dim3(64 * NW), 0, s, a);
+  if (hipGetLastError() != hipSuccess) return EAS_ERR_HIP;
+  if (!join) return EAS_OK;
+  const int64_t rows = (int64_t)a.n_seqs * a.max_q * a.heads;
+  hipLaunchKernelGGL((kv8_join_kernel<T, D>), dim3((unsigned)((rows + NW - 1) / NW)), dim3(64 * NW), 0, s, a);
+  return hipGetLastError() == hipSuccess ? EAS_OK : EAS_ERR_HIP;
+}
+
+}  // namespace
+}  // namespace eas
+
+using namespace eas;
+
+extern "C" eas_status eas_kv8_attention_workspace(const eas_attn_shape* shape, int32_t max_q, int32_t max_len,
+                                                  int32_t n_seqs, int64_t* bytes) {
+  const eas_status st = check_shape(shape);
+  if (st != EAS_OK) return st;
+  if (max_q < 0 || max_len < 0 || n_seqs < 0 || !bytes) return EAS_ERR_INVALID_ARG;
+  *bytes = max_len <= RUN ? 0 : (int64_t)n_seqs * shape->heads * slots(max_q, max_len) * (shape->head_dim + 1) * 4;
+  return EAS_OK;
+}
+
+extern "C" eas_status eas_kv8_attention(const eas_kv8_cache* cache, const eas_attn_shape* shape, const void* q,
+                                        int32_t n_rows, const int32_t* cu_q, int32_t max_q, const int32_t* lens,
+                                        int32_t max_len, const int32_t* pages, int32_t max_pages, int32_t n_seqs,
+                                        void* out, float* lse, void* workspace, int64_t workspace_bytes,
+                                        void* stream) {
+  eas_status st = check_cache(cache);
+  if (st == EAS_OK) st = check_shape(shape);
+  if (st != EAS_OK) return st;
+  if (shape->kv_heads != cache->kv_heads || shape->head_dim != cache->head_dim) return EAS_ERR_INVALID_ARG;
+  st = check_strides(shape->q);
+  if (st == EAS_OK) st = check_table(cache, pages, max_pages, n_seqs);
+  if (st != EAS_OK) return st;
+  if (n_rows < 0 || max_q < 0 || max_len < 0 || !lens || (uintptr_t)lens % 4 || (uintptr_t)cu_q % 4 ||
+      (uintptr_t)lse % 4)
+    return EAS_ERR_INVALID_ARG;
+  st = check_out_strides(shape->out, n_rows, shape->heads, shape->head_dim);
+  if (st != EAS_OK) return st;
+  if (n_rows == 0 || max_q == 0 || n_seqs == 0) return EAS_OK;
+  if (!q || !out || !aligned16(q) || !aligned16(out)) return EAS_ERR_INVALID_ARG;
+  Kv8AttnArgs a = {};
+  a.c = kv8_args(cache);
+  a.q = q, a.out = out, a.lse = lse;
+  a.qs = shape->q, a.os = shape->out;
+  a.cu_q = cu_q, a.lens = lens, a.pages = pages;
+  a.scale_log2 = shape->scale * kLog2e;
+  a.heads = shape->heads, a.causal = shape->causal;
+  a.n_rows = n_rows, a.max_q = max_q < n_rows ? max_q : n_rows, a.max_pages = max_pages, a.n_seqs = n_seqs;
+  if (!cu_q) a.max_q = max_q;   // a sequence's rows start at multiples of it
+  const int64_t held = (int64_t)max_pages * cache->page_tokens;
+  a.max_len = max_len < held ? max_len : (int)held;
+  const bool join = a.max_len > RUN;
+  a.slots = (int)slots(a.max_q, a.max_len);
+  if (join) {
+    const int64_t parts = (int64_t)n_seqs * a.heads * a.slots;
+    if (!workspace || !aligned16(workspace)) return EAS_ERR_INVALID_ARG;
+    if (workspace_bytes < parts * (shape->head_dim + 1) * 4) return EAS_ERR_CAPACITY;
+    a.part = static_cast<float*>(workspace);
+    a.part_lse = a.part + parts * shape->head_dim;
+  }
+  const int group = a.heads / a.c.kv_heads;
+  const int64_t tiles = ((int64_t)(a.max_q < n_rows ? a.max_q : n_rows) * group + 15) / 16;
+  a.runs = n_runs(a.max_len, 1);
+  const int64_t blocks = tiles * a.runs * a.c.kv_heads * n_seqs;
+  if (tiles > 0x7fffffff || blocks > 0x7fffffff || (int64_t)n_seqs * a.max_q * a.heads > 0x7fffffff)
+    return EAS_ERR_UNSUPPORTED;
+  a.row_tiles = (int)tiles;
+#define EAS_KV8_CASE(DT, T, F, D)                                                   \
+  if (shape->dtype == DT && cache->format == F && shape->head_dim == D) \
+    return launch<T, F, D>(a, (unsigned)blocks, join, (hipStream_t)stream)
+  EAS_KV8_CASE(EAS_BF16, bf16, EAS_KV_INT8, 64);
+  EAS_KV8_CASE(EAS_BF16, bf16, EAS_KV_INT8, 128);
+  EAS_KV8_CASE(EAS_BF16, bf16, EAS_KV_E4M3, 64);
+  EAS_KV8_CASE(EAS_BF16, bf16, EAS_KV_E4M3, 128);
+  EAS_KV8_CASE(EAS_FP16, f16, EAS_KV_INT8, 64);
+  EAS_KV8_CASE(EAS_FP16, f16, EAS_KV_INT8, 128);
+  EAS_KV8_CASE(EAS_FP16, f16, EAS_KV_E4M3, 64);
+  EAS_KV8_CASE(EAS_FP16, f16, EAS_KV_E4M3, 128);
+#undef EAS_KV8_CASE
+  return EAS_ERR_UNSUPPORTED;
+}
