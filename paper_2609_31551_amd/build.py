@@ -20,7 +20,8 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-u
 # (the softmax works on them with VALU ops; AGPRs would need a copy each way),
 # and their running maxima are taken without NaN-quieting copies (the scores
 # are finite or -inf there, never NaN)
-FILE_FLAGS = {"attention_dma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans"]}
+_ATTENTION = ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans"]
+FILE_FLAGS = {"attention_dma.hip": _ATTENTION, "prompt_attention.hip": _ATTENTION}
 
 
 # Host-code sanitizers (AddressSanitizer + UndefinedBehaviorSanitizer) for a

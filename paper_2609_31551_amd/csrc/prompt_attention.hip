@@ -13,7 +13,6 @@
 namespace eas {
 namespace {
 
-constexpr int QT = 128;   // queries per workgroup
 constexpr int KT = 64;    // keys per tile
 
 // Work list: the query tiles of all sequences.
@@ -91,131 +90,247 @@ __device__ __forceinline__ bool any_not_finite(const f32x16* o) {
   return __any(top >= 0x7f800000u);
 }
 
-template <class T, int HD>
-__global__ __launch_bounds__(256) void prompt_kernel(PromptArgs a, PromptWork w) {
+#pragma clang diagnostic ignored "-Winline-asm"
+// 64 lanes' 16-byte pieces at base + voff, to 1 KB of LDS in lane order
+__device__ __forceinline__ void dma16(unsigned lds_addr, unsigned voff, const void* base) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n"
+               :: "s"(lds_addr), "v"(voff), "s"(base) : "memory", "m0");
+}
+
+typedef short v4i16 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
+
+template <int HD, int NW_>
+struct Cfg {
+  static constexpr int NW = NW_;                 // waves per workgroup, 32 queries each
+  static constexpr int QT = 32 * NW;             // queries per workgroup
+  static constexpr int R = HD / 8;               // 16-byte chunks per row
+  static constexpr int KS = HD / 16;             // 16-wide steps of q . k
+  static constexpr int HB = HD / 32;             // 32-row blocks of O^T
+  static constexpr int TILE = KT * HD * 2;       // bytes of a key or value tile
+  static constexpr int NDMA = TILE / 1024 / NW;  // DMA instructions per wave and tile
+  // Chunk L of a tile's row is stored at chunk (L + rot) % R.  A key read takes one chunk of 16 consecutive
+  // rows at a time, a transposing value read 64 bytes of 4 consecutive rows: both hit all banks once.
+  __device__ static int rot(int row) {
+    return R == 16 ? 4 * (row & 3) + ((row >> 2) & 3) : 2 * (row & 3) + ((row >> 2) & 1);
+  }
+  __device__ static int phys(int row, int L) { return (L + rot(row)) % R; }
+  __device__ static int logical(int row, int p) { return (p + R - rot(row)) % R; }
+};
+
+template <class T, int HD, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, PromptWork w) {
+  using C = Cfg<HD, NW>;
   typedef typename Mfma<T>::x8 x8;
-  constexpr int KS = HD / 16;      // 16-wide steps of q . k
-  constexpr int HB = HD / 32;      // 32-row blocks of O^T
-  constexpr int LDK = HD + 8;      // row stride of the key tile
-  constexpr int LDV = KT + 4;      // row stride of the transposed value tile
-  __shared__ __attribute__((aligned(16))) T Ks[KT * LDK];
-  __shared__ __attribute__((aligned(16))) T Vt[HD * LDV];
+  extern __shared__ __attribute__((aligned(1024))) char smem[];   // keys x 2, values x 2
+  __attribute__((address_space(3))) char* lds = (__attribute__((address_space(3))) char*)smem;
+  const unsigned lds0 = (unsigned)(size_t)lds;
 
   const int h = blockIdx.x % a.heads, tile = blockIdx.x / a.heads;
   int i = 0;
   while (i + 1 < w.n && w.tile_start[i + 1] <= tile) ++i;
   const int r = w.order[i];
   const int lq = w.cu_q[r + 1] - w.cu_q[r], lk = w.cu_k[r + 1] - w.cu_k[r];
-  const int q0 = (tile - w.tile_start[i]) * QT;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 5, l32 = lane & 31;
+  const int q0 = (w.tile_start[i + 1] - 1 - tile) * C::QT;   // the last tiles, which see most, first
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, l32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const T* qp = static_cast<const T*>(a.q) + w.cu_q[r] * a.qs.row + h * a.qs.head;
   const T* kp = static_cast<const T*>(a.k) + w.cu_k[r] * a.ks.row + h / a.group * a.ks.head;
   const T* vp = static_cast<const T*>(a.v) + w.cu_k[r] * a.vs.row + h / a.group * a.vs.head;
 
-  const int qi = q0 + wave * 32 + l32;   // this lane's query; past the end it is computed, not stored
-  const int qr = min(qi, lq - 1);
-  const int sees = a.causal ? max(0, min(lk, qr + lk - lq + 1)) : lk;
-  const int most = a.causal ? max(0, min(lk, min(q0 + QT, lq) + lk - lq)) : lk;   // over the workgroup
-  x8 qf[KS];
-#pragma unroll
-  for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const x8*>(qp + qr * a.qs.row + ks * 16 + g * 8);
+  // keys that a query sees: this lane's, the wave's fewest and most, the workgroup's most
+  auto seen = [&](int q) { return a.causal ? max(0, min(lk, min(q, lq - 1) + 1 + lk - lq)) : lk; };
+  const int qw = q0 + wave * 32, qi = qw + l32;
+  const int sees = seen(qi), fewest = seen(qw), most = qw < lq ? seen(qw + 31) : 0;
+  const int nt = (seen(q0 + C::QT - 1) + KT - 1) / KT, nt_w = (most + KT - 1) / KT;
 
-  f32x16 o[HB];
+  x8 qf[C::KS];
 #pragma unroll
-  for (int hb = 0; hb < HB; ++hb)
+  for (int ks = 0; ks < C::KS; ++ks)
+    qf[ks] = *reinterpret_cast<const x8*>(qp + min(qi, lq - 1) * a.qs.row + ks * 16 + g * 8);
+  // consumed here, before any DMA is in flight, so that the wait for them does not wait for a tile
+#pragma unroll
+  for (int ks = 0; ks < C::KS; ++ks) asm volatile("" ::"v"(qf[ks]));
+
+  // a tile's DMA: instruction wave + NW j fills LDS slots (its number) * 64 + lane; slot s is chunk s % R of row s / R
+  int drow[C::NDMA], dcol[C::NDMA];
+#pragma unroll
+  for (int j = 0; j < C::NDMA; ++j) {
+    const int slot = (wave + NW * j) * 64 + lane;
+    drow[j] = slot / C::R;
+    dcol[j] = C::logical(drow[j], slot % C::R) * 16;
+  }
+  auto fetch = [&](const T* p, long stride, int t, int lds_off) {
+    const int left = lk - 1 - t * KT;   // rows behind the last key read it again
+    const T* base = p + (long)t * KT * stride;
+#pragma unroll
+    for (int j = 0; j < C::NDMA; ++j)
+      dma16(lds0 + lds_off + (wave + NW * j) * 1024, (unsigned)min(drow[j], left) * (unsigned)(stride * 2) + dcol[j],
+            base);
+  };
+  auto fetch_k = [&](int t) { fetch(kp, a.ks.row, t, (t & 1) * C::TILE); };
+  auto fetch_v = [&](int t) { fetch(vp, a.vs.row, t, (2 + (t & 1)) * C::TILE); };
+
+  int kofs[C::KS];
+#pragma unroll
+  for (int ks = 0; ks < C::KS; ++ks) kofs[ks] = l32 * HD * 2 + C::phys(l32, 2 * ks + g) * 16;
+  // V^T operand: lane 16 q + 4 e + t reads row 16 (..) + 8 half + 4 g + e, columns 32 hb + 16 (q % 2) + 4 t .. + 4
+  int vofs[C::HB][2];
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const int row = 8 * half + 4 * g + ((lane >> 2) & 3);
+#pragma unroll
+    for (int hb = 0; hb < C::HB; ++hb) {
+      const int col = hb * 32 + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+      vofs[hb][half] = row * HD * 2 + C::phys(row, col >> 3) * 16 + (col & 7) * 2;
+    }
+  }
+
+  f32x16 o[C::HB];
+#pragma unroll
+  for (int hb = 0; hb < C::HB; ++hb)
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[hb][e] = 0.0f;
-  float m = -INFINITY, l = 0.0f;
+  float m = 0.0f, l = 0.0f;
 
-  for (int k0 = 0; k0 < most; k0 += KT) {
-    __syncthreads();
-    for (int c = tid; c < KT * (HD / 8); c += 256) {
-      const int key = c / (HD / 8), d = c % (HD / 8) * 8;
-      uint4 x = make_uint4(0, 0, 0, 0);
-      if (k0 + key < lk) x = *reinterpret_cast<const uint4*>(kp + (k0 + key) * a.ks.row + d);
-      *reinterpret_cast<uint4*>(Ks + key * LDK + d) = x;
-    }
-    for (int c = tid; c < KT * (HD / 8); c += 256) {
-      const int key = c % KT, d = c / KT * 8;
-      union { uint4 u; T e[8]; } x;
-      x.u = make_uint4(0, 0, 0, 0);   // values behind the last key may be anything, and 0 * NaN is NaN
-      if (k0 + key < lk) x.u = *reinterpret_cast<const uint4*>(vp + (k0 + key) * a.vs.row + d);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) Vt[(d + e) * LDV + key] = x.e[e];
-    }
-    __syncthreads();
-
-    f32x16 s[2];
+  auto scores = [&](int t, f32x16* s) {
+    const char* K = smem + (t & 1) * C::TILE;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[kb][e] = 0.0f;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const x8 kf = *reinterpret_cast<const x8*>(Ks + (kb * 32 + l32) * LDK + ks * 16 + g * 8);
-        s[kb] = Mfma<T>::go(kf, qf[ks], s[kb]);
-      }
+      for (int ks = 0; ks < C::KS; ++ks)
+        s[kb] = Mfma<T>::go(*reinterpret_cast<const x8*>(K + kb * 32 * HD * 2 + kofs[ks]), qf[ks], s[kb]);
     }
-    float mx = -INFINITY;
+  };
+  // Online softmax of the tile's scores s and O^T += V^T P^T.  One FMA turns a score into x = s c - m, in log2
+  // units over the maximum m.  m is raised lazily, when some x exceeds 8, so p = 2^x <= 256 and O is rarely
+  // scaled; O and l share m, so O / l is the same.  The first tile always sets it.
+  auto accumulate = [&](int t, f32x16* s) {
+    const int k0 = t * KT;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int key = k0 + kb * 32 + (e >> 2) * 8 + g * 4 + (e & 3);
-        s[kb][e] = key < sees ? s[kb][e] * a.scale_log2 : -INFINITY;
-        mx = fmaxf(mx, s[kb][e]);
-      }
-    mx = fmaxf(m, fmaxf(mx, __shfl_xor(mx, 32, 64)));
-    const float base = mx == -INFINITY ? 0.0f : mx;   // a query that has seen no key yet
-    const float alpha = __builtin_amdgcn_exp2f(m - base);
-    m = mx;
-    l *= alpha;
+      for (int e = 0; e < 16; ++e) s[kb][e] = fmaf(s[kb][e], a.scale_log2, -m);
+    if (k0 + KT > fewest) {
 #pragma unroll
-    for (int hb = 0; hb < HB; ++hb)
+      for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) o[hb][e] *= alpha;
+        for (int e = 0; e < 16; ++e)
+          if (k0 + kb * 32 + (e >> 2) * 8 + g * 4 + (e & 3) >= sees) s[kb][e] = -INFINITY;
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[kb][e]);
+    {   // the query's other half of the keys is in lane ^ 32
+      const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+      mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+    }
+    const bool need = t == 0 ? mx > -INFINITY : mx > 8.0f;   // a query that sees nothing keeps m = 0, l = 0
+    if (__any(need)) {
+      const float d = need ? mx : 0.0f;
+      const float alpha = t == 0 ? 0.0f : __builtin_amdgcn_exp2f(-d);
+      m += d;
+      l *= alpha;
+#pragma unroll
+      for (int hb = 0; hb < C::HB; ++hb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[hb][e] *= alpha;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[kb][e] -= d;
+    }
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int ch = 0; ch < 2; ++ch) {
         x8 p;
+        float sum = 0.0f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float x = __builtin_amdgcn_exp2f(s[kb][8 * ch + e] - base);
-          l += x;
+          const float x = __builtin_amdgcn_exp2f(s[kb][8 * ch + e]);
+          sum = e ? sum + x : x;
           p[e] = (T)x;
         }
+        l += sum;
 #pragma unroll
-        for (int hb = 0; hb < HB; ++hb) {
-          const T* t = Vt + (hb * 32 + l32) * LDV + kb * 32 + ch * 16 + 4 * g;
-          union { x8 v; uint2 u[2]; } va;
-          va.u[0] = *reinterpret_cast<const uint2*>(t);
-          va.u[1] = *reinterpret_cast<const uint2*>(t + 8);
-          o[hb] = Mfma<T>::go(va.v, p, o[hb]);
+        for (int hb = 0; hb < C::HB; ++hb) {
+          union { x8 v; v4i16 h[2]; } u;
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
+            u.h[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (lds_v4i16*)(lds + (2 + (t & 1)) * C::TILE + (kb * 32 + 16 * ch) * HD * 2 + vofs[hb][half]));
+          o[hb] = Mfma<T>::go(u.v, p, o[hb]);
         }
       }
+  };
+
+  // Tile t's softmax and the next tile's scores are independent, so the vector and matrix units overlap.
+  auto step = [&](int t, f32x16* now, f32x16* next) {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // keys t + 1 and values t are there
+    __syncthreads();                                              // and keys t and values t - 1 read by all
+    if (t + 2 < nt) fetch_k(t + 2);
+    if (t + 1 < nt) fetch_v(t + 1);
+    if (t + 1 < nt_w) scores(t + 1, next);
+    if (t < nt_w) accumulate(t, now);
+  };
+  if (nt > 0) {
+    f32x16 sa[2], sb[2];
+    fetch_k(0);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    fetch_v(0);
+    if (nt > 1) fetch_k(1);
+    if (nt_w > 0) scores(0, sa);
+    for (int t = 0; t < nt; t += 2) {
+      step(t, sa, sb);
+      if (t + 1 < nt) step(t + 1, sb, sa);
+    }
   }
 
-  l += __shfl_xor(l, 32, 64);
   T* first = static_cast<T*>(a.out) + w.cu_q[r] * a.os.row + h * a.os.head;
   float* first_lse = a.lse ? a.lse + (long)w.cu_q[r] * a.heads + h : nullptr;
-  if (a.causal && any_not_finite<HB>(o)) {
-    careful_rows<T, HD>(a, qp, kp, vp, lq, lk, q0 + wave * 32, first, first_lse);
+  // every wave is past its last read: the tiles' memory now stages each wave's 32 x HD results, chunks of row r
+  // rotated by r, so that the stores are of whole rows
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (qw >= lq) return;
+  if (a.causal && any_not_finite<C::HB>(o)) {
+    careful_rows<T, HD>(a, qp, kp, vp, lq, lk, qw, first, first_lse);
     return;
   }
-  if (qi >= lq) return;
+  l += __shfl_xor(l, 32, 64);
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  T* out = first + qi * a.os.row;
+  if (first_lse && g == 0 && qi < lq)
+    first_lse[(long)qi * a.heads] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
+  char* stage = smem + wave * 32 * HD * 2;
 #pragma unroll
-  for (int hb = 0; hb < HB; ++hb)
+  for (int hb = 0; hb < C::HB; ++hb)
 #pragma unroll
     for (int e4 = 0; e4 < 4; ++e4) {
       union { uint2 u; T e[4]; } st;
 #pragma unroll
       for (int e = 0; e < 4; ++e) st.e[e] = (T)(o[hb][e4 * 4 + e] * inv);
-      *reinterpret_cast<uint2*>(out + hb * 32 + e4 * 8 + g * 4) = st.u;
+      *reinterpret_cast<uint2*>(stage + l32 * HD * 2 + (hb * 4 + e4 + l32) % C::R * 16 + g * 8) = st.u;
     }
-  if (first_lse && g == 0) first_lse[(long)qi * a.heads] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+  for (int k = 0; k < C::R / 2; ++k) {
+    const int c = lane + 64 * k, row = c / C::R, ch = c % C::R;
+    const uint4 x = *reinterpret_cast<const uint4*>(stage + row * HD * 2 + (ch + row) % C::R * 16);
+    if (qw + row < lq) *reinterpret_cast<uint4*>(first + (qw + row) * a.os.row + ch * 8) = x;
+  }
+}
+
+template <class T, int HD, int NW>
+eas_status launch(const PromptArgs& a, const PromptWork& w, unsigned grid, hipStream_t s) {
+  constexpr int lds = 4 * Cfg<HD, NW>::TILE;
+  hipLaunchKernelGGL((prompt_kernel<T, HD, NW>), dim3(grid), dim3(64 * NW), lds, s, a, w);
+  return hipGetLastError() == hipSuccess ? EAS_OK : EAS_ERR_HIP;
 }
 
 eas_status check_cu(const int32_t* cu, int32_t n) {
@@ -249,28 +364,26 @@ extern "C" eas_status eas_prompt_attention(const eas_attn_shape* shape, const vo
   if (!q || !out || !aligned16(q) || !aligned16(out) || (uintptr_t)lse % 4) return EAS_ERR_INVALID_ARG;
   if (cu_k[n_seqs] > 0 && (!k || !v || !aligned16(k) || !aligned16(v))) return EAS_ERR_INVALID_ARG;
 
+  const int qt = 256;
   PromptWork w = {};
   w.n = n_seqs;
   int64_t tiles = 0;
   for (int r = 0; r < n_seqs; ++r) {
     w.order[r] = r;
     w.tile_start[r] = (int)tiles;
-    tiles += ((int64_t)cu_q[r + 1] - cu_q[r] + QT - 1) / QT;
+    tiles += ((int64_t)cu_q[r + 1] - cu_q[r] + qt - 1) / qt;
   }
   w.tile_start[n_seqs] = (int)tiles;
   for (int r = 0; r <= n_seqs; ++r) w.cu_q[r] = cu_q[r], w.cu_k[r] = cu_k[r];
   if (tiles * shape->heads > 0x7fffffff) return EAS_ERR_UNSUPPORTED;
   const PromptArgs a = {q, k, v, out, lse, shape->q, shape->k, shape->v, shape->out, shape->heads,
                         shape->heads / shape->kv_heads, shape->causal, shape->scale * kLog2e};
-  const dim3 grid((unsigned)(tiles * shape->heads));
-  const hipStream_t s = (hipStream_t)stream;
-  if (shape->dtype == EAS_BF16 && shape->head_dim == 64)
-    hipLaunchKernelGGL((prompt_kernel<bf16, 64>), grid, dim3(256), 0, s, a, w);
-  else if (shape->dtype == EAS_BF16)
-    hipLaunchKernelGGL((prompt_kernel<bf16, 128>), grid, dim3(256), 0, s, a, w);
-  else if (shape->head_dim == 64)
-    hipLaunchKernelGGL((prompt_kernel<f16, 64>), grid, dim3(256), 0, s, a, w);
-  else
-    hipLaunchKernelGGL((prompt_kernel<f16, 128>), grid, dim3(256), 0, s, a, w);
-  return hipGetLastError() == hipSuccess ? EAS_OK : EAS_ERR_HIP;
+  const unsigned grid = (unsigned)(tiles * shape->heads);
+  const hipStream_t st_ = (hipStream_t)stream;
+  if (shape->dtype == EAS_BF16) {
+    if (shape->head_dim == 64) return launch<bf16, 64, 8>(a, w, grid, st_);
+    return launch<bf16, 128, 8>(a, w, grid, st_);
+  }
+  if (shape->head_dim == 64) return launch<f16, 64, 8>(a, w, grid, st_);
+  return launch<f16, 128, 8>(a, w, grid, st_);
 }
