@@ -5,9 +5,9 @@ shapes, devices); PyTorch supplies device memory and the stream.
 All tensors of a call are on the current device.  Work is enqueued on ``stream`` (a torch stream; None: the
 current one); tensors made here are known to it, the caller's own are kept alive by the caller.
 """
+import array
 import ctypes
 
-import numpy as np
 import torch
 
 from .eas import EAS_MAX_SEQS, EAS_OK, LIB, EasError  # noqa: F401  (EAS_MAX_SEQS: the most packed prompts)
@@ -33,8 +33,9 @@ class Kv8CacheStruct(ctypes.Structure):
                 ("k", VP), ("v", VP), ("k_scale", VP), ("v_scale", VP)]
 
 
+_NO_STRIDES = Strides()
 _SIG = {
-    "eas_prompt_attention": [P(AttnShape), VP, VP, VP, P(I32), P(I32), I32, VP, VP, VP],
+    "eas_prompt_attention": [P(AttnShape), VP, VP, VP, VP, VP, I32, VP, VP, VP],
     "eas_kv8_append": [P(Kv8CacheStruct), I32, VP, Strides, VP, Strides, I32, VP, I32, VP, VP, I32, I32, VP],
     "eas_kv8_rows": [P(Kv8CacheStruct), I32, VP, I32, I32, VP, VP, I32, I32, VP, Strides, VP, Strides, VP],
     "eas_kv8_attention": [P(Kv8CacheStruct), P(AttnShape), VP, I32, VP, I32, VP, I32, VP, I32, I32, VP, VP, VP, I64,
@@ -53,31 +54,35 @@ def _check(status, what):
         raise EasError(status, what)
 
 
-def _rows(t, name, heads=None, dim=None, dtype=None, device=None):
-    """[rows, heads, dim] with consecutive dims; its strides."""
-    if t.dim() != 3 or (heads is not None and t.shape[1] != heads) or (dim is not None and t.shape[2] != dim):
-        raise ValueError("%s has shape %s, wanted [rows, %s, %s]" % (name, tuple(t.shape), heads or "heads",
-                                                                     dim or "head_dim"))
-    if (dtype is not None and t.dtype != dtype) or (device is not None and t.device != device):
-        raise ValueError("%s is %s on %s, wanted %s on %s" % (name, t.dtype, t.device, dtype, device))
+_current_stream = torch._C._cuda_getCurrentRawStream   # of a device; torch.cuda.current_stream takes 3 us
+
+
+def _rows(t, name, heads, dim, dtype, index):
+    """Strides of [rows, heads, dim] (heads None: any) with consecutive dims."""
+    shape = t.shape
+    if len(shape) != 3 or shape[2] != dim or (heads is not None and shape[1] != heads):
+        raise ValueError("%s has shape %s, wanted [rows, %s, %d]" % (name, tuple(shape), heads or "heads", dim))
+    if t.dtype != dtype or t.get_device() != index:
+        raise ValueError("%s is %s on %s, wanted %s on cuda:%d" % (name, t.dtype, t.device, dtype, index))
     row, head, one = t.stride()
     if one != 1 and t.numel():
         raise ValueError("%s: the values of a head must be consecutive" % name)
     # a stride that no step is taken by says nothing
-    return Strides(row if t.shape[0] > 1 else 0, head if t.shape[1] > 1 else 0)
+    return Strides(row if shape[0] > 1 else 0, head if shape[1] > 1 else 0)
 
 
 def _device(t):
-    """The calls run on the current device."""
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+    """Index of the tensor's device, which has to be the current one."""
+    index = t.get_device()
+    if index < 0 or index != torch.cuda.current_device():
         raise ValueError("tensors must be on the current CUDA device, got %s" % t.device)
-    return t.device
+    return index
 
 
-def _ints(t, name, device, shape):
-    if t.dtype != torch.int32 or t.device != device or tuple(t.shape) != shape or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous int32 tensor of shape %s on %s, got %s %s on %s"
-                         % (name, shape, device, t.dtype, tuple(t.shape), t.device))
+def _ints(t, name, index, shape):
+    if t.dtype != torch.int32 or t.get_device() != index or t.shape != shape or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous int32 tensor of shape %s on cuda:%d, got %s %s on %s"
+                         % (name, tuple(shape), index, t.dtype, tuple(t.shape), t.device))
     return t.data_ptr()
 
 
@@ -87,45 +92,36 @@ def _dtype(dtype):
     return _DTYPE[dtype]
 
 
-def _scale(scale, dim):
-    return dim ** -0.5 if scale is None else float(scale)
+def _on(stream, make):
+    """make() with its tensors known to ``stream`` (None: the current one)."""
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream):
+        return make()
 
 
-class _On:
-    """The stream of a call, and tensors that it may use."""
-
-    def __init__(self, stream):
-        self.stream = stream
-        self.ptr = (stream if stream is not None else torch.cuda.current_stream()).cuda_stream
-
-    def empty(self, shape, dtype, device):
-        if self.stream is None:
-            return torch.empty(shape, dtype=dtype, device=device)
-        with torch.cuda.stream(self.stream):
-            return torch.empty(shape, dtype=dtype, device=device)
-
-
-def _lse_ptr(lse, rows, heads, device):
-    if lse.dtype != torch.float32 or lse.device != device or tuple(lse.shape) != (rows, heads) \
-            or not lse.is_contiguous():
-        raise ValueError("lse must be a contiguous float32 tensor [%d, %d] on %s" % (rows, heads, device))
-    return lse.data_ptr()
-
-
-def _outputs(on, q, rows, heads, out, lse, with_lse):
-    """The output tensors: the caller's, or new ones."""
+def _outputs(q, out, lse, with_lse, index, stream):
+    """The output tensors -- the caller's, or new ones -- the strides of out, and lse's address."""
+    rows, heads, dim = q.shape
     if out is None:
-        out = on.empty((rows, heads, q.shape[2]), q.dtype, q.device)
+        out = _on(stream, lambda: torch.empty_like(q))
     elif out.shape[0] != rows:
         raise ValueError("out has %d rows, q %d" % (out.shape[0], rows))
-    if lse is None and with_lse:
-        lse = on.empty((rows, heads), torch.float32, q.device)
-    return out, lse, None if lse is None else _lse_ptr(lse, rows, heads, q.device)
+    strides = _rows(out, "out", heads, dim, q.dtype, index)
+    if lse is None:
+        if not with_lse:
+            return out, None, strides, None
+        lse = _on(stream, lambda: torch.empty((rows, heads), dtype=torch.float32, device=q.device))
+    elif lse.dtype != torch.float32 or lse.get_device() != index or lse.shape != (rows, heads) \
+            or not lse.is_contiguous():
+        raise ValueError("lse must be a contiguous float32 tensor [%d, %d] on cuda:%d" % (rows, heads, index))
+    return out, lse, strides, lse.data_ptr()
 
 
 def _cu(cu, rows, name):
-    cu = np.ascontiguousarray(cu, dtype=np.int32)
-    if cu.ndim != 1 or cu.shape[0] < 1 or cu[-1] > rows:
+    """Host prefix sums as an array of C ints."""
+    cu = array.array("i", cu)
+    if not cu or cu[-1] > rows:
         raise ValueError("%s must be [n_seqs + 1] prefix sums of at most %d rows" % (name, rows))
     return cu
 
@@ -137,22 +133,27 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, *, causal=True, scale=None, out=N
     queries and keys (cu_k None: the same).  scale None: head_dim ** -0.5.  Returns (out, lse): out like q, in
     ``out`` where given, rows behind the last sequence untouched; lse [rows, heads] float32 with with_lse or where
     given, else None."""
-    device, dt = _device(q), _dtype(q.dtype)
-    s = AttnShape(dt, q.shape[1] if q.dim() == 3 else 0, k.shape[1] if k.dim() == 3 else 0, q.shape[-1],
-                  1 if causal else 0, _scale(scale, q.shape[-1]))
-    s.q = _rows(q, "q")
-    s.k = _rows(k, "k", None, s.head_dim, q.dtype, device)
-    s.v = _rows(v, "v", s.kv_heads, s.head_dim, q.dtype, device)
-    cu_q = _cu(cu_q, q.shape[0], "cu_q")
-    cu_k = cu_q if cu_k is None else _cu(cu_k, min(k.shape[0], v.shape[0]), "cu_k")
-    if cu_k.shape != cu_q.shape or cu_k[-1] > min(k.shape[0], v.shape[0]):
+    index, dtype = _device(q), q.dtype
+    code = _dtype(dtype)
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q and k must be [rows, heads, head_dim]")
+    rows, heads, dim = q.shape
+    keys, kv_heads = k.shape[0], k.shape[1]
+    cu_q = _cu(cu_q, rows, "cu_q")
+    keys = min(keys, v.shape[0])
+    cu_k = cu_q if cu_k is None else _cu(cu_k, keys, "cu_k")
+    if len(cu_k) != len(cu_q) or cu_k[-1] > keys:
         raise ValueError("cu_q and cu_k: of the same sequences, keys within k and v")
-    on = _On(stream)
-    out, lse, lse_ptr = _outputs(on, q, q.shape[0], s.heads, out, lse, with_lse)
-    s.out = _rows(out, "out", s.heads, s.head_dim, q.dtype, device)
-    _check(LIB.eas_prompt_attention(ctypes.byref(s), q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                                    cu_q.ctypes.data_as(P(I32)), cu_k.ctypes.data_as(P(I32)), cu_q.shape[0] - 1,
-                                    out.data_ptr(), lse_ptr, on.ptr), "prompt_attention")
+    qs = _rows(q, "q", None, dim, dtype, index)
+    ks = _rows(k, "k", None, dim, dtype, index)
+    vs = _rows(v, "v", kv_heads, dim, dtype, index)
+    out, lse, strides, lse_ptr = _outputs(q, out, lse, with_lse, index, stream)
+    shape = AttnShape(code, heads, kv_heads, dim, 1 if causal else 0, dim ** -0.5 if scale is None else scale,
+                      qs, ks, vs, strides)
+    _check(LIB.eas_prompt_attention(shape, q.data_ptr(), k.data_ptr(), v.data_ptr(), cu_q.buffer_info()[0],
+                                    cu_k.buffer_info()[0], len(cu_q) - 1, out.data_ptr(), lse_ptr,
+                                    _current_stream(index) if stream is None else stream.cuda_stream),
+           "prompt_attention")
     return out, lse
 
 
@@ -173,10 +174,9 @@ class Kv8Cache:
                 raise ValueError("%s must be a contiguous %s tensor of shape %s on %s" % (name, dtype, shape, k.device))
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.n_pages, self.kv_heads, self.page_tokens, self.head_dim = n, h, p, d
-        self.device = k.device
+        self.device, self._index = k.device, k.get_device()
         self._c = Kv8CacheStruct(_FORMAT[k.dtype], h, d, p, n, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(),
                                  v_scale.data_ptr())
-        self._ref = ctypes.byref(self._c)
 
     @classmethod
     def empty(cls, n_pages, kv_heads, head_dim, page_tokens=64, dtype=torch.int8, device="cuda"):
@@ -190,14 +190,15 @@ class Kv8Cache:
     def _table(self, pages):
         if pages.dim() != 2:
             raise ValueError("pages must be [n_seqs, max_pages]")
-        if _device(pages) != self.device:
+        if _device(pages) != self._index:
             raise ValueError("pages on %s, the cache on %s" % (pages.device, self.device))
-        return _ints(pages, "pages", self.device, tuple(pages.shape)), pages.shape[1], pages.shape[0]
+        n, max_pages = pages.shape
+        return _ints(pages, "pages", self._index, (n, max_pages)), max_pages, n
 
     def _split(self, cu, most, rows, n, name):
         """(pointer to the prefix sums or None, the most rows of a sequence)"""
         if cu is not None:
-            return _ints(cu, name, self.device, (n + 1,)), rows if most is None else int(most)
+            return _ints(cu, name, self._index, (n + 1,)), rows if most is None else int(most)
         if most is None:
             most = rows // n if n else 0
         if most * n != rows:
@@ -210,14 +211,16 @@ class Kv8Cache:
         of each sequence (eas_kv8_append).  cu_new: int32 device prefix sums of the new tokens; None: the same
         number for all.  max_new: the most of a sequence (None: all rows)."""
         table, max_pages, n = self._table(pages)
-        dt = _dtype(k.dtype)
-        ks = _rows(k, "k", self.kv_heads, self.head_dim, k.dtype, self.device)
-        vs = _rows(v, "v", self.kv_heads, self.head_dim, k.dtype, self.device)
-        if v.shape[0] != k.shape[0]:
-            raise ValueError("k has %d rows, v %d" % (k.shape[0], v.shape[0]))
-        cu, most = self._split(cu_new, max_new, k.shape[0], n, "cu_new")
-        _check(LIB.eas_kv8_append(self._ref, dt, k.data_ptr(), ks, v.data_ptr(), vs, k.shape[0], cu, most,
-                                  _ints(held, "held", self.device, (n,)), table, max_pages, n, _On(stream).ptr),
+        index, dtype, rows = self._index, k.dtype, k.shape[0]
+        code = _dtype(dtype)
+        ks = _rows(k, "k", self.kv_heads, self.head_dim, dtype, index)
+        vs = _rows(v, "v", self.kv_heads, self.head_dim, dtype, index)
+        if v.shape[0] != rows:
+            raise ValueError("k has %d rows, v %d" % (rows, v.shape[0]))
+        cu, most = self._split(cu_new, max_new, rows, n, "cu_new")
+        _check(LIB.eas_kv8_append(self._c, code, k.data_ptr(), ks, v.data_ptr(), vs, rows, cu, most,
+                                  _ints(held, "held", index, (n,)), table, max_pages, n,
+                                  _current_stream(index) if stream is None else stream.cuda_stream),
                "Kv8Cache.append")
 
     def rows(self, pages, cu_rows, n_rows, first=None, max_len=None, dtype=torch.bfloat16, k=None, v=None, stream=None):
@@ -225,19 +228,21 @@ class Kv8Cache:
         the ``n_rows`` receive sequence r's tokens from first[r] (int32 device; None: 0) on.  max_len: the most of a
         sequence (None: n_rows).  Returns (k, v) [n_rows, kv_heads, head_dim]; rows of no sequence are not written."""
         table, max_pages, n = self._table(pages)
-        on = _On(stream)
+        index, code = self._index, _dtype(dtype)
         shape = (int(n_rows), self.kv_heads, self.head_dim)
-        k = on.empty(shape, dtype, self.device) if k is None else k
-        v = on.empty(shape, dtype, self.device) if v is None else v
-        ks = _rows(k, "k", self.kv_heads, self.head_dim, dtype, self.device)
-        vs = _rows(v, "v", self.kv_heads, self.head_dim, dtype, self.device)
+        if k is None:
+            k = _on(stream, lambda: torch.empty(shape, dtype=dtype, device=self.device))
+        if v is None:
+            v = _on(stream, lambda: torch.empty(shape, dtype=dtype, device=self.device))
+        ks = _rows(k, "k", self.kv_heads, self.head_dim, dtype, index)
+        vs = _rows(v, "v", self.kv_heads, self.head_dim, dtype, index)
         if k.shape[0] != shape[0] or v.shape[0] != shape[0]:
             raise ValueError("k has %d rows, v %d, wanted %d" % (k.shape[0], v.shape[0], shape[0]))
-        _check(LIB.eas_kv8_rows(self._ref, _dtype(dtype), table, max_pages, n,
-                                _ints(cu_rows, "cu_rows", self.device, (n + 1,)),
-                                None if first is None else _ints(first, "first", self.device, (n,)),
+        _check(LIB.eas_kv8_rows(self._c, code, table, max_pages, n, _ints(cu_rows, "cu_rows", index, (n + 1,)),
+                                None if first is None else _ints(first, "first", index, (n,)),
                                 shape[0] if max_len is None else int(max_len), shape[0], k.data_ptr(), ks,
-                                v.data_ptr(), vs, on.ptr), "Kv8Cache.rows")
+                                v.data_ptr(), vs, _current_stream(index) if stream is None else stream.cuda_stream),
+               "Kv8Cache.rows")
         return k, v
 
     def attention(self, q, lens, pages, cu_q=None, max_q=None, max_len=None, *, causal=True, scale=None, out=None,
@@ -247,26 +252,28 @@ class Kv8Cache:
         max_len: the most tokens of a sequence (None: what the page table holds).  workspace: a uint8 device tensor
         to use instead of a new one.  Returns (out, lse) as prompt_attention."""
         table, max_pages, n = self._table(pages)
-        dt = _dtype(q.dtype)
-        qs = _rows(q, "q", None, self.head_dim, q.dtype, self.device)
+        index, dtype, dim = self._index, q.dtype, self.head_dim
+        code = _dtype(dtype)
+        qs = _rows(q, "q", None, dim, dtype, index)
         rows, heads = q.shape[0], q.shape[1]
         cu, most_q = self._split(cu_q, max_q, rows, n, "cu_q")
         most = max_pages * self.page_tokens
-        most = most if max_len is None else min(int(max_len), most)
-        on = _On(stream)
-        out, lse, lse_ptr = _outputs(on, q, rows, heads, out, lse, with_lse)
-        s = AttnShape(dt, heads, self.kv_heads, self.head_dim, 1 if causal else 0, _scale(scale, self.head_dim))
-        s.q, s.out = qs, _rows(out, "out", heads, self.head_dim, q.dtype, self.device)
+        if max_len is not None and max_len < most:
+            most = int(max_len)
+        out, lse, strides, lse_ptr = _outputs(q, out, lse, with_lse, index, stream)
+        shape = AttnShape(code, heads, self.kv_heads, dim, 1 if causal else 0, dim ** -0.5 if scale is None else scale,
+                          qs, _NO_STRIDES, _NO_STRIDES, strides)
         need = I64()
-        _check(LIB.eas_kv8_attention_workspace(ctypes.byref(s), most_q, most, n, ctypes.byref(need)),
-               "Kv8Cache.attention")
-        if need.value and workspace is None:
-            workspace = on.empty((need.value,), torch.uint8, self.device)
-        elif workspace is not None and (workspace.dtype != torch.uint8 or workspace.device != self.device
-                                        or not workspace.is_contiguous()):
+        _check(LIB.eas_kv8_attention_workspace(shape, most_q, most, n, need), "Kv8Cache.attention")
+        if workspace is None:
+            if need.value:
+                workspace = _on(stream, lambda: torch.empty((need.value,), dtype=torch.uint8, device=self.device))
+        elif workspace.dtype != torch.uint8 or workspace.get_device() != index or not workspace.is_contiguous():
             raise ValueError("workspace must be a contiguous uint8 tensor on %s" % self.device)
-        _check(LIB.eas_kv8_attention(self._ref, ctypes.byref(s), q.data_ptr(), rows, cu, most_q,
-                                     _ints(lens, "lens", self.device, (n,)), most, table, max_pages, n,
-                                     out.data_ptr(), lse_ptr, None if workspace is None else workspace.data_ptr(),
-                                     0 if workspace is None else workspace.numel(), on.ptr), "Kv8Cache.attention")
+        _check(LIB.eas_kv8_attention(self._c, shape, q.data_ptr(), rows, cu, most_q, _ints(lens, "lens", index, (n,)),
+                                     most, table, max_pages, n, out.data_ptr(), lse_ptr,
+                                     None if workspace is None else workspace.data_ptr(),
+                                     0 if workspace is None else workspace.numel(),
+                                     _current_stream(index) if stream is None else stream.cuda_stream),
+               "Kv8Cache.attention")
         return out, lse
