@@ -28,26 +28,34 @@ namespace {
 
 constexpr int TILE = 64;         // tokens per wave and step
 constexpr int NW = 4;            // waves per workgroup
-constexpr int RUN = NW * TILE;   // smallest run: a tile for each wave
 constexpr int MAX_RUNS = 64;     // runs per sequence
 constexpr int RUN_ROWS = 256;    // runs * queries of a sequence that is split
 
-// Runs that `len` tokens are split into for nq queries, and a run's tokens.
+// Runs that `len` tokens are split into for nq queries, and a run's tokens: 512 at least, 1,024 over 2,048 tokens.
+// A run costs its first loads' latency and its share of the join, so full batches want long ones (64 sequences of
+// 4,096 tokens, 8 heads of 128: 147 us with runs of 256 tokens, 124 with 512, 117 with 1,024; 16 of 32,768: 246 /
+// 221 / 204), single sequences short ones (one of 4,096: 11.2 / 12.6 / 16.1 us).
 __host__ __device__ inline int n_runs(int len, int nq) {
-  const int by_len = (int)(((int64_t)len + RUN - 1) / RUN);
+  const int shortest = len <= 2048 ? 512 : 1024;
+  const int by_len = (int)(((int64_t)len + shortest - 1) / shortest);
   int most = nq > 0 ? RUN_ROWS / nq : 1;
   most = most < 1 ? 1 : most > MAX_RUNS ? MAX_RUNS : most;
   return by_len < 1 ? 1 : by_len < most ? by_len : most;
 }
 __host__ __device__ inline int run_tokens(int len, int runs) {
-  return (int)(((int64_t)len + (int64_t)runs * RUN - 1) / ((int64_t)runs * RUN)) * RUN;
+  constexpr int step = NW * TILE;
+  return (int)(((int64_t)len + (int64_t)runs * step - 1) / ((int64_t)runs * step)) * step;
+}
+// the most runs of a sequence of up to max_len tokens (2,048 have 4, 2,049 have 3)
+inline int most_runs(int max_len) {
+  const int upto = n_runs(max_len < 2048 ? max_len : 2048, 1), over = n_runs(max_len, 1);
+  return upto > over ? upto : over;
 }
 // Workspace slots per sequence and head: at least n_runs * nq for every nq <= max_q, len <= max_len
 // of a sequence that is split
 inline int64_t slots(int max_q, int max_len) {
-  const int64_t by_len = ((int64_t)max_len + RUN - 1) / RUN;
-  const int64_t runs = by_len < 1 ? 1 : by_len < MAX_RUNS ? by_len : MAX_RUNS;
-  return runs * max_q < RUN_ROWS ? runs * max_q : RUN_ROWS;
+  const int64_t rows = (int64_t)most_runs(max_len) * max_q;
+  return rows < RUN_ROWS ? rows : RUN_ROWS;
 }
 
 struct Kv8AttnArgs {
@@ -160,21 +168,38 @@ __global__ __launch_bounds__(64 * NW) void kv8_attention_kernel(Kv8AttnArgs a) {
   const long t_begin = (long)run * each;
   const int t_end = (int)min((long)most, t_begin + each);
 
+  constexpr int STEP = NW * TILE;
+  long t0 = t_begin + wave * TILE;
+  const int page_mask = (1 << a.c.page_shift) - 1;
+  const int* table = a.pages + (long)r * a.max_pages;
+  uint4 kw[4][DX], vw[DB];
+  float ks, vs;
+  int pv, pk;    // pages of the tokens whose scores and values the lane holds, and of those whose keys it loads
+  bool there;    // pv is one
+  const auto find = [&](long t0) {
+    const long tv = t0 + 16 * g, tk = t0 + 16 * (c >> 2);
+    pv = tv < t_end ? table[tv >> a.c.page_shift] : -1;   // t_end <= len <= what the table holds
+    pk = tk < t_end ? table[tk >> a.c.page_shift] : -1;
+  };
+  find(t0);
+  Tx8 qv[2 * DX];
+  {
+    const T* q = static_cast<const T*>(a.q) + (s.row0 + qi) * a.qs.row + h * a.qs.head + 16 * g;
+#pragma unroll
+    for (int x = 0; x < DX; ++x)
+#pragma unroll
+      for (int y = 0; y < 2; ++y) qv[2 * x + y] = *reinterpret_cast<const Tx8*>(q + 64 * x + 8 * y);
+  }
+
   // queries times a power of two that brings the row's largest to [2^14, 2^15)
   f16x8 qf[2 * DX];
   float q_scale;
   {
-    const T* q = static_cast<const T*>(a.q) + (s.row0 + qi) * a.qs.row + h * a.qs.head;
-    Tx8 v[2 * DX];
     float top = 0.0f;
 #pragma unroll
-    for (int x = 0; x < DX; ++x)
+    for (int i = 0; i < 2 * DX; ++i)
 #pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        v[2 * x + y] = *reinterpret_cast<const Tx8*>(q + 64 * x + 16 * g + 8 * y);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)v[2 * x + y][e]));
-      }
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)qv[i][e]));
     top = column_max(top);
     // 2^(14 - floor(log2 top)), kept in the normal range
     const int e = min(max((int)(__float_as_uint(top) >> 23), 15), 254);
@@ -183,7 +208,7 @@ __global__ __launch_bounds__(64 * NW) void kv8_attention_kernel(Kv8AttnArgs a) {
 #pragma unroll
     for (int i = 0; i < 2 * DX; ++i)
 #pragma unroll
-      for (int e8 = 0; e8 < 8; ++e8) qf[i][e8] = (f16)((float)v[i][e8] * up);
+      for (int e8 = 0; e8 < 8; ++e8) qf[i][e8] = (f16)((float)qv[i][e8] * up);
   }
 
   f32x4 o[DB];
@@ -191,50 +216,73 @@ __global__ __launch_bounds__(64 * NW) void kv8_attention_kernel(Kv8AttnArgs a) {
   for (int i = 0; i < DB; ++i) o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   float m = -INFINITY, mv = -INFINITY, l = 0.0f;
 
-  const int page_mask = (1 << a.c.page_shift) - 1;
-  const int* table = a.pages + (long)r * a.max_pages;
-  for (long t0 = t_begin + wave * TILE; t0 < t_end; t0 += NW * TILE) {
-    // pages of the 16 tokens whose scores and values this lane holds, and of those whose keys it loads
-    const int tv = (int)t0 + 16 * g, tk = (int)t0 + 16 * (c >> 2);
-    int pv = tv < s.len ? table[tv >> a.c.page_shift] : -1;
-    int pk = tk < s.len ? table[tk >> a.c.page_shift] : -1;
-    const bool there = pv >= 0 && pv < a.c.n_pages;
-    pv = there ? pv : 0;
-    pk = pk >= 0 && pk < a.c.n_pages ? pk : 0;
-    const long bv = (long)pv * a.c.kv_heads + kvh, bk = (long)pk * a.c.kv_heads + kvh;
-    const uint8_t* kp = a.c.k + ((bk << a.c.page_shift) + (tk & page_mask) + (c & 3)) * D + 16 * g;
-    const uint8_t* vp = a.c.v + (((bv * D) + c) << a.c.page_shift) + (tv & page_mask);
-    const float ks = a.c.k_scale[bv], vs = a.c.v_scale[bv];
-    uint4 kw[4][DX], vw[DB];
+  // The next tile's keys are fetched as soon as a tile's scores have taken theirs, its values behind the products
+  // with this tile's, its page numbers a tile before: loads are in flight all the time, in one tile's registers.
+  // Lane (c, g) holds scores and values of tokens t0 + 16 g .. + 16, and loads keys of tokens
+  // t0 + 16 (c / 4) + 4 i + c % 4, i < 4.
+  const auto load_k = [&](long t0) {
+    const int tk = (int)t0 + 16 * (c >> 2);
+    const long block = (long)(pk >= 0 && pk < a.c.n_pages ? pk : 0) * a.c.kv_heads + kvh;
+    const uint8_t* kp = a.c.k + ((block << a.c.page_shift) + (tk & page_mask) + (c & 3)) * D + 16 * g;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int x = 0; x < DX; ++x) kw[i][x] = *reinterpret_cast<const uint4*>(kp + 4 * i * D + 64 * x);
+  };
+  const auto load_v = [&](long t0, int page) {
+    const int tv = (int)t0 + 16 * g;
+    const long block = (long)(page >= 0 && page < a.c.n_pages ? page : 0) * a.c.kv_heads + kvh;
+    const uint8_t* vp = a.c.v + (((block * D) + c) << a.c.page_shift) + (tv & page_mask);
 #pragma unroll
-    for (int i = 0; i < DB; ++i)
-      vw[i] = *reinterpret_cast<const uint4*>(vp + ((long)16 * i << a.c.page_shift));
+    for (int i = 0; i < DB; ++i) vw[i] = *reinterpret_cast<const uint4*>(vp + ((long)16 * i << a.c.page_shift));
+  };
+  const auto load_scales = [&](float* k, float* v) {
+    const long block = (long)(pv >= 0 && pv < a.c.n_pages ? pv : 0) * a.c.kv_heads + kvh;
+    *k = a.c.k_scale[block];
+    *v = a.c.v_scale[block];
+  };
 
-    // scores of tokens tv + 4 i + e of this lane's query, in log2 units
-    float x[16];
-    const float ck = q_scale * ks;
-    const int left = there ? sees - tv : 0;   // of the lane's 16 tokens, those its query sees
+  if (t0 < t_end) {
+    load_k(t0);
+    load_scales(&ks, &vs);
+    load_v(t0, pv);
+    there = pv >= 0 && pv < a.c.n_pages;
+    find(t0 + STEP);
+  }
+  for (; t0 < t_end; t0 += STEP) {
+    const int tv = (int)t0 + 16 * g;
+    const bool more = t0 + STEP < t_end;
+    // scores of tokens tv + 4 i + e of this lane's query
+    f32x4 sc[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      f32x4 sc = {0.0f, 0.0f, 0.0f, 0.0f};
+      sc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int d = 0; d < DX; ++d) {
         f16x8 k0, k1;
         codes_to_f16<FORMAT>(kw[i][d], &k0, &k1);
-        sc = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, qf[2 * d], sc, 0, 0, 0);
-        sc = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, qf[2 * d + 1], sc, 0, 0, 0);
+        sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, qf[2 * d], sc[i], 0, 0, 0);
+        sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, qf[2 * d + 1], sc[i], 0, 0, 0);
       }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[4 * i + e] = 4 * i + e < left ? sc[e] * ck : -INFINITY;
     }
+    const float ck = q_scale * ks;
+    const float f = vs > 0.0f ? (float)((int)(__float_as_uint(vs) >> 23) - 127) : -INFINITY;
+    const int left = there ? sees - tv : 0;       // of the lane's 16 tokens, those its query sees
+    const int held = there ? s.len - tv : 0;      // places behind the last token may hold anything
+    const int page_next = pv;
+    there = pv >= 0 && pv < a.c.n_pages;
+    if (more) {
+      load_k(t0 + STEP);
+      load_scales(&ks, &vs);
+      find(t0 + 2 * STEP);
+    }
+    // in log2 units
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = i < left ? sc[i >> 2][i & 3] * ck : -INFINITY;
     float top = x[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
-    const float f = vs > 0.0f ? (float)((int)(__float_as_uint(vs) >> 23) - 127) : -INFINITY;
     const float top_m = column_max(top), top_v = column_max(top + f);
     if (__any(top_m > m)) {
       const float up = fmaxf(m, top_m);
@@ -250,15 +298,14 @@ __global__ __launch_bounds__(64 * NW) void kv8_attention_kernel(Kv8AttnArgs a) {
     }
     // p = 2^(x - m); a code's weight is p 2^(m + f - m')
     const float m0 = m == -INFINITY ? 0.0f : m, mv0 = mv == -INFINITY ? 0.0f : mv;
-    const float w = f == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(fminf(m0 + f - mv0, 126.0f));
+    const float weight = f == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(fminf(m0 + f - mv0, 126.0f));
     f16x8 p[2];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const float e = __builtin_amdgcn_exp2f(x[i] - m0);
       l += e;
-      p[i >> 3][i & 7] = (f16)(e * w);
+      p[i >> 3][i & 7] = (f16)(e * weight);
     }
-    const int held = there ? s.len - tv : 0;   // places behind the last token may hold anything
     const bool ragged = __any(held < 16);
 #pragma unroll
     for (int i = 0; i < DB; ++i) {
@@ -268,6 +315,7 @@ __global__ __launch_bounds__(64 * NW) void kv8_attention_kernel(Kv8AttnArgs a) {
       o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[0], o[i], 0, 0, 0);
       o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[1], o[i], 0, 0, 0);
     }
+    if (more) load_v(t0 + STEP, page_next);
   }
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
@@ -336,11 +384,21 @@ __global__ __launch_bounds__(64 * NW) void kv8_join_kernel(Kv8AttnArgs a) {
   const float w = __builtin_amdgcn_exp2f(lse2 - M0);
   const float W = wave_sum(w), inv = W == 0.0f ? 0.0f : 1.0f / W;
   constexpr int E = D / 64;
+  // runs in order, eight loads in flight; behind the last one the last again, with weight 0
   float sum[E] = {};
-  for (int k = 0; k < runs; ++k) {
-    const float wk = __shfl(w, k, 64);
+  for (int k = 0; k < runs; k += 8) {
+    float x[8][E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) sum[e] += wk * a.part[(slot + k) * D + lane * E + e];
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[i][e] = a.part[(slot + min(k + i, runs - 1)) * D + lane * E + e];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float wk = __shfl(w, min(k + i, 63), 64);
+      if (k + i < runs)
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum[e] += wk * x[i][e];
+    }
   }
   T* out = static_cast<T*>(a.out) + (s.row0 + q) * a.os.row + h * a.os.head + lane * E;
 #pragma unroll
@@ -368,7 +426,7 @@ extern "C" eas_status eas_kv8_attention_workspace(const eas_attn_shape* shape, i
   const eas_status st = check_shape(shape);
   if (st != EAS_OK) return st;
   if (max_q < 0 || max_len < 0 || n_seqs < 0 || !bytes) return EAS_ERR_INVALID_ARG;
-  *bytes = max_len <= RUN ? 0 : (int64_t)n_seqs * shape->heads * slots(max_q, max_len) * (shape->head_dim + 1) * 4;
+  *bytes = most_runs(max_len) == 1 ? 0 : (int64_t)n_seqs * shape->heads * slots(max_q, max_len) * (shape->head_dim + 1) * 4;
   return EAS_OK;
 }
 
@@ -402,7 +460,8 @@ extern "C" eas_status eas_kv8_attention(const eas_kv8_cache* cache, const eas_at
   if (!cu_q) a.max_q = max_q;   // a sequence's rows start at multiples of it
   const int64_t held = (int64_t)max_pages * cache->page_tokens;
   a.max_len = max_len < held ? max_len : (int)held;
-  const bool join = a.max_len > RUN;
+  a.runs = most_runs(a.max_len);
+  const bool join = a.runs > 1;
   a.slots = (int)slots(a.max_q, a.max_len);
   if (join) {
     const int64_t parts = (int64_t)n_seqs * a.heads * a.slots;
@@ -413,7 +472,6 @@ extern "C" eas_status eas_kv8_attention(const eas_kv8_cache* cache, const eas_at
   }
   const int group = a.heads / a.c.kv_heads;
   const int64_t tiles = ((int64_t)(a.max_q < n_rows ? a.max_q : n_rows) * group + 15) / 16;
-  a.runs = n_runs(a.max_len, 1);
   const int64_t blocks = tiles * a.runs * a.c.kv_heads * n_seqs;
   if (tiles > 0x7fffffff || blocks > 0x7fffffff || (int64_t)n_seqs * a.max_q * a.heads > 0x7fffffff)
     return EAS_ERR_UNSUPPORTED;

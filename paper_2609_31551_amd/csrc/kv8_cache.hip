@@ -1,14 +1,15 @@
 // The 8-bit key / value cache: append and rows (include/eas_attention.h).
 //
-// A workgroup owns one block -- a page's tokens of one head -- of one sequence, in
-// both calls, so nothing is shared between workgroups and no order matters.  Both are
-// bound by HBM: an append reads 2 bytes and writes 1 for each value, rows the reverse.
+// Both are bound by HBM: an append reads 2 bytes and writes 1 for each value, rows the reverse.  So every value is
+// read once, in registers, and all loads of a workgroup are issued before the first is used.  An append's
+// workgroup owns one block -- a page's tokens of one head --, so nothing is shared between workgroups and no order
+// matters; rows are taken 64 tokens of a head at a time.  Value codes are stored dimension by dimension: a thread
+// takes 4 tokens of 8 dimensions and turns the 4 x 4 bytes in registers, so both sides move by 16 and 4 bytes.
 #include "attention_ops.h"
 
 namespace eas {
 namespace {
 
-constexpr int NT = 256;
 
 struct AppendArgs {
   Kv8Args c;
@@ -52,80 +53,145 @@ __device__ __forceinline__ bool find_span(const AppendArgs& a, int r, int b, Spa
   return true;
 }
 
-__device__ __forceinline__ float group_max(float v, float* red) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+// Byte j of word i becomes byte i of word j.
+__device__ __forceinline__ void turn4(const uint32_t* w, uint32_t* t) {
+  const uint32_t a = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), b = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u);
+  const uint32_t c = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u), d = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+  t[0] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+  t[1] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+  t[2] = __builtin_amdgcn_perm(d, c, 0x05040100u);
+  t[3] = __builtin_amdgcn_perm(d, c, 0x07060302u);
 }
 
-// One block of keys (TURNED false: codes [page][D]) or values (codes [D][page]).
-template <class T, int FORMAT, int D, bool TURNED>
-__device__ void append_block(const AppendArgs& a, const Span& s, int h, const T* x, const eas_strides& st,
-                             uint8_t* codes, float* scales, float* red) {
-  typedef T Tx8 __attribute__((ext_vector_type(8)));
-  const int page = 1 << a.c.page_shift, chunks = (s.hi - s.lo) * (D / 8);
-  const long block = (long)s.page * a.c.kv_heads + h;
-  codes += block << (a.c.page_shift + (D == 64 ? 6 : 7));
-  x += s.row * st.row + h * st.head;
-  float top = 0.0f;
-  for (int i = threadIdx.x; i < chunks; i += NT) {
-    const Tx8 v = *reinterpret_cast<const Tx8*>(x + (long)(i / (D / 8)) * st.row + i % (D / 8) * 8);
+// The earlier tokens' codes of a block to a larger step (ratio = old scale / new), token t's code of dimension d at
+// t * token_step + d * dim_step.
+template <int FORMAT, int D, int NT>
+__device__ void rescale_codes(uint8_t* codes, int tokens, int token_step, int dim_step, float ratio) {
+  for (int i = threadIdx.x; i < tokens * (D / 4); i += NT) {
+    uint8_t* p = codes + i % tokens * token_step + i / tokens * 4 * dim_step;
+    float y[4];
+    unpack_codes<FORMAT>(p[0] | p[dim_step] << 8 | p[2 * dim_step] << 16 | (uint32_t)p[3 * dim_step] << 24, y);
+    const uint32_t w = pack_codes<FORMAT>(y[0] * ratio, y[1] * ratio, y[2] * ratio, y[3] * ratio);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) top = fmaxf(top, finite_magnitude(v[e]));
-  }
-  top = group_max(top, red);
-  const float before = s.lo > 0 ? scales[block] : 0.0f;
-  const float scale = fmaxf(before, block_scale<FORMAT>(top)), inv = inverse_scale(scale);
-  __syncthreads();   // every thread has read the old scale
-  if (threadIdx.x == 0) scales[block] = scale;
-  if (scale > before && before > 0.0f) {   // the earlier tokens' codes to the larger step
-    const float ratio = before * inv;
-    for (int i = threadIdx.x; i < s.lo * (D / 4); i += NT) {
-      uint8_t* p;
-      int step;
-      if (TURNED) {
-        p = codes + ((i / s.lo * 4) << a.c.page_shift) + i % s.lo;
-        step = page;
-      } else {
-        p = codes + i * 4;
-        step = 1;
-      }
-      float y[4];
-      unpack_codes<FORMAT>(p[0] | p[step] << 8 | p[2 * step] << 16 | (uint32_t)p[3 * step] << 24, y);
-      const uint32_t w = pack_codes<FORMAT>(y[0] * ratio, y[1] * ratio, y[2] * ratio, y[3] * ratio);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) p[e * step] = (uint8_t)(w >> 8 * e);
-    }
-  }
-  for (int i = threadIdx.x; i < chunks; i += NT) {
-    const int t = i / (D / 8), d = i % (D / 8) * 8;
-    const Tx8 v = *reinterpret_cast<const Tx8*>(x + (long)t * st.row + d);
-#pragma unroll
-    for (int e = 0; e < 8; e += 4) {
-      const uint32_t w = pack_codes<FORMAT>((float)v[e] * inv, (float)v[e + 1] * inv, (float)v[e + 2] * inv,
-                                            (float)v[e + 3] * inv);
-      if (TURNED) {
-#pragma unroll
-        for (int f = 0; f < 4; ++f)
-          codes[((d + e + f) << a.c.page_shift) + s.lo + t] = (uint8_t)(w >> 8 * f);
-      } else {
-        *reinterpret_cast<uint32_t*>(codes + (s.lo + t) * D + d + e) = w;
-      }
-    }
+    for (int e = 0; e < 4; ++e) p[e * dim_step] = (uint8_t)(w >> 8 * e);
   }
 }
 
-template <class T, int FORMAT, int D>
+// A workgroup of NT threads takes up to NT * IT 16-byte pieces of keys, and as many of values: a whole page's, or
+// with FEW those of up to FEW_TOKENS tokens.
+constexpr int FEW_TOKENS = 4;
+template <class T, int FORMAT, int D, int NT, int IT, bool FEW>
 __global__ __launch_bounds__(NT) void kv8_append_kernel(AppendArgs a) {
-  __shared__ float red[4];
+  typedef T Tx8 __attribute__((ext_vector_type(8)));
+  constexpr int C = D / 8;               // 16-byte pieces of a row
+  constexpr int IV = (IT + 3) / 4;       // a thread's values: 4 tokens of a piece each
+  __shared__ float red[2][NT / 64];
   Span s;
   if (!find_span(a, blockIdx.x / a.blocks, blockIdx.x % a.blocks, &s)) return;
-  const int h = blockIdx.y;
-  append_block<T, FORMAT, D, false>(a, s, h, static_cast<const T*>(a.k), a.ks, a.c.k, a.c.k_scale, red);
-  append_block<T, FORMAT, D, true>(a, s, h, static_cast<const T*>(a.v), a.vs, a.c.v, a.c.v_scale, red);
+  const int h = blockIdx.y, tid = threadIdx.x, shift = a.c.page_shift;
+  const long block = (long)s.page * a.c.kv_heads + h;
+  uint8_t* kc = a.c.k + (block << shift) * D;
+  uint8_t* vc = a.c.v + (block << shift) * D;
+  // row of the page's token 0
+  const T* kx = static_cast<const T*>(a.k) + (s.row - s.lo) * a.ks.row + h * a.ks.head;
+  const T* vx = static_cast<const T*>(a.v) + (s.row - s.lo) * a.vs.row + h * a.vs.head;
+  const float k_old = s.lo > 0 ? a.c.k_scale[block] : 0.0f, v_old = s.lo > 0 ? a.c.v_scale[block] : 0.0f;
+
+  Tx8 k[IT], v[IV][4];
+#pragma unroll
+  for (int i = 0; i < IT; ++i) {
+    const int c = tid + NT * i, t = s.lo + c / C;
+    if (t < s.hi) k[i] = *reinterpret_cast<const Tx8*>(kx + (long)t * a.ks.row + c % C * 8);
+  }
+  // values: the page's 4-token groups from g0 on, group c % groups of piece c / groups
+  const int glog = FEW ? 1 : shift - 2, groups = 1 << glog, g0 = FEW ? s.lo >> 2 : 0;
+#pragma unroll
+  for (int i = 0; i < IV; ++i) {
+    const int c = tid + NT * i, t = (g0 + (c & (groups - 1))) * 4, d = (c >> glog) * 8;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (d < D && t + j >= s.lo && t + j < s.hi)
+        v[i][j] = *reinterpret_cast<const Tx8*>(vx + (long)(t + j) * a.vs.row + d);
+  }
+  float k_top = 0.0f, v_top = 0.0f;
+#pragma unroll
+  for (int i = 0; i < IT; ++i)
+    if (s.lo + (tid + NT * i) / C < s.hi)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) k_top = fmaxf(k_top, finite_magnitude(k[i][e]));
+#pragma unroll
+  for (int i = 0; i < IV; ++i) {
+    const int c = tid + NT * i, t = (g0 + (c & (groups - 1))) * 4, d = (c >> glog) * 8;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (d < D && t + j >= s.lo && t + j < s.hi)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v_top = fmaxf(v_top, finite_magnitude(v[i][j][e]));
+  }
+#pragma unroll
+  for (int o = 32; o; o >>= 1) {
+    k_top = fmaxf(k_top, __shfl_xor(k_top, o, 64));
+    v_top = fmaxf(v_top, __shfl_xor(v_top, o, 64));
+  }
+  if ((tid & 63) == 0) {
+    red[0][tid >> 6] = k_top;
+    red[1][tid >> 6] = v_top;
+  }
+  __syncthreads();   // every thread has read the old scales, too
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) {
+    k_top = fmaxf(k_top, red[0][w]);
+    v_top = fmaxf(v_top, red[1][w]);
+  }
+  const float k_scale = fmaxf(k_old, block_scale<FORMAT>(k_top)), v_scale = fmaxf(v_old, block_scale<FORMAT>(v_top));
+  const float k_inv = inverse_scale(k_scale), v_inv = inverse_scale(v_scale);
+  if (tid == 0) {
+    a.c.k_scale[block] = k_scale;
+    a.c.v_scale[block] = v_scale;
+  }
+  if (k_scale > k_old && k_old > 0.0f) rescale_codes<FORMAT, D, NT>(kc, s.lo, D, 1, k_old * k_inv);
+  if (v_scale > v_old && v_old > 0.0f) rescale_codes<FORMAT, D, NT>(vc, s.lo, 1, 1 << shift, v_old * v_inv);
+
+  const auto codes = [](Tx8 x, float inv, uint32_t* w) {
+    w[0] = pack_codes<FORMAT>((float)x[0] * inv, (float)x[1] * inv, (float)x[2] * inv, (float)x[3] * inv);
+    w[1] = pack_codes<FORMAT>((float)x[4] * inv, (float)x[5] * inv, (float)x[6] * inv, (float)x[7] * inv);
+  };
+#pragma unroll
+  for (int i = 0; i < IT; ++i) {
+    const int c = tid + NT * i, t = s.lo + c / C;
+    if (t < s.hi) {
+      uint32_t w[2];
+      codes(k[i], k_inv, w);
+      *reinterpret_cast<uint2*>(kc + t * D + c % C * 8) = make_uint2(w[0], w[1]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < IV; ++i) {
+    const int c = tid + NT * i, t = (g0 + (c & (groups - 1))) * 4, d = (c >> glog) * 8;
+    if (d >= D || t + 3 < s.lo || t >= s.hi) continue;
+    uint32_t w[2][4], x[2][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      uint32_t y[2] = {0, 0};
+      if (t + j >= s.lo && t + j < s.hi) codes(v[i][j], v_inv, y);
+      w[0][j] = y[0];
+      w[1][j] = y[1];
+    }
+    turn4(w[0], x[0]);
+    turn4(w[1], x[1]);
+    uint8_t* p = vc + (d << shift) + t;
+    const bool whole = t >= s.lo && t + 4 <= s.hi;
+#pragma unroll
+    for (int e = 0; e < 8; ++e, p += 1 << shift) {
+      if (whole) {
+        *reinterpret_cast<uint32_t*>(p) = x[e >> 2][e & 3];
+      } else {   // other tokens' codes stay
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (t + j >= s.lo && t + j < s.hi) p[j] = (uint8_t)(x[e >> 2][e & 3] >> 8 * j);
+      }
+    }
+  }
 }
 
 struct RowsArgs {
@@ -136,56 +202,109 @@ struct RowsArgs {
   const int* cu;
   const int* first;
   const int* pages;
-  int n_rows, max_rows, max_pages, blocks;   // blocks: pages that one sequence's rows can touch
+  int n_rows, max_rows, max_pages, blocks;   // blocks: SPAN-token spans that one sequence's rows can touch
 };
+
+constexpr int SPAN = 64;   // tokens per workgroup
+constexpr int NT = 256;
 
 template <class T, int FORMAT, int D>
 __global__ __launch_bounds__(NT) void kv8_rows_kernel(RowsArgs a) {
   typedef T Tx8 __attribute__((ext_vector_type(8)));
-  const int r = blockIdx.x / a.blocks, b = blockIdx.x % a.blocks, h = blockIdx.y;
-  const int page = 1 << a.c.page_shift;
+  constexpr int C = D / 8;                         // 8-code pieces of a row
+  constexpr int IK = SPAN * C / NT;                // a thread's pieces of keys
+  constexpr int IV = (SPAN / 4 * C + NT - 1) / NT; // and of values, 4 tokens each
+  const int r = blockIdx.x / a.blocks, b = blockIdx.x % a.blocks, h = blockIdx.y, tid = threadIdx.x;
+  const int shift = a.c.page_shift, mask = (1 << shift) - 1;
   const long row0 = a.cu[r], n = min((long)a.cu[r + 1] - row0, (long)a.max_rows);
   const long first = a.first ? a.first[r] : 0;
-  const long slot = (first >> a.c.page_shift) + b;   // of a sequence that starts below 0, pages below 0 too
-  const long lo = max(first, slot * page), hi = min(first + n, (slot + 1) * page);
+  // tokens of this workgroup; a sequence that starts below 0 has spans below 0 too
+  const long base = (first >= 0 ? first / SPAN : -((-first + SPAN - 1) / SPAN)) * SPAN + (long)b * SPAN;
+  const long lo = max(first, base), hi = min(first + n, base + SPAN);
   if (lo >= hi) return;
-  int id = -1;
-  if (slot >= 0 && slot < a.max_pages) id = a.pages[(long)r * a.max_pages + slot];
-  const bool there = id >= 0 && id < a.c.n_pages;
-  const long block = (long)(there ? id : 0) * a.c.kv_heads + h;
-  const int chunks = (int)(hi - lo) * (D / 8), t0 = (int)(lo - slot * page);
-  const uint8_t* kc = a.c.k + block * page * D;
-  const uint8_t* vc = a.c.v + block * page * D;
-  const float ks = there ? a.c.k_scale[block] : 0.0f, vs = there ? a.c.v_scale[block] : 0.0f;
-  for (int i = threadIdx.x; i < chunks; i += NT) {
-    const int t = i / (D / 8), d = i % (D / 8) * 8;
-    const long row = row0 + (lo - first) + t;
-    if (row < 0 || row >= a.n_rows) continue;
-    if (a.k) {
-      Tx8 o;
+  const auto page_of = [&](long t) {
+    const long slot = t >> shift;
+    const int id = t >= 0 && slot < a.max_pages ? a.pages[(long)r * a.max_pages + slot] : -1;
+    return id >= 0 && id < a.c.n_pages ? id : -1;
+  };
+  // a token's row, if it has one
+  const auto row_of = [&](long t) {
+    const long row = row0 + (t - first);
+    return t >= lo && t < hi && row >= 0 && row < a.n_rows ? row : -1;
+  };
+  uint2 k[IK];
+  float ks[IK];
+  uint32_t v[IV][8];
+  float vs[IV];
+  if (a.k) {
 #pragma unroll
-      for (int e = 0; e < 8; e += 4) {
-        float x[4];
-        unpack_codes<FORMAT>(*reinterpret_cast<const uint32_t*>(kc + (t0 + t) * D + d + e), x);
-#pragma unroll
-        for (int f = 0; f < 4; ++f) o[e + f] = there ? (T)(x[f] * ks) : (T)0.0f;
+    for (int i = 0; i < IK; ++i) {
+      const int c = tid + NT * i;
+      const long t = base + c / C;
+      const int id = row_of(t) >= 0 ? page_of(t) : -1;
+      k[i] = make_uint2(0, 0);   // code 0 in either format
+      ks[i] = 0.0f;
+      if (id >= 0) {
+        const long block = (long)id * a.c.kv_heads + h;
+        ks[i] = a.c.k_scale[block];
+        k[i] = *reinterpret_cast<const uint2*>(a.c.k + ((block << shift) + (t & mask)) * D + c % C * 8);
       }
-      *reinterpret_cast<Tx8*>(static_cast<T*>(a.k) + row * a.ks.row + h * a.ks.head + d) = o;
     }
-    if (a.v) {
-      Tx8 o;
+  }
+  if (a.v) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float x[4];
-        unpack_codes<FORMAT>(vc[((d + e) << a.c.page_shift) + t0 + t], x);
-        o[e] = there ? (T)(x[0] * vs) : (T)0.0f;
+    for (int i = 0; i < IV; ++i) {
+      const int c = tid + NT * i, d = c % C * 8;
+      const long t = base + c / C * 4;
+      const int id = c < SPAN / 4 * C && t + 3 >= lo && t < hi ? page_of(t) : -1;
+      vs[i] = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] = 0;
+      if (id >= 0) {
+        const long block = (long)id * a.c.kv_heads + h;
+        vs[i] = a.c.v_scale[block];
+        const uint8_t* p = a.c.v + ((block * D + d) << shift) + (t & mask);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[i][e] = *reinterpret_cast<const uint32_t*>(p + ((long)e << shift));
       }
-      *reinterpret_cast<Tx8*>(static_cast<T*>(a.v) + row * a.vs.row + h * a.vs.head + d) = o;
+    }
+  }
+  const auto store = [&](T* out, const uint32_t* w, float scale) {
+    float x[8];
+    unpack_codes<FORMAT>(w[0], x);
+    unpack_codes<FORMAT>(w[1], x + 4);
+    Tx8 o;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = (T)(x[e] * scale);
+    *reinterpret_cast<Tx8*>(out) = o;
+  };
+  if (a.k) {
+#pragma unroll
+    for (int i = 0; i < IK; ++i) {
+      const int c = tid + NT * i;
+      const long row = row_of(base + c / C);
+      const uint32_t w[2] = {k[i].x, k[i].y};
+      if (row >= 0) store(static_cast<T*>(a.k) + row * a.ks.row + h * a.ks.head + c % C * 8, w, ks[i]);
+    }
+  }
+  if (a.v) {
+#pragma unroll
+    for (int i = 0; i < IV; ++i) {
+      const int c = tid + NT * i, d = c % C * 8;
+      uint32_t x[2][4];
+      turn4(v[i], x[0]);
+      turn4(v[i] + 4, x[1]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const long row = c < SPAN / 4 * C ? row_of(base + c / C * 4 + j) : -1;
+        const uint32_t w[2] = {x[0][j], x[1][j]};
+        if (row >= 0) store(static_cast<T*>(a.v) + row * a.vs.row + h * a.vs.head + d, w, vs[i]);
+      }
     }
   }
 }
 
-// Pages that `tokens` consecutive tokens can touch, wherever they start
+// Pages (or spans) of `page` tokens that `tokens` consecutive tokens can touch, wherever they start
 int touched(int tokens, int page, int max_pages) {
   const int64_t n = ((int64_t)tokens + page - 2) / page + 1;
   return (int)(n < max_pages ? n : max_pages);
@@ -210,7 +329,21 @@ eas_status by_type(int dtype, int format, int dim, const Args& a, dim3 grid, hip
 template <class T, int F, int D>
 struct LaunchAppend {
   static eas_status go(const AppendArgs& a, dim3 grid, hipStream_t s) {
-    hipLaunchKernelGGL((kv8_append_kernel<T, F, D>), grid, dim3(NT), 0, s, a);
+    // a decoding step's tokens by one wave each (16 sequences 5.0 us, with 256 threads 5.4); small pages
+    // by fewer threads (16,384 tokens in 16-token pages, 8 heads of 64: 17.5 us, with 256 threads 25.6)
+    const int pieces = (D << a.c.page_shift) / 8;
+    if (a.max_new <= FEW_TOKENS)
+      hipLaunchKernelGGL((kv8_append_kernel<T, F, D, 64, 1, true>), grid, dim3(64), 0, s, a);
+    else if (pieces == 128)
+      hipLaunchKernelGGL((kv8_append_kernel<T, F, D, 64, 2, false>), grid, dim3(64), 0, s, a);
+    else if (pieces == 256)
+      hipLaunchKernelGGL((kv8_append_kernel<T, F, D, 64, 4, false>), grid, dim3(64), 0, s, a);
+    else if (pieces == 512)
+      hipLaunchKernelGGL((kv8_append_kernel<T, F, D, 128, 4, false>), grid, dim3(128), 0, s, a);
+    else if (pieces == 1024)
+      hipLaunchKernelGGL((kv8_append_kernel<T, F, D, 256, 4, false>), grid, dim3(256), 0, s, a);
+    else
+      hipLaunchKernelGGL((kv8_append_kernel<T, F, D, 256, 8, false>), grid, dim3(256), 0, s, a);
     return hipGetLastError() == hipSuccess ? EAS_OK : EAS_ERR_HIP;
   }
 };
@@ -264,7 +397,7 @@ extern "C" eas_status eas_kv8_rows(const eas_kv8_cache* cache, int32_t dtype, co
   if (n_rows == 0 || max_rows == 0 || n_seqs == 0) return EAS_OK;
   if (!k && !v) return EAS_ERR_INVALID_ARG;
   RowsArgs a = {kv8_args(cache), k, v, k_strides, v_strides, cu_rows, first, pages, n_rows, max_rows, max_pages,
-                touched(max_rows, cache->page_tokens, 0x7fffffff)};
+                touched(max_rows, SPAN, 0x7fffffff)};
   if ((int64_t)a.blocks * n_seqs > 0x7fffffff) return EAS_ERR_UNSUPPORTED;
   return by_type<LaunchRows>(dtype, cache->format, cache->head_dim, a,
                              dim3((unsigned)(a.blocks * n_seqs), (unsigned)cache->kv_heads), (hipStream_t)stream);

@@ -113,7 +113,7 @@ def rows(c=None, dtype=A.EAS_FP16, pages=PTR, max_pages=5, n=2, cu=PTR, first=No
                                 A.Strides(*strides), v, A.Strides(*strides), None)
 
 
-def attend(c=None, s=None, q=PTR, rows=2, cu=None, most_q=1, lens=PTR, most=320, pages=PTR, max_pages=5, n=2, out=PTR,
+def attend(c=None, s=None, q=PTR, rows=2, cu=None, most_q=1, lens=PTR, most=4000, pages=PTR, max_pages=70, n=2, out=PTR,
            lse=None, ws=PTR, ws_bytes=1 << 30):
     return eas.LIB.eas_kv8_attention(ctypes.byref(c or cache()), ctypes.byref(s or shape()), q, rows, cu, most_q, lens,
                                      most, pages, max_pages, n, out, lse, ws, ws_bytes, None)
@@ -185,12 +185,12 @@ def workspace(max_q, max_len, n, s=None):
 
 
 def test_workspace_sizes_grow_with_queries_and_tokens_up_to_a_bound():
-    assert workspace(1, 256, 3) == 0                       # short: nothing is split
-    one = workspace(1, 257, 1)
-    assert one > 0 and workspace(1, 257, 5) == 5 * one
-    assert workspace(1, 1 << 20, 1) >= workspace(1, 4096, 1) >= one
+    assert workspace(1, 64, 3) == 0                        # short: nothing is split
+    one = workspace(1, 4000, 1)
+    assert one > 0 and workspace(1, 4000, 5) == 5 * one
+    assert workspace(1, 1 << 20, 1) >= workspace(1, 9000, 1) >= one
     assert workspace(1 << 20, 1 << 30, 1) == workspace(1 << 21, 1 << 30, 1)
-    assert attend(ws_bytes=workspace(1, 320, 2) - 1) == CAPACITY
+    assert attend(ws_bytes=workspace(1, 4000, 2) - 1) == CAPACITY
     b = ctypes.c_int64()
     call = eas.LIB.eas_kv8_attention_workspace
     assert call(None, 1, 1, 1, ctypes.byref(b)) == BAD
