@@ -8,6 +8,8 @@
 //   S^T = K Q^T (v_mfma_f32_32x32x16: keys are rows, so a lane holds 16 scores of one
 //   query), softmax in fp32 on exp2, O^T += V^T P^T with P rounded to the element type.
 // Bound by the matrix units: 4 * head_dim flops for each visible (query, key) pair.
+#include <type_traits>
+
 #include "attention_ops.h"
 
 namespace eas {
@@ -199,38 +201,58 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
     for (int e = 0; e < 16; ++e) o[hb][e] = 0.0f;
   float m = 0.0f, l = 0.0f;
 
-  auto scores = [&](int t, f32x16* s) {
-    const char* K = smem + (t & 1) * C::TILE;
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[kb][e] = 0.0f;
-#pragma unroll
-      for (int ks = 0; ks < C::KS; ++ks)
-        s[kb] = Mfma<T>::go(*reinterpret_cast<const x8*>(K + kb * 32 * HD * 2 + kofs[ks]), qf[ks], s[kb]);
-    }
+  constexpr int NK = 2 * C::KS, NV = 4 * C::HB;   // MFMAs of a tile's scores, and of its products with the values
+  // A operand of score MFMA i: keys 32 (i % 2) .. of k-step i / 2; of value MFMA j: block j % HB, keys 16 (j / HB) ..
+  const auto read_k = [&](int t, int i) {
+    return *reinterpret_cast<const x8*>(smem + (t & 1) * C::TILE + (i & 1) * 32 * HD * 2 + kofs[i >> 1]);
   };
-  // Online softmax of the tile's scores s and O^T += V^T P^T.  One FMA turns a score into x = s c - m, in log2
-  // units over the maximum m.  m is raised lazily, when some x exceeds 8, so p = 2^x <= 256 and O is rarely
-  // scaled; O and l share m, so O / l is the same.  The first tile always sets it.
-  auto accumulate = [&](int t, f32x16* s) {
+  const auto read_v = [&](int t, int j) {
+    union { x8 v; v4i16 h[2]; } u;
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+      u.h[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (lds_v4i16*)(lds + (2 + (t & 1)) * C::TILE + j / C::HB * 16 * HD * 2 + vofs[j % C::HB][half]));
+    return u.v;
+  };
+  const f32x16 zero = {};
+  // The scores of tile t, keys 32 .. in s[1].
+  const auto scores = [&](int t, f32x16* s) {
+#pragma unroll
+    for (int i = 0; i < NK; ++i)
+      s[i & 1] = Mfma<T>::go(read_k(t, i), qf[i >> 1], i < 2 ? zero : s[i & 1]);
+  };
+  // Tile t: the online softmax of its scores s and O^T += V^T P^T, and beside them the next tile's scores n.  One
+  // FMA turns a score into x = s c - m, in log2 units over the maximum m.  m is raised lazily, when some x exceeds
+  // 8, so p = 2^x <= 256 and O is rarely scaled; O and l share m, so O / l is the same.  The first tile always
+  // sets it.  The matrix unit takes 32 cycles an MFMA, in which the wave issues some 8 other instructions: the
+  // softmax's are dealt out behind the MFMAs by hand, in steps that nothing is moved across, each with the operands
+  // of the MFMA four steps on.  (Left to the compiler they come in blocks, and both waves of a SIMD wait for the
+  // same unit: matrix units 53% busy.)
+  const auto step = [&](int t, f32x16* s, f32x16* n, auto masked, auto next) {
+    constexpr bool MASKED = decltype(masked)::value, NEXT = decltype(next)::value;
     const int k0 = t * KT;
+    x8 kf[4], vf[4], p[4];
+    if constexpr (NEXT) {
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[kb][e] = fmaf(s[kb][e], a.scale_log2, -m);
-    if (k0 + KT > fewest) {
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (k0 + kb * 32 + (e >> 2) * 8 + g * 4 + (e & 3) >= sees) s[kb][e] = -INFINITY;
+      for (int i = 0; i < 4; ++i) kf[i] = read_k(t + 1, i);
     }
-    float mx = s[0][0];
+    float mx = -INFINITY;
+    constexpr int H = NK / 2, E = 32 / H;   // steps of the first part, and scores of each
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+    for (int i = 0; i < H; ++i) {
+      if constexpr (NEXT) {
+        n[i & 1] = Mfma<T>::go(kf[i & 3], qf[i >> 1], i < 2 ? zero : n[i & 1]);
+        kf[i & 3] = read_k(t + 1, i + 4);
+      }
 #pragma unroll
-      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[kb][e]);
+      for (int v = E * i; v < E * i + E; ++v) {
+        float x = fmaf(s[v >> 4][v & 15], a.scale_log2, -m);
+        if (MASKED && k0 + (v >> 4) * 32 + (v & 15) / 4 * 8 + g * 4 + (v & 3) >= sees) x = -INFINITY;
+        mx = fmaxf(mx, x);
+        s[v >> 4][v & 15] = x;
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
     {   // the query's other half of the keys is in lane ^ 32
       const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
       mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
@@ -250,39 +272,53 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[kb][e] -= d;
     }
+    float sum[4];
+    const auto weigh = [&](int v) {
+      const float x = __builtin_amdgcn_exp2f(s[v >> 4][v & 15]);
+      sum[v >> 3] = v & 7 ? sum[v >> 3] + x : x;
+      p[v >> 3][v & 7] = (T)x;
+    };
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (!NEXT) {
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+      for (int i = 0; i < 4; ++i) vf[i] = read_v(t, i);
+    }
+    constexpr int W = 16 / H;   // weights of the first 32 keys, a step
 #pragma unroll
-      for (int ch = 0; ch < 2; ++ch) {
-        x8 p;
-        float sum = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float x = __builtin_amdgcn_exp2f(s[kb][8 * ch + e]);
-          sum = e ? sum + x : x;
-          p[e] = (T)x;
-        }
-        l += sum;
-#pragma unroll
-        for (int hb = 0; hb < C::HB; ++hb) {
-          union { x8 v; v4i16 h[2]; } u;
-#pragma unroll
-          for (int half = 0; half < 2; ++half)
-            u.h[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (lds_v4i16*)(lds + (2 + (t & 1)) * C::TILE + (kb * 32 + 16 * ch) * HD * 2 + vofs[hb][half]));
-          o[hb] = Mfma<T>::go(u.v, p, o[hb]);
-        }
+    for (int i = H; i < NK; ++i) {
+      if constexpr (NEXT) {
+        n[i & 1] = Mfma<T>::go(kf[i & 3], qf[i >> 1], n[i & 1]);
+        if (i + 4 < NK)
+          kf[i & 3] = read_k(t + 1, i + 4);
+        else
+          vf[i + 4 - NK] = read_v(t, i + 4 - NK);
       }
+#pragma unroll
+      for (int v = W * (i - H); v < W * (i - H) + W; ++v) weigh(v);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    constexpr int Y = 32 / NV;   // of the others, beside the products with the first half's values
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      o[j % C::HB] = Mfma<T>::go(vf[j & 3], p[j / C::HB], o[j % C::HB]);
+      if (j + 4 < NV) vf[j & 3] = read_v(t, j + 4);
+      if (j < NV / 2)
+#pragma unroll
+        for (int v = 16 + Y * j; v < 16 + Y * j + Y; ++v) weigh(v);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
   };
-
-  // Tile t's softmax and the next tile's scores are independent, so the vector and matrix units overlap.
-  auto step = [&](int t, f32x16* now, f32x16* next) {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // keys t + 1 and values t are there
-    __syncthreads();                                              // and keys t and values t - 1 read by all
+  constexpr std::integral_constant<bool, true> yes{};
+  constexpr std::integral_constant<bool, false> no{};
+  // Waits until the wave's own DMA has landed and its LDS reads are done, and for the other waves to be as far.  One
+  // asm: no read may move up between the wait and the barrier.  Every wave passes it once a tile, from whichever of
+  // the loops below it is in.
+  const auto meet = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+  const auto arrive = [&](int t) {
+    meet();   // keys t + 1 and values t are there, keys t and values t - 1 read by all
     if (t + 2 < nt) fetch_k(t + 2);
     if (t + 1 < nt) fetch_v(t + 1);
-    if (t + 1 < nt_w) scores(t + 1, next);
-    if (t < nt_w) accumulate(t, now);
   };
   if (nt > 0) {
     f32x16 sa[2], sb[2];
@@ -294,12 +330,28 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
     // left to the loop, where it would wait for a tile
 #pragma unroll
     for (int ks = 0; ks < C::KS; ++ks) asm volatile("" ::"v"(qf[ks]));
-    __syncthreads();
-    if (nt_w > 0) scores(0, sa);
-    for (int t = 0; t < nt; t += 2) {
-      step(t, sa, sb);
-      if (t + 1 < nt) step(t + 1, sb, sa);
+    meet();
+    int t = 0;
+    if (nt_w > 0) {
+      scores(0, sa);
+      // tiles that all the wave's queries see whole, in pairs; those at the border; the last one
+      for (const int whole = min(fewest / KT, nt_w - 1); t + 2 <= whole; t += 2) {
+        arrive(t);
+        step(t, sa, sb, no, yes);
+        arrive(t + 1);
+        step(t + 1, sb, sa, no, yes);
+      }
+      for (; t + 1 < nt_w; ++t) {
+        arrive(t);
+        step(t, sa, sb, yes, yes);
+        sa[0] = sb[0];
+        sa[1] = sb[1];
+      }
+      arrive(t);
+      step(t, sa, sb, yes, no);
+      ++t;
     }
+    for (; t < nt; ++t) arrive(t);
   }
 
   T* first = static_cast<T*>(a.out) + w.cu_q[r] * a.os.row + h * a.os.head;
