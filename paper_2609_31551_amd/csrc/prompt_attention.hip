@@ -36,7 +36,7 @@ struct PromptArgs {
   void* out;
   float* lse;
   eas_strides qs, ks, vs, os;
-  int heads, group, causal;
+  int heads, group, causal, tiles;
   float scale_log2;
 };
 
@@ -124,6 +124,33 @@ struct Cfg {
   __device__ static int logical(int row, int p) { return (p + R - rot(row)) % R; }
 };
 
+// The head and query tile of a workgroup.  Workgroups go to the 8 XCDs in turn, each with an L2 of its own, so the
+// query heads of one key / value head, which read the same keys, are kept on one XCD (of 8 or more heads a whole
+// number each; 1, 2 or 4 heads get 8, 4 or 2 XCDs each); other numbers are dealt out as they come.  All heads of a
+// query tile, then those of the next.
+__device__ __forceinline__ bool place(const PromptArgs& a, int* h, int* tile) {
+  const int b = blockIdx.x, xcd = b & 7, i = b >> 3, kv_heads = a.heads / a.group;
+  if (kv_heads % 8 == 0) {
+    const int each = a.heads / 8;
+    *h = xcd * each + i % each;
+    *tile = i / each;
+  } else if (8 % kv_heads == 0) {
+    const int xcds = 8 / kv_heads, item = i * xcds + xcd % xcds;
+    *h = xcd / xcds * a.group + item % a.group;
+    *tile = item / a.group;
+  } else {
+    *h = b % a.heads;
+    *tile = b / a.heads;
+  }
+  return *tile < a.tiles;
+}
+// Workgroups that place() spreads `tiles` tiles of all heads over
+int64_t workgroups(int64_t tiles, int heads, int kv_heads) {
+  if (kv_heads % 8 == 0 || 8 % kv_heads) return tiles * heads;
+  const int64_t xcds = 8 / kv_heads;
+  return (tiles * (heads / kv_heads) + xcds - 1) / xcds * 8;
+}
+
 template <class T, int HD, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, PromptWork w) {
   using C = Cfg<HD, NW>;
@@ -132,7 +159,8 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
   __attribute__((address_space(3))) char* lds = (__attribute__((address_space(3))) char*)smem;
   const unsigned lds0 = (unsigned)(size_t)lds;
 
-  const int h = blockIdx.x % a.heads, tile = blockIdx.x / a.heads;
+  int h, tile;
+  if (!place(a, &h, &tile)) return;
   int r = 0, qt;
   if (w.listed) {
     r = w.tile[tile] & 63;
@@ -492,10 +520,11 @@ extern "C" eas_status eas_prompt_attention(const eas_attn_shape* shape, const vo
   for (int r = 0; r <= n_seqs; ++r) w.cu_q[r] = cu_q[r], w.cu_k[r] = cu_k[r];
   const int qt = query_tile(w, shape->heads, shape->causal);
   const int64_t tiles = list_tiles(&w, qt, shape->causal);
-  if (tiles * shape->heads > 0x7fffffff) return EAS_ERR_UNSUPPORTED;
+  const int64_t blocks = workgroups(tiles, shape->heads, shape->kv_heads);
+  if (blocks > 0x7fffffff) return EAS_ERR_UNSUPPORTED;
   const PromptArgs a = {q, k, v, out, lse, shape->q, shape->k, shape->v, shape->out, shape->heads,
-                        shape->heads / shape->kv_heads, shape->causal, shape->scale * kLog2e};
-  const unsigned grid = (unsigned)(tiles * shape->heads);
+                        shape->heads / shape->kv_heads, shape->causal, (int)tiles, shape->scale * kLog2e};
+  const unsigned grid = (unsigned)blocks;
   const hipStream_t st_ = (hipStream_t)stream;
 #define EAS_PROMPT_CASE(DT, T, D) \
   if (shape->dtype == DT && shape->head_dim == D) \
