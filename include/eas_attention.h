@@ -70,11 +70,22 @@ typedef struct {
  * Rows of out and lse outside [0, cu_q[n_seqs]) are not touched.  A sequence's
  * result does not depend on the others, to the bit.
  * k and v may hold anything, NaN included, outside the sequences' keys.
- * Errors: INVALID_ARG, SHAPE (cu_q, cu_k), CAPACITY (n_seqs), UNSUPPORTED
- * (element type, head_dim, strides, more than 2^31 - 1 work items). */
+ * workspace: device, 16-byte aligned, at least the bytes that
+ * eas_prompt_attention_workspace gives for the same arguments (0: NULL is
+ * fine), which is more than 0 only where few queries see over 4,096 keys; calls
+ * that may overlap, captured ones included, need one each.  Nothing in it has
+ * to be set before, or is kept from call to call.
+ * Errors: INVALID_ARG, SHAPE (cu_q, cu_k), CAPACITY (n_seqs, the workspace),
+ * UNSUPPORTED (element type, head_dim, strides, more than 2^30 queries or keys,
+ * more than 2^31 - 1 work items). */
 eas_status eas_prompt_attention(const eas_attn_shape* shape, const void* q, const void* k, const void* v,
                                 const int32_t* cu_q, const int32_t* cu_k, int32_t n_seqs, void* out, float* lse,
-                                void* stream);
+                                void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Workspace bytes of eas_prompt_attention (host only, no HIP calls; the
+ * shape's strides are not read). */
+eas_status eas_prompt_attention_workspace(const eas_attn_shape* shape, const int32_t* cu_q, const int32_t* cu_k,
+                                          int32_t n_seqs, int64_t* bytes);
 
 /* The cache.  A block -- page_tokens tokens of one head -- is held as 8-bit
  * codes and one scale, a power of two or 0: value = code * scale.  Scale 2^e

@@ -35,7 +35,8 @@ class Kv8CacheStruct(ctypes.Structure):
 
 _NO_STRIDES = Strides()
 _SIG = {
-    "eas_prompt_attention": [P(AttnShape), VP, VP, VP, VP, VP, I32, VP, VP, VP],
+    "eas_prompt_attention": [P(AttnShape), VP, VP, VP, VP, VP, I32, VP, VP, VP, I64, VP],
+    "eas_prompt_attention_workspace": [P(AttnShape), VP, VP, I32, P(I64)],
     "eas_kv8_append": [P(Kv8CacheStruct), I32, VP, Strides, VP, Strides, I32, VP, I32, VP, VP, I32, I32, VP],
     "eas_kv8_rows": [P(Kv8CacheStruct), I32, VP, I32, I32, VP, VP, I32, I32, VP, Strides, VP, Strides, VP],
     "eas_kv8_attention": [P(Kv8CacheStruct), P(AttnShape), VP, I32, VP, I32, VP, I32, VP, I32, I32, VP, VP, VP, I64,
@@ -118,6 +119,18 @@ def _outputs(q, out, lse, with_lse, index, stream):
     return out, lse, strides, lse.data_ptr()
 
 
+def _workspace(workspace, need, index, device, stream):
+    """The workspace of a call that needs ``need`` bytes -- the caller's or a new one --, its address and size."""
+    if workspace is None:
+        if not need:
+            return None, None, 0
+        workspace = _on(stream, lambda: torch.empty((need,), dtype=torch.uint8, device=device))
+        return workspace, workspace.data_ptr(), need
+    if workspace.dtype != torch.uint8 or workspace.get_device() != index or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 tensor on cuda:%d" % index)
+    return workspace, workspace.data_ptr(), workspace.numel()
+
+
 def _cu(cu, rows, name):
     """Host prefix sums as an array of C ints."""
     cu = array.array("i", cu)
@@ -127,12 +140,12 @@ def _cu(cu, rows, name):
 
 
 def prompt_attention(q, k, v, cu_q, cu_k=None, *, causal=True, scale=None, out=None, lse=None, with_lse=False,
-                     stream=None):
+                     workspace=None, stream=None):
     """Attention over packed prompts (eas_prompt_attention).  q [rows, heads, head_dim] and k, v [rows, kv_heads,
     head_dim] in bfloat16 or float16, any row and head strides; cu_q, cu_k: host prefix sums of the sequences'
     queries and keys (cu_k None: the same).  scale None: head_dim ** -0.5.  Returns (out, lse): out like q, in
     ``out`` where given, rows behind the last sequence untouched; lse [rows, heads] float32 with with_lse or where
-    given, else None."""
+    given, else None.  workspace: a uint8 device tensor to use instead of a new one where one is needed."""
     index, dtype = _device(q), q.dtype
     code = _dtype(dtype)
     if q.dim() != 3 or k.dim() != 3:
@@ -150,8 +163,12 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, *, causal=True, scale=None, out=N
     out, lse, strides, lse_ptr = _outputs(q, out, lse, with_lse, index, stream)
     shape = AttnShape(code, heads, kv_heads, dim, 1 if causal else 0, dim ** -0.5 if scale is None else scale,
                       qs, ks, vs, strides)
-    _check(LIB.eas_prompt_attention(shape, q.data_ptr(), k.data_ptr(), v.data_ptr(), cu_q.buffer_info()[0],
-                                    cu_k.buffer_info()[0], len(cu_q) - 1, out.data_ptr(), lse_ptr,
+    n, cu_q_ptr, cu_k_ptr = len(cu_q) - 1, cu_q.buffer_info()[0], cu_k.buffer_info()[0]
+    need = I64()
+    _check(LIB.eas_prompt_attention_workspace(shape, cu_q_ptr, cu_k_ptr, n, need), "prompt_attention")
+    workspace, ws_ptr, ws_bytes = _workspace(workspace, need.value, index, q.device, stream)
+    _check(LIB.eas_prompt_attention(shape, q.data_ptr(), k.data_ptr(), v.data_ptr(), cu_q_ptr, cu_k_ptr, n,
+                                    out.data_ptr(), lse_ptr, ws_ptr, ws_bytes,
                                     _current_stream(index) if stream is None else stream.cuda_stream),
            "prompt_attention")
     return out, lse
@@ -265,15 +282,9 @@ class Kv8Cache:
                           qs, _NO_STRIDES, _NO_STRIDES, strides)
         need = I64()
         _check(LIB.eas_kv8_attention_workspace(shape, most_q, most, n, need), "Kv8Cache.attention")
-        if workspace is None:
-            if need.value:
-                workspace = _on(stream, lambda: torch.empty((need.value,), dtype=torch.uint8, device=self.device))
-        elif workspace.dtype != torch.uint8 or workspace.get_device() != index or not workspace.is_contiguous():
-            raise ValueError("workspace must be a contiguous uint8 tensor on %s" % self.device)
+        workspace, ws_ptr, ws_bytes = _workspace(workspace, need.value, index, self.device, stream)
         _check(LIB.eas_kv8_attention(self._c, shape, q.data_ptr(), rows, cu, most_q, _ints(lens, "lens", index, (n,)),
-                                     most, table, max_pages, n, out.data_ptr(), lse_ptr,
-                                     None if workspace is None else workspace.data_ptr(),
-                                     0 if workspace is None else workspace.numel(),
+                                     most, table, max_pages, n, out.data_ptr(), lse_ptr, ws_ptr, ws_bytes,
                                      _current_stream(index) if stream is None else stream.cuda_stream),
                "Kv8Cache.attention")
         return out, lse

@@ -366,16 +366,16 @@ __global__ __launch_bounds__(64 * NW) void kv8_attention_kernel(Kv8AttnArgs a) {
 // Joins the runs of the sequences that were split: a wave for each row.
 template <class T, int D>
 __global__ __launch_bounds__(64 * NW) void kv8_join_kernel(Kv8AttnArgs a) {
-  const long row = (long)blockIdx.x * NW + (threadIdx.x >> 6);   // (sequence, query, head)
+  const unsigned row = blockIdx.x * NW + (threadIdx.x >> 6);   // (sequence, query, head), below 2^31
   const int lane = threadIdx.x & 63;
-  const int h = (int)(row % a.heads), q = (int)(row / a.heads % a.max_q);
-  const long r = row / a.heads / a.max_q;
+  const int h = row % (unsigned)a.heads, q = row / (unsigned)a.heads % (unsigned)a.max_q;
+  const int r = row / (unsigned)a.heads / (unsigned)a.max_q;
   if (r >= a.n_seqs) return;
-  const Seq s = find_seq(a, (int)r);
+  const Seq s = find_seq(a, r);
   if (q >= s.nq) return;
   const int runs = n_runs(s.len, s.nq);
   if (runs == 1) return;
-  const long slot = (r * a.heads + h) * a.slots + (long)q * runs;
+  const long slot = ((long)r * a.heads + h) * a.slots + q * runs;
   const float lse2 = lane < runs ? a.part_lse[slot + lane] : -INFINITY;
   float M = lse2;
 #pragma unroll

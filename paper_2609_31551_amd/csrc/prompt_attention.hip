@@ -15,17 +15,31 @@
 namespace eas {
 namespace {
 
-constexpr int KT = 64;    // keys per tile
+constexpr int KT = 64;               // keys per tile
+constexpr int kMaxRows = 1 << 30;    // queries or keys of a call
+constexpr int MAX_RUNS = 16;         // runs that a sequence's keys are split into
 
-// Work list: the query tiles of all sequences, those with most keys first where they are few enough to be listed
-// (when they are many, what the last ones leave idle is little).
+// Runs of keys that each query tile of a sequence is split into, a workgroup each: of 4,096 keys at least, where the
+// sequence alone leaves CUs without a workgroup.  A call waits for its longest walk: 128 queries over 32,896 keys of 32
+// heads 86 us, in one walk 471; 512 over 8,704 91 and 134; chunks of 700 - 1,024 queries over 1,535 - 9,916 keys of 16
+// heads 104 and 126.  A batch that fills the chip anyway pays for the runs' sums: eight chunks of 512 over 9,512 keys
+// 620 and 551.  By a sequence's own sizes only: the join rounds otherwise, and a result must not depend on the batch.
+__host__ __device__ inline int n_runs(int lq, int lk, int heads) {
+  if ((int64_t)((lq + 127) / 128) * heads > 256) return 1;
+  const int runs = lk / 4096;
+  return runs < 1 ? 1 : runs < MAX_RUNS ? runs : MAX_RUNS;
+}
+
+// Work list: the query tiles of all sequences, a run each, those with most keys first where they are few enough to be
+// listed (when they are many, what the last ones leave idle is little).
 constexpr int LISTED = 768;
 struct PromptWork {
   int n, listed;
   int cu_q[kMaxSeqs + 1], cu_k[kMaxSeqs + 1];
+  int slot0[kMaxSeqs + 1];        // prefix sums of the split sequences' slots in the workspace, queries * heads * runs
   union {
-    int tile_start[kMaxSeqs + 1];   // not listed: prefix sums of query tiles, each sequence's from its last on
-    uint16_t tile[LISTED];          // listed: sequence | tile << 6
+    int tile_start[kMaxSeqs + 1];   // not listed: prefix sums of tiles * runs, each sequence's from its last on
+    uint16_t tile[LISTED];          // listed: sequence | (tile * runs + run) << 6
   };
 };
 
@@ -38,6 +52,8 @@ struct PromptArgs {
   eas_strides qs, ks, vs, os;
   int heads, group, causal, tiles;
   float scale_log2;
+  float* part;       // results of runs [slots, head_dim]
+  float* part_lse;   // and their softmax's log2 sums [slots]
 };
 
 template <class T>
@@ -53,20 +69,29 @@ struct Mfma<f16> {
   __device__ static f32x16 go(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
 
-// Queries first .. first + 32 of a sequence by one wave, query by query and key by key, a lane holding HD / 64
-// dimensions: touches no key or value that a query does not see.  Only for results that the tiled products, in
-// which a hidden value is multiplied by a weight of 0, leave infinite or NaN.
+// Where a head's results go: rows of the output, or with several runs slots of the workspace.
+template <class T>
+struct Results {
+  T* out;        // head h of the sequence's first query
+  float* lse;    // or null
+  float* part;   // slot of the sequence's first query, head and run
+  float* part_lse;
+};
+
+// Queries first .. first + 32 of a sequence over keys from .. to by one wave, query by query and key by key, a lane
+// holding HD / 64 dimensions: touches no key or value that a query does not see.  Only for results that the tiled
+// products, in which a hidden value is multiplied by a weight of 0, leave infinite or NaN.
 template <class T, int HD>
 __device__ void careful_rows(const PromptArgs& a, const T* qp, const T* kp, const T* vp, int lq, int lk, int first,
-                             T* out, float* lse) {
+                             int from, int to, int runs, const Results<T>& res) {
   constexpr int E = HD / 64;
   const int d = (threadIdx.x & 63) * E;
   for (int i = first; i < min(first + 32, lq); ++i) {
-    const int sees = a.causal ? max(0, min(lk, i + lk - lq + 1)) : lk;
+    const int sees = min(to, a.causal ? max(0, min(lk, lk - lq + i + 1)) : lk);
     float q[E], o[E], m = -INFINITY, l = 0.0f;
 #pragma unroll
     for (int e = 0; e < E; ++e) q[e] = (float)qp[i * a.qs.row + d + e], o[e] = 0.0f;
-    for (int j = 0; j < sees; ++j) {
+    for (int j = from; j < sees; ++j) {
       float s = 0.0f;
 #pragma unroll
       for (int e = 0; e < E; ++e) s = fmaf(q[e], (float)kp[j * a.ks.row + d + e], s);
@@ -78,10 +103,16 @@ __device__ void careful_rows(const PromptArgs& a, const T* qp, const T* kp, cons
 #pragma unroll
       for (int e = 0; e < E; ++e) o[e] = fmaf(o[e], alpha, p * (float)vp[j * a.vs.row + d + e]);
     }
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l, lse2 = l == 0.0f ? -INFINITY : m + __log2f(l);
 #pragma unroll
-    for (int e = 0; e < E; ++e) out[i * a.os.row + d + e] = (T)(o[e] * inv);
-    if (lse && d == 0) lse[(long)i * a.heads] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
+    for (int e = 0; e < E; ++e) {
+      if (runs > 1)
+        res.part[(long)i * HD + d + e] = o[e] * inv;
+      else
+        res.out[i * a.os.row + d + e] = (T)(o[e] * inv);
+    }
+    if (d == 0 && runs > 1) res.part_lse[i] = lse2;
+    if (d == 0 && runs == 1 && res.lse) res.lse[(long)i * a.heads] = lse2 * kLn2;
   }
 }
 
@@ -161,15 +192,16 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
 
   int h, tile;
   if (!place(a, &h, &tile)) return;
-  int r = 0, qt;
+  int r = 0, item;
   if (w.listed) {
     r = w.tile[tile] & 63;
-    qt = w.tile[tile] >> 6;
+    item = w.tile[tile] >> 6;
   } else {
     while (r + 1 < w.n && w.tile_start[r + 1] <= tile) ++r;
-    qt = w.tile_start[r + 1] - 1 - tile;
+    item = w.tile_start[r + 1] - 1 - tile;
   }
   const int lq = w.cu_q[r + 1] - w.cu_q[r], lk = w.cu_k[r + 1] - w.cu_k[r];
+  const int runs = n_runs(lq, lk, a.heads), qt = item / runs, run = item % runs;
   const int q0 = qt * C::QT;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, l32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -178,10 +210,12 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
   const T* vp = static_cast<const T*>(a.v) + w.cu_k[r] * a.vs.row + h / a.group * a.vs.head;
 
   // keys that a query sees: this lane's, the wave's fewest and most, the workgroup's most
-  auto seen = [&](int q) { return a.causal ? max(0, min(lk, min(q, lq - 1) + 1 + lk - lq)) : lk; };
+  auto seen = [&](int q) { return a.causal ? max(0, min(lk, lk - lq + min(q, lq - 1) + 1)) : lk; };
   const int qw = q0 + wave * 32, qi = qw + l32;
   const int sees = seen(qi), fewest = seen(qw), most = qw < lq ? seen(qw + 31) : 0;
-  const int nt = (seen(q0 + C::QT - 1) + KT - 1) / KT, nt_w = (most + KT - 1) / KT;
+  // key tiles of the query tile, from tb on those of the run, and of these the wave's
+  const int all = (seen(q0 + C::QT - 1) + KT - 1) / KT, each = (all + runs - 1) / runs, tb = run * each;
+  const int nt = max(0, min(each, all - tb)), nt_w = max(0, min(nt, (most + KT - 1) / KT - tb));
 
   x8 qf[C::KS];
 #pragma unroll
@@ -197,8 +231,8 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
     dcol[j] = C::logical(drow[j], slot % C::R) * 16;
   }
   auto fetch = [&](const T* p, long stride, int t, int lds_off) {
-    const int left = lk - 1 - t * KT;   // rows behind the last key read it again
-    const T* base = p + (long)t * KT * stride;
+    const int left = lk - 1 - (tb + t) * KT;   // rows behind the last key read it again
+    const T* base = p + (long)(tb + t) * KT * stride;
 #pragma unroll
     for (int j = 0; j < C::NDMA; ++j)
       dma16(lds0 + lds_off + (wave + NW * j) * 1024, (unsigned)min(drow[j], left) * (unsigned)(stride * 2) + dcol[j],
@@ -258,7 +292,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
   // same unit: matrix units 53% busy.)
   const auto step = [&](int t, f32x16* s, f32x16* n, auto masked, auto next) {
     constexpr bool MASKED = decltype(masked)::value, NEXT = decltype(next)::value;
-    const int k0 = t * KT;
+    const int k0 = (tb + t) * KT;
     x8 kf[4], vf[4], p[4];
     if constexpr (NEXT) {
 #pragma unroll
@@ -363,7 +397,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
     if (nt_w > 0) {
       scores(0, sa);
       // tiles that all the wave's queries see whole, in pairs; those at the border; the last one
-      for (const int whole = min(fewest / KT, nt_w - 1); t + 2 <= whole; t += 2) {
+      for (const int whole = min(fewest / KT - tb, nt_w - 1); t + 2 <= whole; t += 2) {
         arrive(t);
         step(t, sa, sb, no, yes);
         arrive(t + 1);
@@ -382,21 +416,35 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
     for (; t < nt; ++t) arrive(t);
   }
 
-  T* first = static_cast<T*>(a.out) + w.cu_q[r] * a.os.row + h * a.os.head;
-  float* first_lse = a.lse ? a.lse + (long)w.cu_q[r] * a.heads + h : nullptr;
-  // every wave is past its last read: the tiles' memory now stages each wave's 32 x HD results, chunks of row r
-  // rotated by r, so that the stores are of whole rows
+  const long slot0 = w.slot0[r] + ((long)run * a.heads + h) * lq;   // [run, head, query]: a wave's are consecutive
+  const Results<T> res = {static_cast<T*>(a.out) + w.cu_q[r] * a.os.row + h * a.os.head,
+                          a.lse ? a.lse + (long)w.cu_q[r] * a.heads + h : nullptr, a.part + slot0 * HD,
+                          a.part_lse + slot0};
+  // every wave is past its last read
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   __syncthreads();
   if (qw >= lq) return;
   if (a.causal && any_not_finite<C::HB>(o)) {
-    careful_rows<T, HD>(a, qp, kp, vp, lq, lk, qw, first, first_lse);
+    careful_rows<T, HD>(a, qp, kp, vp, lq, lk, qw, min(tb * KT, lk), (int)min((long)lk, (long)(tb + nt) * KT), runs, res);
     return;
   }
   l += __shfl_xor(l, 32, 64);
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  if (first_lse && g == 0 && qi < lq)
-    first_lse[(long)qi * a.heads] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l, lse2 = l == 0.0f ? -INFINITY : m + __log2f(l);
+  if (runs > 1) {
+    if (qi < lq) {
+#pragma unroll
+      for (int hb = 0; hb < C::HB; ++hb)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4)
+          *reinterpret_cast<float4*>(res.part + (long)qi * HD + hb * 32 + e * 2 + g * 4) =
+              make_float4(o[hb][e] * inv, o[hb][e + 1] * inv, o[hb][e + 2] * inv, o[hb][e + 3] * inv);
+      if (g == 0) res.part_lse[qi] = lse2;
+    }
+    return;
+  }
+  if (res.lse && g == 0 && qi < lq) res.lse[(long)qi * a.heads] = lse2 * kLn2;
+  // the tiles' memory stages each wave's 32 x HD results, chunks of row r rotated by r, so that the stores are of
+  // whole rows
   char* stage = smem + wave * 32 * HD * 2;
 #pragma unroll
   for (int hb = 0; hb < C::HB; ++hb)
@@ -412,8 +460,45 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
   for (int k = 0; k < C::R / 2; ++k) {
     const int c = lane + 64 * k, row = c / C::R, ch = c % C::R;
     const uint4 x = *reinterpret_cast<const uint4*>(stage + row * HD * 2 + (ch + row) % C::R * 16);
-    if (qw + row < lq) *reinterpret_cast<uint4*>(first + (qw + row) * a.os.row + ch * 8) = x;
+    if (qw + row < lq) *reinterpret_cast<uint4*>(res.out + (qw + row) * a.os.row + ch * 8) = x;
   }
+}
+
+// Joins the runs of the split sequences, in order.
+struct JoinWork {
+  int n;
+  int seq[kMaxSeqs], row0[kMaxSeqs + 1];   // split sequences, prefix sums of their queries
+};
+template <class T, int HD>
+__global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, PromptWork w, JoinWork j) {
+  constexpr int ROWS = 256 / (HD / 4);   // queries of a workgroup, a thread 4 dimensions; a run's of a head lie together
+  const int row = blockIdx.x * ROWS + threadIdx.x / (HD / 4), h = blockIdx.y, d = threadIdx.x % (HD / 4) * 4;
+  if (row >= j.row0[j.n]) return;
+  int s = 0;
+  while (j.row0[s + 1] <= row) ++s;
+  const int r = j.seq[s], i = row - j.row0[s];
+  const int lq = w.cu_q[r + 1] - w.cu_q[r], runs = n_runs(lq, w.cu_k[r + 1] - w.cu_k[r], a.heads);
+  const long slot = w.slot0[r] + (long)h * lq + i, step = (long)a.heads * lq;   // of run 0, and from run to run
+  float M = -INFINITY;
+  for (int k = 0; k < runs; ++k) M = fmaxf(M, a.part_lse[slot + k * step]);
+  const float base = M == -INFINITY ? 0.0f : M;
+  float W = 0.0f;
+  f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int k = 0; k < runs; ++k) {
+    const f32x4 x = *reinterpret_cast<const f32x4*>(a.part + (slot + k * step) * HD + d);
+    const float wk = __builtin_amdgcn_exp2f(a.part_lse[slot + k * step] - base);
+    W += wk;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[e] = fmaf(wk, x[e], sum[e]);
+  }
+  const float inv = W == 0.0f ? 0.0f : 1.0f / W;
+  typedef T Tx4 __attribute__((ext_vector_type(4)));
+  Tx4 y;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = (T)(sum[e] * inv);
+  *reinterpret_cast<Tx4*>(static_cast<T*>(a.out) + (w.cu_q[r] + i) * a.os.row + h * a.os.head + d) = y;
+  if (d == 0 && a.lse) a.lse[(long)(w.cu_q[r] + i) * a.heads + h] = W == 0.0f ? -INFINITY : (M + __log2f(W)) * kLn2;
 }
 
 template <class T, int HD, int NW>
@@ -432,10 +517,11 @@ int64_t key_tiles(int64_t lq, int64_t lk, int64_t t, int qt, int causal) {
 
 // Queries per workgroup.  256 share each key and value tile among twice the queries, which halves the DMA per score:
 // 3-6% faster where both fill the chip (16,484 causal tokens of 32 heads 2,049 us against 2,129; 8,192 full 984
-// against 1,055).  128 leave less of a workgroup idle behind a sequence's end and at the diagonal, and spread few
-// queries over more CUs: eight image prompts of 97 to 2,309 tokens 130 us against 140, 2,048 tokens of 28 heads 57
-// against 60.  So 256 where they take at most 8% more key tiles per query and two workgroups a CU remain.  A
-// query's arithmetic is the same in both.
+// against 1,055).  128 leave less of a workgroup idle behind a sequence's end and at the diagonal, spread few
+// queries over more CUs, and put two workgroups on a CU, one's loads and stores beside the other's products: eight
+// image prompts of 97 to 2,309 tokens 130 us against 140, 64 prompts of 256 125 against 138.  So 256 where they
+// take at most 8% more key tiles per query, walk 16 at least, and two workgroups a CU remain.  A query's arithmetic
+// is the same in both.
 int query_tile(const PromptWork& w, int heads, int causal) {
   int64_t cost[2] = {}, tiles = 0;
   for (int big = 0; big < 2; ++big)
@@ -443,20 +529,21 @@ int query_tile(const PromptWork& w, int heads, int causal) {
       const int64_t lq = (int64_t)w.cu_q[r + 1] - w.cu_q[r], lk = (int64_t)w.cu_k[r + 1] - w.cu_k[r];
       const int qt = big ? 256 : 128;
       const int64_t n = (lq + qt - 1) / qt;
-      // key tiles of the first, the last and, as they grow evenly, all
-      cost[big] += n ? (key_tiles(lq, lk, 0, qt, causal) + key_tiles(lq, lk, n - 1, qt, causal)) * n * (big + 1) : 0;
+      // twice the key tiles of all: of the first and the last, as they grow evenly
+      cost[big] += n ? (key_tiles(lq, lk, 0, qt, causal) + key_tiles(lq, lk, n - 1, qt, causal)) * n : 0;
       if (big) tiles += n;
     }
-  return cost[1] * 100 <= cost[0] * 108 && tiles * heads >= 2l * device_cus() ? 256 : 128;
+  return 2 * cost[1] * 100 <= cost[0] * 108 && cost[1] >= 32 * tiles && tiles * heads >= 2l * device_cus() ? 256 : 128;
 }
 
-// Fills the work list for tiles of qt queries; their number.
-int64_t list_tiles(PromptWork* w, int qt, int causal) {
+// Fills the work list for tiles of qt queries; their number, one for each run.
+int64_t list_tiles(PromptWork* w, int heads, int qt, int causal) {
   const auto queries = [&](int r) { return (int64_t)w->cu_q[r + 1] - w->cu_q[r]; };
   const auto keys = [&](int r) { return (int64_t)w->cu_k[r + 1] - w->cu_k[r]; };
+  const auto runs = [&](int r) { return n_runs((int)queries(r), (int)keys(r), heads); };
   int64_t tiles = 0, most = 0;
   for (int r = 0; r < w->n; ++r) {
-    tiles += (queries(r) + qt - 1) / qt;
+    tiles += (queries(r) + qt - 1) / qt * runs(r);
     most = keys(r) > most ? keys(r) : most;
   }
   w->listed = tiles <= LISTED;
@@ -464,7 +551,7 @@ int64_t list_tiles(PromptWork* w, int qt, int causal) {
     int64_t at = 0;
     for (int r = 0; r < w->n; ++r) {
       w->tile_start[r] = (int)at;
-      at += (queries(r) + qt - 1) / qt;
+      at += (queries(r) + qt - 1) / qt * runs(r);
     }
     w->tile_start[w->n] = (int)at;
     return tiles;
@@ -473,15 +560,53 @@ int64_t list_tiles(PromptWork* w, int qt, int causal) {
   constexpr int CLASSES = 128;
   int at[CLASSES + 1] = {};
   const int64_t top = (most + KT - 1) / KT + 1;
-  const auto each = [&](auto&& f) {
+  const auto every = [&](auto&& f) {
     for (int r = 0; r < w->n; ++r)
-      for (int64_t t = 0; t * qt < queries(r); ++t)
-        f(r, (int)t, (int)(CLASSES - 1 - key_tiles(queries(r), keys(r), t, qt, causal) * CLASSES / top));
+      for (int64_t t = 0; t * qt < queries(r); ++t) {
+        const int n = runs(r);
+        const int c = (int)(CLASSES - 1 - key_tiles(queries(r), keys(r), t, qt, causal) / n * CLASSES / top);
+        for (int k = 0; k < n; ++k) f(r, (int)t * n + k, c);
+      }
   };
-  each([&](int, int, int c) { ++at[c + 1]; });
+  every([&](int, int, int c) { ++at[c + 1]; });
   for (int c = 0; c < CLASSES; ++c) at[c + 1] += at[c];
-  each([&](int r, int t, int c) { w->tile[at[c]++] = (uint16_t)(r | t << 6); });
+  every([&](int r, int t, int c) { w->tile[at[c]++] = (uint16_t)(r | t << 6); });
   return tiles;
+}
+
+// The sequences, their slots in the workspace, and those that are split
+void fill_work(PromptWork* w, JoinWork* j, const int32_t* cu_q, const int32_t* cu_k, int32_t n, int heads) {
+  w->n = n;
+  j->n = 0;
+  int slots = 0, rows = 0;   // at most 64 * 256 * 128 * MAX_RUNS slots
+  for (int r = 0; r <= n; ++r) {
+    w->cu_q[r] = cu_q[r], w->cu_k[r] = cu_k[r];
+    w->slot0[r] = slots;
+    if (r == n) break;
+    const int lq = cu_q[r + 1] - cu_q[r], runs = n_runs(lq, cu_k[r + 1] - cu_k[r], heads);
+    if (runs == 1 || lq == 0) continue;
+    slots += lq * heads * runs;
+    j->seq[j->n] = r;
+    j->row0[j->n++] = rows;
+    rows += lq;
+  }
+  j->row0[j->n] = rows;
+}
+
+template <class T, int HD>
+eas_status launch_all(const eas_attn_shape* shape, PromptArgs a, PromptWork* w, const JoinWork& j, hipStream_t s) {
+  const int qt = query_tile(*w, shape->heads, shape->causal);
+  const int64_t tiles = list_tiles(w, shape->heads, qt, shape->causal);
+  const int64_t blocks = workgroups(tiles, shape->heads, shape->kv_heads);
+  if (blocks > 0x7fffffff) return EAS_ERR_UNSUPPORTED;
+  a.tiles = (int)tiles;
+  const eas_status st = qt == 256 ? launch<T, HD, 8>(a, *w, (unsigned)blocks, s)
+                                  : launch<T, HD, 4>(a, *w, (unsigned)blocks, s);
+  if (st != EAS_OK || !j.n) return st;
+  constexpr int each = 256 / (HD / 4);
+  const dim3 grid((unsigned)((j.row0[j.n] + each - 1) / each), (unsigned)shape->heads);
+  hipLaunchKernelGGL((prompt_join_kernel<T, HD>), grid, dim3(256), 0, s, a, *w, j);
+  return hipGetLastError() == hipSuccess ? EAS_OK : EAS_ERR_HIP;
 }
 
 eas_status check_cu(const int32_t* cu, int32_t n) {
@@ -496,39 +621,59 @@ eas_status check_cu(const int32_t* cu, int32_t n) {
 
 using namespace eas;
 
-extern "C" eas_status eas_prompt_attention(const eas_attn_shape* shape, const void* q, const void* k, const void* v,
-                                           const int32_t* cu_q, const int32_t* cu_k, int32_t n_seqs, void* out,
-                                           float* lse, void* stream) {
+namespace {
+// What both calls refuse; *work and *join are filled
+eas_status check_call(const eas_attn_shape* shape, const int32_t* cu_q, const int32_t* cu_k, int32_t n_seqs,
+                      PromptWork* work, JoinWork* join) {
   eas_status st = check_shape(shape);
-  if (st == EAS_OK) st = check_strides(shape->q);
-  if (st == EAS_OK) st = check_strides(shape->k);
-  if (st == EAS_OK) st = check_strides(shape->v);
   if (st != EAS_OK) return st;
   if (!cu_q) return EAS_ERR_INVALID_ARG;
   if (n_seqs < 0 || n_seqs > EAS_MAX_SEQS) return EAS_ERR_CAPACITY;
   if (!cu_k) cu_k = cu_q;
   st = check_cu(cu_q, n_seqs);
   if (st == EAS_OK) st = check_cu(cu_k, n_seqs);
+  if (st != EAS_OK) return st;
+  if (cu_q[n_seqs] > kMaxRows || cu_k[n_seqs] > kMaxRows) return EAS_ERR_UNSUPPORTED;
+  fill_work(work, join, cu_q, cu_k, n_seqs, shape->heads);
+  return EAS_OK;
+}
+int64_t workspace_bytes_of(const PromptWork& w, int head_dim) { return (int64_t)w.slot0[w.n] * (head_dim + 1) * 4; }
+}  // namespace
+
+extern "C" eas_status eas_prompt_attention_workspace(const eas_attn_shape* shape, const int32_t* cu_q,
+                                                     const int32_t* cu_k, int32_t n_seqs, int64_t* bytes) {
+  PromptWork w;
+  JoinWork j;
+  const eas_status st = check_call(shape, cu_q, cu_k, n_seqs, &w, &j);
+  if (st != EAS_OK) return st;
+  if (!bytes) return EAS_ERR_INVALID_ARG;
+  *bytes = workspace_bytes_of(w, shape->head_dim);
+  return EAS_OK;
+}
+
+extern "C" eas_status eas_prompt_attention(const eas_attn_shape* shape, const void* q, const void* k, const void* v,
+                                           const int32_t* cu_q, const int32_t* cu_k, int32_t n_seqs, void* out,
+                                           float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
+  PromptWork w;
+  JoinWork j;
+  eas_status st = check_call(shape, cu_q, cu_k, n_seqs, &w, &j);
+  if (st == EAS_OK) st = check_strides(shape->q);
+  if (st == EAS_OK) st = check_strides(shape->k);
+  if (st == EAS_OK) st = check_strides(shape->v);
   if (st == EAS_OK) st = check_out_strides(shape->out, cu_q[n_seqs], shape->heads, shape->head_dim);
   if (st != EAS_OK) return st;
   if (cu_q[n_seqs] == 0) return EAS_OK;
   if (!q || !out || !aligned16(q) || !aligned16(out) || (uintptr_t)lse % 4) return EAS_ERR_INVALID_ARG;
-  if (cu_k[n_seqs] > 0 && (!k || !v || !aligned16(k) || !aligned16(v))) return EAS_ERR_INVALID_ARG;
+  if (w.cu_k[n_seqs] > 0 && (!k || !v || !aligned16(k) || !aligned16(v))) return EAS_ERR_INVALID_ARG;
+  if (j.n && (!workspace || !aligned16(workspace))) return EAS_ERR_INVALID_ARG;
+  if (j.n && workspace_bytes < workspace_bytes_of(w, shape->head_dim)) return EAS_ERR_CAPACITY;
 
-  PromptWork w;
-  w.n = n_seqs;
-  for (int r = 0; r <= n_seqs; ++r) w.cu_q[r] = cu_q[r], w.cu_k[r] = cu_k[r];
-  const int qt = query_tile(w, shape->heads, shape->causal);
-  const int64_t tiles = list_tiles(&w, qt, shape->causal);
-  const int64_t blocks = workgroups(tiles, shape->heads, shape->kv_heads);
-  if (blocks > 0x7fffffff) return EAS_ERR_UNSUPPORTED;
+  float* part = static_cast<float*>(workspace);
   const PromptArgs a = {q, k, v, out, lse, shape->q, shape->k, shape->v, shape->out, shape->heads,
-                        shape->heads / shape->kv_heads, shape->causal, (int)tiles, shape->scale * kLog2e};
-  const unsigned grid = (unsigned)blocks;
-  const hipStream_t st_ = (hipStream_t)stream;
+                        shape->heads / shape->kv_heads, shape->causal, 0, shape->scale * kLog2e, part,
+                        j.n ? part + (int64_t)w.slot0[n_seqs] * shape->head_dim : nullptr};
 #define EAS_PROMPT_CASE(DT, T, D) \
-  if (shape->dtype == DT && shape->head_dim == D) \
-    return qt == 256 ? launch<T, D, 8>(a, w, grid, st_) : launch<T, D, 4>(a, w, grid, st_)
+  if (shape->dtype == DT && shape->head_dim == D) return launch_all<T, D>(shape, a, &w, j, (hipStream_t)stream)
   EAS_PROMPT_CASE(EAS_BF16, bf16, 64);
   EAS_PROMPT_CASE(EAS_BF16, bf16, 128);
   EAS_PROMPT_CASE(EAS_FP16, f16, 64);

@@ -22,7 +22,7 @@ PTR = 0x10000   # an aligned address that nothing reads
 def test_every_declared_symbol_is_exported():
     text = open(os.path.join(ROOT, "include", "eas_attention.h")).read()
     names = sorted(set(re.findall(r"^\s*eas_status\s+(eas_\w+)\s*\(", text, re.M)))
-    assert len(names) == 5
+    assert len(names) == 6
     for n in names:
         assert hasattr(eas.LIB, n), n
     assert list(A.EXPORTS) == names
@@ -42,10 +42,12 @@ def ints(*v):
     return (ctypes.c_int32 * len(v))(*v)
 
 
-def prompt(s=None, q=PTR, k=PTR, v=PTR, cu_q=(0, 5, 9), cu_k=None, n=None, out=PTR, lse=None):
+def prompt(s=None, q=PTR, k=PTR, v=PTR, cu_q=(0, 5, 9), cu_k=None, n=None, out=PTR, lse=None, ws=PTR,
+           ws_bytes=1 << 30):
     cu = None if cu_q is None else ints(*cu_q)
     return eas.LIB.eas_prompt_attention(ctypes.byref(s or shape()), q, k, v, cu, None if cu_k is None else ints(*cu_k),
-                                        (len(cu_q) - 1 if cu_q else 1) if n is None else n, out, lse, None)
+                                        (len(cu_q) - 1 if cu_q else 1) if n is None else n, out, lse, ws, ws_bytes,
+                                        None)
 
 
 SHAPE_REFUSALS = [
@@ -69,16 +71,39 @@ def test_prompt_attention_refuses_shapes(over, status):
     (dict(cu_k=(0, 5, 4)), SHAPE), (dict(cu_k=(2, 5, 8)), SHAPE), (dict(n=-1), CAPACITY),
     (dict(cu_q=tuple(range(66))), CAPACITY), (dict(q=None), BAD), (dict(k=None), BAD), (dict(v=None), BAD),
     (dict(out=None), BAD), (dict(q=PTR + 8), BAD), (dict(k=PTR + 2), BAD), (dict(out=PTR + 8), BAD),
-    (dict(lse=PTR + 2), BAD),
+    (dict(lse=PTR + 2), BAD), (dict(cu_q=(0, 9), cu_k=(0, 90000), ws=None), BAD),
+    (dict(cu_q=(0, 9), cu_k=(0, 90000), ws=PTR + 8), BAD), (dict(cu_q=(0, 9), cu_k=(0, 90000), ws_bytes=64), CAPACITY),
+    (dict(cu_q=(0, 9), cu_k=(0, (1 << 30) + 1)), UNSUPPORTED),
 ], ids=lambda x: str(x))
 def test_prompt_attention_refuses_arguments(over, status):
     assert prompt(**over) == status
-    assert eas.LIB.eas_prompt_attention(None, PTR, PTR, PTR, ints(0, 5), None, 1, PTR, None, None) == BAD
+    assert eas.LIB.eas_prompt_attention(None, PTR, PTR, PTR, ints(0, 5), None, 1, PTR, None, None, 0,
+                                        None) == BAD
 
 
 def test_prompt_attention_refuses_more_work_items_than_a_launch_holds():
     s = shape(heads=1024, kv_heads=1024, q=(1 << 17, 128), k=(1 << 17, 128), v=(1 << 17, 128), out=(1 << 17, 128))
     assert prompt(s, cu_q=(0, 2147483647)) == UNSUPPORTED
+
+
+def test_prompt_attention_workspace():
+    def size(cu_q, cu_k, s=None):
+        b = ctypes.c_int64(-1)
+        assert eas.LIB.eas_prompt_attention_workspace(ctypes.byref(s or shape()), ints(*cu_q), ints(*cu_k),
+                                                      len(cu_q) - 1, ctypes.byref(b)) == 0
+        return b.value
+    assert size((0, 100, 300), (0, 100, 300)) == 0 and size((0,), (0,)) == 0
+    assert size((0, 8000), (0, 8000)) == 0                  # many queries fill the chip
+    one = size((0, 100), (0, 100000))
+    assert one > 0 and size((0, 100, 200), (0, 100000, 200000)) == 2 * one
+    assert size((0, 0, 100), (0, 50000, 150000)) == one
+    assert prompt(cu_q=(0, 100), cu_k=(0, 100000), ws_bytes=one - 1) == CAPACITY
+    call, b = eas.LIB.eas_prompt_attention_workspace, ctypes.c_int64()
+    assert call(None, ints(0, 5), None, 1, ctypes.byref(b)) == BAD
+    assert call(ctypes.byref(shape()), None, None, 1, ctypes.byref(b)) == BAD
+    assert call(ctypes.byref(shape()), ints(0, 5), None, 1, None) == BAD
+    assert call(ctypes.byref(shape()), ints(1, 5), None, 1, ctypes.byref(b)) == SHAPE
+    assert call(ctypes.byref(shape()), ints(0, 5), None, 65, ctypes.byref(b)) == CAPACITY
 
 
 def test_prompt_attention_with_nothing_to_do():

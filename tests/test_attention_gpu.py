@@ -93,6 +93,7 @@ LENS = {
     "behind": ([1, 40, 70, 128, 3], [200, 129, 70, 333, 64]),            # queries behind cached keys
     "few_keys": ([50, 5, 130, 3], [20, 0, 64, 1]),                       # first queries see nothing
     "long": ([300, 517], [700, 517]),
+    "runs": ([5, 33, 0, 2, 129], [13000, 8193, 9000, 8192, 130]),        # few queries over keys in several runs
 }
 
 
@@ -159,6 +160,61 @@ def test_prompt_attention_does_not_depend_on_the_batch():
         assert torch.equal(one, every[s]) and torch.equal(one_lse, lse[s])
 
 
+def test_prompt_attention_of_a_large_launch_is_that_of_a_small_one():
+    """The workgroup's size goes by the launch's work (here 256 queries, and 128 for one sequence), a query's
+    arithmetic does not."""
+    torch, A = lib()
+    c = [0, 4000, 8000, 12000, 16100]
+    q, k, v = (make(torch, (c[-1], h, 64), torch.bfloat16, 24 + h) for h in (16, 8, 8))
+    every, lse = A.prompt_attention(q, k, v, c, with_lse=True)
+    for r in (0, 3):
+        s = slice(c[r], c[r + 1])
+        one, one_lse = A.prompt_attention(q[s], k[s], v[s], [0, c[r + 1] - c[r]], with_lse=True)
+        assert torch.equal(one, every[s]) and torch.equal(one_lse, lse[s])
+
+
+def test_prompt_attention_of_many_sequences():
+    """More query tiles than the work list holds, empty sequences among them."""
+    torch, A = lib()
+    lens = [1700 if i % 3 else 0 for i in range(64)]
+    c = cu(lens)
+    q, k, v = (make(torch, (c[-1], h, 64), torch.float16, 27 + h) for h in (2, 1, 1))
+    every, lse = A.prompt_attention(q, k, v, c, with_lse=True)
+    assert c[-1] > 768 * 64
+    for r in (1, 32, 62):
+        s = slice(c[r], c[r + 1])
+        one, one_lse = A.prompt_attention(q[s], k[s], v[s], [0, lens[r]], with_lse=True)
+        assert torch.equal(one, every[s]) and torch.equal(one_lse, lse[s])
+    run_prompt(q[:c[2]], k[:c[2]], v[:c[2]], [0, 0, 200], [0, 0, 200], True)
+
+
+def test_prompt_attention_runs_do_not_depend_on_the_batch():
+    torch, A = lib()
+    new, held = [100, 700, 40, 9], [13000, 300, 0, 8190]
+    cq, ck = cu(new), cu([a + b for a, b in zip(new, held)])
+    q = make(torch, (cq[-1], 4, 128), torch.bfloat16, 28)
+    k, v = (make(torch, (ck[-1], 2, 128), torch.bfloat16, s) for s in (29, 30))
+    every, lse = A.prompt_attention(q, k, v, cq, ck, with_lse=True)
+    for r in range(4):
+        s, t = slice(cq[r], cq[r + 1]), slice(ck[r], ck[r + 1])
+        one, one_lse = A.prompt_attention(q[s], k[t], v[t], [0, new[r]], [0, new[r] + held[r]], with_lse=True)
+        assert torch.equal(one, every[s]) and torch.equal(one_lse, lse[s])
+
+
+@pytest.mark.parametrize("what", ["nan", "inf"])
+def test_prompt_attention_hidden_tokens_in_runs(what):
+    torch, A = lib()
+    q = make(torch, (64, 2, 128), torch.float16, 33)
+    k, v = make(torch, (9000, 1, 128), torch.float16, 34), make(torch, (9000, 1, 128), torch.float16, 35)
+    want, want_lse = A.prompt_attention(q, k, v, [0, 64], [0, 9000], with_lse=True)
+    k2, v2 = k.clone(), v.clone()
+    k2[8980:, :, 3], v2[8980:, :, 5] = float(what), float(what)     # hidden from the first 44 queries
+    got, lse = A.prompt_attention(q, k2, v2, [0, 64], [0, 9000], with_lse=True)
+    assert (got[:44].float() - want[:44].float()).abs().max() <= 4 * HALF["float16"] * v.abs().max()
+    assert (lse[:44] - want_lse[:44]).abs().max() <= 1e-4
+    assert not torch.isfinite(got[44:, :, 5]).any()
+
+
 @pytest.mark.parametrize("what", ["nan", "inf"])
 def test_prompt_attention_hidden_tokens_may_hold_anything(what):
     """A later token's key and value never reach an earlier query, NaN and infinities included."""
@@ -222,6 +278,8 @@ def test_binding_refusals():
                 lambda: A.prompt_attention(q, k, k, [0, 10], out=q[:9]),
                 lambda: A.prompt_attention(q, k, k, [0, 10], lse=torch.empty(10, 4, device="cuda").half()),
                 lambda: A.prompt_attention(q, k, k, list(range(11)) + [10] * 60),
+                lambda: A.prompt_attention(q[:2], k.expand(-1, 2, -1), k, [0, 2], [0, 10],
+                                           workspace=torch.zeros(8, device="cuda")),
                 lambda: A.prompt_attention(q.transpose(1, 2), k, k, [0, 10])):
         with pytest.raises((ValueError, RuntimeError)):
             bad()
