@@ -63,7 +63,8 @@ def parse():
     ap.add_argument("--no-profile", action="store_true", help="skip the event-timed roofline pass")
     ap.add_argument("--colocation", default="",
                     help="micro-batch sizes of a co-location profile of the headline preset: encode latency "
-                         "with 12.5/30/50/70/90%% of the CUs and the smallest-safe-share table ('' to skip)")
+                         "with 12.5/30/50/70/90%% of the CUs and the smallest-safe-share table, and beside a "
+                         "prefill worker's attention ('' to skip)")
     ap.add_argument("--details", default="", help="file to write the whole record to (JSON)")
     ap.add_argument("--copy-calib-mib", type=int, default=0,
                     help="only run a plain device copy of this many MiB (HBM counter calibration)")
@@ -376,12 +377,19 @@ def colocation(wl, sizes, reps=3):
     exclusive, latency = K.profile(run_for, sizes, K.LEVELS, reps, max_s=3.0, log=log)
     wl.stream = keep
     table = K.safe_share_table(latency, exclusive)
+    work, live = K.PrefillWork(), {}
+    for b in sizes:
+        live[str(b)] = K.beside_prefill(run_for(b), work, reps)
+        log("micro-batch %d beside prompt and cache attention: %s" % (
+            b, ", ".join("%s %.3f ms" % kv for kv in live[str(b)].items())))
+    wl.stream = keep
     return {"levels": list(K.LEVELS), "micro_batches": list(sizes), "threshold": K.THRESHOLD,
             "reps": reps, "cus": K.device_cus(),
             "exclusive_ms": {str(b): exclusive[b] for b in sizes},
             "latency_ms": {str(lv): {str(b): latency[lv][b] for b in sizes} for lv in K.LEVELS},
             "largest_safe_batch": {str(lv): table[lv] for lv in K.LEVELS},
             "share_for_batch": {str(b): K.select_share(table, b) for b in sizes},
+            "beside_prefill_ms": live,
             "mechanism": "CUs held by a reservation kernel (one workgroup per CU) while encode runs on the rest"}
 
 

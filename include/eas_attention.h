@@ -72,7 +72,7 @@ typedef struct {
  * k and v may hold anything, NaN included, outside the sequences' keys.
  * workspace: device, 16-byte aligned, at least the bytes that
  * eas_prompt_attention_workspace gives for the same arguments (0: NULL is
- * fine), which is more than 0 only where few queries see over 4,096 keys; calls
+ * fine), which is more than 0 only where few queries see 8,192 keys or more; calls
  * that may overlap, captured ones included, need one each.  Nothing in it has
  * to be set before, or is kept from call to call.
  * Errors: INVALID_ARG, SHAPE (cu_q, cu_k), CAPACITY (n_seqs, the workspace),
@@ -158,8 +158,8 @@ eas_status eas_kv8_rows(const eas_kv8_cache* cache, int32_t dtype, const int32_t
  * touched.  A query that sees no token gets zeros and lse -inf.
  * lse: device fp32 [n_rows, heads] or NULL.
  * workspace: device, 16-byte aligned, at least the bytes that
- * eas_kv8_attention_workspace gives for the same arguments (0: NULL is fine);
- * calls that may overlap, captured ones included, need one each.  Nothing in
+ * eas_kv8_attention_workspace gives for the same arguments (0, up to a max_len
+ * of 512: NULL is fine); calls that may overlap, captured ones included, need one each.  Nothing in
  * it has to be set before, or is kept from call to call.
  * A sequence's result does not depend on the other sequences, on max_q, on
  * max_len or on which pages hold its tokens, to the bit. */

@@ -15,6 +15,7 @@ from .eas import EAS_MAX_SEQS, EAS_OK, LIB, EasError  # noqa: F401  (EAS_MAX_SEQ
 P, I32, I64, VP = ctypes.POINTER, ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p
 EAS_FP32, EAS_BF16, EAS_FP16 = range(3)
 EAS_KV_INT8, EAS_KV_E4M3 = range(2)
+SPLIT_KEYS, SPLIT_TOKENS = 8192, 512   # calls below / up to these need no workspace
 _DTYPE = {torch.float32: EAS_FP32, torch.bfloat16: EAS_BF16, torch.float16: EAS_FP16}
 _FORMAT = {torch.int8: EAS_KV_INT8, torch.float8_e4m3fn: EAS_KV_E4M3}
 
@@ -61,15 +62,14 @@ _current_stream = torch._C._cuda_getCurrentRawStream   # of a device; torch.cuda
 def _rows(t, name, heads, dim, dtype, index):
     """Strides of [rows, heads, dim] (heads None: any) with consecutive dims."""
     shape = t.shape
-    if len(shape) != 3 or shape[2] != dim or (heads is not None and shape[1] != heads):
-        raise ValueError("%s has shape %s, wanted [rows, %s, %d]" % (name, tuple(shape), heads or "heads", dim))
-    if t.dtype != dtype or t.get_device() != index:
-        raise ValueError("%s is %s on %s, wanted %s on cuda:%d" % (name, t.dtype, t.device, dtype, index))
-    row, head, one = t.stride()
-    if one != 1 and t.numel():
-        raise ValueError("%s: the values of a head must be consecutive" % name)
-    # a stride that no step is taken by says nothing
-    return Strides(row if shape[0] > 1 else 0, head if shape[1] > 1 else 0)
+    if len(shape) == 3 and t.dtype == dtype and t.get_device() == index:
+        n, h, d = shape
+        row, head, one = t.stride()
+        if d == dim and (heads is None or h == heads) and (one == 1 or not t.numel()):
+            # a stride that no step is taken by says nothing
+            return Strides(row if n > 1 else 0, head if h > 1 else 0)
+    raise ValueError("%s must be [rows, %s, %d], the values of a head consecutive, %s on cuda:%d: got %s, strides %s, %s "
+                     "on %s" % (name, heads or "heads", dim, dtype, index, tuple(shape), t.stride(), t.dtype, t.device))
 
 
 def _device(t):
@@ -112,7 +112,7 @@ def _outputs(q, out, lse, with_lse, index, stream):
     if lse is None:
         if not with_lse:
             return out, None, strides, None
-        lse = _on(stream, lambda: torch.empty((rows, heads), dtype=torch.float32, device=q.device))
+        lse = _on(stream, lambda: q.new_empty((rows, heads), dtype=torch.float32))
     elif lse.dtype != torch.float32 or lse.get_device() != index or lse.shape != (rows, heads) \
             or not lse.is_contiguous():
         raise ValueError("lse must be a contiguous float32 tensor [%d, %d] on cuda:%d" % (rows, heads, index))
@@ -165,7 +165,8 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, *, causal=True, scale=None, out=N
                       qs, ks, vs, strides)
     n, cu_q_ptr, cu_k_ptr = len(cu_q) - 1, cu_q.buffer_info()[0], cu_k.buffer_info()[0]
     need = I64()
-    _check(LIB.eas_prompt_attention_workspace(shape, cu_q_ptr, cu_k_ptr, n, need), "prompt_attention")
+    if cu_k[-1] >= SPLIT_KEYS:
+        _check(LIB.eas_prompt_attention_workspace(shape, cu_q_ptr, cu_k_ptr, n, need), "prompt_attention")
     workspace, ws_ptr, ws_bytes = _workspace(workspace, need.value, index, q.device, stream)
     _check(LIB.eas_prompt_attention(shape, q.data_ptr(), k.data_ptr(), v.data_ptr(), cu_q_ptr, cu_k_ptr, n,
                                     out.data_ptr(), lse_ptr, ws_ptr, ws_bytes,
@@ -183,16 +184,16 @@ class Kv8Cache:
     def __init__(self, k, v, k_scale, v_scale):
         if k.dim() != 4 or k.dtype not in _FORMAT:
             raise ValueError("k must be int8 or float8_e4m3fn codes [pages, kv_heads, page_tokens, head_dim]")
-        n, h, p, d = k.shape
-        for t, name, shape, dtype in ((k, "k", (n, h, p, d), k.dtype), (v, "v", (n, h, d, p), k.dtype),
+        (n, h, p, d), codes, index = k.shape, k.dtype, k.get_device()
+        for t, name, shape, dtype in ((k, "k", (n, h, p, d), codes), (v, "v", (n, h, d, p), codes),
                                       (k_scale, "k_scale", (n, h), torch.float32),
                                       (v_scale, "v_scale", (n, h), torch.float32)):
-            if tuple(t.shape) != shape or t.dtype != dtype or t.device != k.device or not t.is_contiguous():
+            if t.shape != shape or t.dtype != dtype or t.get_device() != index or not t.is_contiguous():
                 raise ValueError("%s must be a contiguous %s tensor of shape %s on %s" % (name, dtype, shape, k.device))
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.n_pages, self.kv_heads, self.page_tokens, self.head_dim = n, h, p, d
-        self.device, self._index = k.device, k.get_device()
-        self._c = Kv8CacheStruct(_FORMAT[k.dtype], h, d, p, n, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(),
+        self.device, self._index = k.device, index
+        self._c = Kv8CacheStruct(_FORMAT[codes], h, d, p, n, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(),
                                  v_scale.data_ptr())
 
     @classmethod
@@ -281,7 +282,8 @@ class Kv8Cache:
         shape = AttnShape(code, heads, self.kv_heads, dim, 1 if causal else 0, dim ** -0.5 if scale is None else scale,
                           qs, _NO_STRIDES, _NO_STRIDES, strides)
         need = I64()
-        _check(LIB.eas_kv8_attention_workspace(shape, most_q, most, n, need), "Kv8Cache.attention")
+        if most > SPLIT_TOKENS:
+            _check(LIB.eas_kv8_attention_workspace(shape, most_q, most, n, need), "Kv8Cache.attention")
         workspace, ws_ptr, ws_bytes = _workspace(workspace, need.value, index, self.device, stream)
         _check(LIB.eas_kv8_attention(self._c, shape, q.data_ptr(), rows, cu, most_q, _ints(lens, "lens", index, (n,)),
                                      most, table, max_pages, n, out.data_ptr(), lse_ptr, ws_ptr, ws_bytes,

@@ -22,6 +22,12 @@ for each of the device's 32 shader engines.  With fewer, some shader engine has
 no free CU, and the encoder's kernels wait behind it until the reservation
 ends (measured: 26 free CUs stall the encoder for the whole reservation, 32 do
 not).
+
+A held CU does no work, so the table says nothing about the memory and the power
+that a prefill worker shares with encode.  ``PrefillWork`` is such a worker's
+attention (``attention.py``): the prompts of a few requests, their keys and values
+into the 8-bit cache, and a decoding step; ``beside_prefill`` times an encode
+micro-batch and that work alone and side by side on two streams.
 """
 import ctypes
 import statistics
@@ -176,3 +182,82 @@ def select_share(table, batch):
     when none does."""
     fits = [lv for lv, b in table.items() if b >= batch]
     return min(fits) if fits else 1.0
+
+
+class PrefillWork:
+    """The attention of a local prefill worker on a few packed prompts: one step is prompt attention, the append of
+    its keys and values to an 8-bit cache, and one decoding step over that cache (a layer's share of each)."""
+
+    def __init__(self, lens=(620, 1201, 97, 2309, 577, 1764, 333, 915), heads=28, kv_heads=4, head_dim=128,
+                 page_tokens=64, seed=0):
+        import torch
+        from . import attention
+        g = torch.Generator(device="cuda")
+        g.manual_seed(seed)
+
+        def rows(n, h):
+            return torch.randn((n, h, head_dim), generator=g, device="cuda").to(torch.bfloat16)
+
+        def ints(v):
+            return torch.tensor(v, dtype=torch.int32, device="cuda")
+        n, total = len(lens), sum(lens)
+        self.cu = [sum(lens[:i]) for i in range(n + 1)]
+        self.q, self.k, self.v = rows(total, heads), rows(total, kv_heads), rows(total, kv_heads)
+        self.q1, self.k1, self.v1 = rows(n, heads), rows(n, kv_heads), rows(n, kv_heads)
+        need = [length // page_tokens + 1 for length in lens]
+        table = [[sum(need[:r]) + i if i < need[r] else -1 for i in range(max(need))] for r in range(n)]
+        self.cache = attention.Kv8Cache.empty(sum(need), kv_heads, head_dim, page_tokens)
+        self.pages, self.cu_new, self.longest = ints(table), ints(self.cu), max(lens)
+        self.none, self.held, self.now = ints([0] * n), ints(lens), ints([length + 1 for length in lens])
+        self.prompt = attention.prompt_attention
+        self.out, self.out1 = torch.empty_like(self.q), torch.empty_like(self.q1)
+
+    def step(self, stream=None):
+        """Enqueues one step; the prompts' results are in ``out``, the decoding step's in ``out1``."""
+        self.prompt(self.q, self.k, self.v, self.cu, out=self.out, stream=stream)
+        self.cache.append(self.k, self.v, self.none, self.pages, cu_new=self.cu_new, max_new=self.longest, stream=stream)
+        self.cache.append(self.k1, self.v1, self.held, self.pages, stream=stream)
+        self.cache.attention(self.q1, self.now, self.pages, max_len=self.longest + 1, out=self.out1, stream=stream)
+
+
+def beside_prefill(run, work, reps=3):
+    """Times (ms, medians of ``reps``) of ``run(stream)`` -- one encode micro-batch -- and of one ``work.step``, each
+    alone and side by side on two streams: {"encode_alone", "encode_beside", "prefill_alone", "prefill_beside"}.
+    Side by side the prefill stream is given steps enough to outlast the micro-batch."""
+    import torch
+    measure, prefill = _stream("measure"), _stream("prefill")
+
+    def event():
+        return torch.cuda.Event(enable_timing=True)
+
+    def encode():
+        e0, e1 = event(), event()
+        e0.record(measure)
+        run(measure)
+        e1.record(measure)
+        return e0, e1
+
+    def steps(n):
+        e0, e1 = event(), event()
+        e0.record(prefill)
+        for _ in range(n):
+            work.step(prefill)
+        e1.record(prefill)
+        return e0, e1
+
+    def ms(events, n=1):
+        events[1].synchronize()
+        return events[0].elapsed_time(events[1]) / n
+    torch.cuda.synchronize()
+    ms(encode()), ms(steps(2))   # warm-up
+    alone, each, beside, step_beside = [], [], [], []
+    for _ in range(reps):
+        alone.append(ms(encode()))
+        each.append(ms(steps(8), 8))
+        n = int(3 * alone[-1] / each[-1]) + 4
+        p = steps(n)
+        e = encode()
+        beside.append(ms(e))
+        step_beside.append(ms(p, n))
+    return {k: statistics.median(v) for k, v in (("encode_alone", alone), ("encode_beside", beside),
+                                                 ("prefill_alone", each), ("prefill_beside", step_beside))}

@@ -442,7 +442,7 @@ extern "C" eas_status eas_kv8_attention(const eas_kv8_cache* cache, const eas_at
   st = check_strides(shape->q);
   if (st == EAS_OK) st = check_table(cache, pages, max_pages, n_seqs);
   if (st != EAS_OK) return st;
-  if (n_rows < 0 || max_q < 0 || max_len < 0 || !lens || (uintptr_t)lens % 4 || (uintptr_t)cu_q % 4 ||
+  if (n_rows < 0 || max_q < 0 || max_len < 0 || (!lens && n_seqs > 0) || (uintptr_t)lens % 4 || (uintptr_t)cu_q % 4 ||
       (uintptr_t)lse % 4)
     return EAS_ERR_INVALID_ARG;
   st = check_out_strides(shape->out, n_rows, shape->heads, shape->head_dim);

@@ -370,7 +370,7 @@ extern "C" eas_status eas_kv8_append(const eas_kv8_cache* cache, int32_t dtype, 
   if (st == EAS_OK) st = check_strides(v_strides);
   if (st == EAS_OK) st = check_table(cache, pages, max_pages, n_seqs);
   if (st != EAS_OK) return st;
-  if (n_rows < 0 || max_new < 0 || !held || (uintptr_t)held % 4 || (uintptr_t)cu_new % 4) return EAS_ERR_INVALID_ARG;
+  if (n_rows < 0 || max_new < 0 || (!held && n_seqs > 0) || (uintptr_t)held % 4 || (uintptr_t)cu_new % 4) return EAS_ERR_INVALID_ARG;
   if (n_rows == 0 || max_new == 0 || n_seqs == 0) return EAS_OK;
   if (!k || !v || !aligned16(k) || !aligned16(v)) return EAS_ERR_INVALID_ARG;
   AppendArgs a = {kv8_args(cache), k, v, k_strides, v_strides, cu_new, held, pages, n_rows, max_new, max_pages,

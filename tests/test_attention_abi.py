@@ -201,6 +201,8 @@ def test_cache_calls_with_nothing_to_do():
         assert rows(k=None, v=None, **over) == eas.EAS_OK
         assert attend(q=None, out=None, ws=None, **over) == eas.EAS_OK
     assert append(most=0) == rows(most=0) == attend(most_q=0) == eas.EAS_OK
+    # no sequences: their arrays may be empty
+    assert append(n=0, held=None, pages=None) == attend(n=0, lens=None, pages=None) == rows(n=0, pages=None) == eas.EAS_OK
 
 
 def workspace(max_q, max_len, n, s=None):
@@ -222,6 +224,17 @@ def test_workspace_sizes_grow_with_queries_and_tokens_up_to_a_bound():
     assert call(ctypes.byref(shape()), -1, 1, 1, ctypes.byref(b)) == BAD
     assert call(ctypes.byref(shape()), 1, 1, 1, None) == BAD
     assert call(ctypes.byref(shape(head_dim=80)), 1, 1, 1, ctypes.byref(b)) == UNSUPPORTED
+
+
+def test_the_binding_knows_where_no_workspace_is_needed():
+    b = ctypes.c_int64(-1)
+    for heads, kv_heads in ((1, 1), (28, 4), (1024, 8)):
+        s = shape(heads=heads, kv_heads=kv_heads)
+        for lq in (1, 100, 128, 1000):
+            assert eas.LIB.eas_prompt_attention_workspace(ctypes.byref(s), ints(0, lq), ints(0, A.SPLIT_KEYS - 1), 1,
+                                                          ctypes.byref(b)) == 0 and b.value == 0
+        for max_q in (1, 7, 300):
+            assert workspace(max_q, A.SPLIT_TOKENS, 64, s) == 0
 
 
 def test_binding_refuses_tensors_of_other_devices_and_kinds():

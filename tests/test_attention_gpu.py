@@ -609,6 +609,75 @@ def test_cache_behind_four_gib():
         assert torch.equal(a, b)
 
 
+def test_bounds_that_are_smaller_than_the_batch():
+    """Tokens beyond max_new are dropped, rows beyond max_rows not written, queries beyond max_q not computed and
+    tokens beyond max_len not seen."""
+    torch, A = lib()
+    both = Both("int8", 8, 1, 16, 64)
+    table = np.array([[1, 2, 3], [5, 6, 7]])
+    k, v = make(torch, (60, 1, 64), torch.float16, 240), make(torch, (60, 1, 64), torch.float16, 241)
+    both.gpu.append(k, v, i32(torch, [0, 3]), i32(torch, table), i32(torch, [0, 20, 60]), max_new=25)
+    both.ref.append(f64(k)[:20], f64(v)[:20], 0, table[0])
+    both.ref.append(f64(k)[20:45], f64(v)[20:45], 3, table[1])
+    assert (both.gpu.k.view(torch.uint8)[6, :, 12:] == 255).all() and (both.gpu.k.view(torch.uint8)[7] == 255).all()
+    got = torch.full((48, 1, 64), 5.0, dtype=torch.float16, device="cuda")
+    both.gpu.rows(i32(torch, table), i32(torch, [0, 20, 48]), 48, max_len=7, dtype=torch.float16, k=got)
+    for r, a in ((0, 0), (1, 20)):
+        if r == 0:
+            np.testing.assert_array_equal(f64(got)[a:a + 7], both.ref.rows("k", table[r], 0, 7))
+        assert (got[a + 7:a + 20] == 5.0).all()
+    q = make(torch, (5, 2, 64), torch.float16, 242)
+    out = torch.full(q.shape, 9.0, dtype=q.dtype, device="cuda")
+    both.gpu.attention(q, i32(torch, [20, 0]), i32(torch, table), cu_q=i32(torch, [0, 4, 5]), max_q=2, max_len=11,
+                       causal=False, out=out)
+    assert (out[2:4] == 9.0).all() and (out[4] == 0).all()
+    want, _ = both.gpu.attention(q[:2], i32(torch, [11]), i32(torch, table[:1]), causal=False)
+    assert torch.equal(out[:2], want)
+
+
+def test_pages_shared_for_reading():
+    torch, A = lib()
+    both, table = filled("e4m3", [100, 40], 16, 2, 64, 250)
+    shared = table.copy()
+    shared[1, :2] = table[0, :2]                       # the second sequence starts with the first one's pages
+    q = make(torch, (2, 4, 64), torch.bfloat16, 251)
+    out, lse = both.gpu.attention(q, i32(torch, [100, 40]), i32(torch, shared), with_lse=True)
+    check_decode(both, q, [100, 40], shared, [1, 1], 0.125, True, out, lse)
+    both.check_rows([100, 40], shared, torch.bfloat16)
+
+
+def test_rows_of_keys_or_values_alone():
+    import ctypes
+    torch, A = lib()
+    both, table = filled("int8", [50], 32, 2, 128, 260)
+    t, c = i32(torch, table), i32(torch, [0, 50])
+    want = both.gpu.rows(t, c, 50)
+    s = A.Strides(256, 128)
+    for i in range(2):
+        got = torch.zeros_like(want[0])
+        ptr = [None, None]
+        ptr[i] = got.data_ptr()
+        assert A.LIB.eas_kv8_rows(both.gpu._c, A.EAS_BF16, t.data_ptr(), t.shape[1], 1, c.data_ptr(), None, 50, 50, ptr[0],
+                                  s, ptr[1], s, torch.cuda.current_stream().cuda_stream) == 0
+        assert torch.equal(got, want[i])
+
+
+def test_empty_batches():
+    torch, A = lib()
+    q, k = make(torch, (4, 2, 64), torch.bfloat16, 270), make(torch, (0, 1, 64), torch.bfloat16, 271)
+    out, lse = A.prompt_attention(q, k, k, [0, 4], [0, 0], with_lse=True)
+    assert (out == 0).all() and torch.isneginf(lse).all()
+    for cu_q in ([0], [0, 0]):
+        out, lse = A.prompt_attention(q[:0], k, k, cu_q, with_lse=True)
+        assert out.shape == (0, 2, 64) and lse.shape == (0, 2)
+    cache = A.Kv8Cache.empty(2, 1, 64, 16)
+    none, pages = i32(torch, []), torch.zeros((0, 3), dtype=torch.int32, device="cuda")
+    cache.append(k, k, none, pages)
+    assert cache.attention(q[:0], none, pages)[0].shape == (0, 2, 64)
+    assert cache.rows(pages, i32(torch, [0]), 0)[0].shape == (0, 1, 64)
+    torch.cuda.synchronize()
+
+
 # ---- streams, graphs, and the chain ---------------------------------------------------
 
 def test_other_stream():
