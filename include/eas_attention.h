@@ -159,7 +159,7 @@ eas_status eas_kv8_rows(const eas_kv8_cache* cache, int32_t dtype, const int32_t
  * lse: device fp32 [n_rows, heads] or NULL.
  * workspace: device, 16-byte aligned, at least the bytes that
  * eas_kv8_attention_workspace gives for the same arguments (0, up to a max_len
- * of 512: NULL is fine); calls that may overlap, captured ones included, need one each.  Nothing in
+ * of 1,024: NULL is fine); calls that may overlap, captured ones included, need one each.  Nothing in
  * it has to be set before, or is kept from call to call.
  * A sequence's result does not depend on the other sequences, on max_q, on
  * max_len or on which pages hold its tokens, to the bit. */

@@ -21,7 +21,8 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-u
 # and their running maxima are taken without NaN-quieting copies (the scores
 # are finite or -inf there, never NaN)
 _ATTENTION = ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans"]
-FILE_FLAGS = {"attention_dma.hip": _ATTENTION, "prompt_attention.hip": _ATTENTION}
+FILE_FLAGS = {"attention_dma.hip": _ATTENTION, "prompt_attention.hip": _ATTENTION,
+              "kv8_attention.hip": _ATTENTION[:2]}
 
 
 # Host-code sanitizers (AddressSanitizer + UndefinedBehaviorSanitizer) for a

@@ -21,6 +21,8 @@
 // A sequence's tokens are split into runs by a rule on its own length and queries only,
 // so its result does not depend on the batch; each run's result goes to the workspace
 // and a second kernel joins them in order.
+#include <type_traits>
+
 #include "attention_ops.h"
 
 namespace eas {
@@ -31,13 +33,13 @@ constexpr int NW = 4;            // waves per workgroup
 constexpr int MAX_RUNS = 64;     // runs per sequence
 constexpr int RUN_ROWS = 256;    // runs * queries of a sequence that is split
 
-// Runs that `len` tokens are split into for nq queries, and a run's tokens: 512 at least, 1,024 over 2,048 tokens.
-// A run costs its first loads' latency and its share of the join, so full batches want long ones (64 sequences of
-// 4,096 tokens, 8 heads of 128: 147 us with runs of 256 tokens, 124 with 512, 117 with 1,024; 16 of 32,768: 246 /
-// 221 / 204), single sequences short ones (one of 4,096: 11.2 / 12.6 / 16.1 us).
+// Runs that `len` tokens are split into for nq queries, and a run's tokens: 1,024 at least.  A run costs its first
+// loads' latency and its share of the join, so full batches want long ones (16 sequences of 32,768 tokens, 8 heads of
+// 128: 224 us with runs of 512 tokens, 206 with 1,024; 32 of 2,048, 20 heads of 64: 36.3 and 35.0), single sequences
+// short ones (one of 4,096: 11.3 and 13.8 us).
+constexpr int SHORTEST_RUN = 1024;
 __host__ __device__ inline int n_runs(int len, int nq) {
-  const int shortest = len <= 2048 ? 512 : 1024;
-  const int by_len = (int)(((int64_t)len + shortest - 1) / shortest);
+  const int by_len = (int)(((int64_t)len + SHORTEST_RUN - 1) / SHORTEST_RUN);
   int most = nq > 0 ? RUN_ROWS / nq : 1;
   most = most < 1 ? 1 : most > MAX_RUNS ? MAX_RUNS : most;
   return by_len < 1 ? 1 : by_len < most ? by_len : most;
@@ -46,15 +48,10 @@ __host__ __device__ inline int run_tokens(int len, int runs) {
   constexpr int step = NW * TILE;
   return (int)(((int64_t)len + (int64_t)runs * step - 1) / ((int64_t)runs * step)) * step;
 }
-// the most runs of a sequence of up to max_len tokens (2,048 have 4, 2,049 have 3)
-inline int most_runs(int max_len) {
-  const int upto = n_runs(max_len < 2048 ? max_len : 2048, 1), over = n_runs(max_len, 1);
-  return upto > over ? upto : over;
-}
 // Workspace slots per sequence and head: at least n_runs * nq for every nq <= max_q, len <= max_len
 // of a sequence that is split
 inline int64_t slots(int max_q, int max_len) {
-  const int64_t rows = (int64_t)most_runs(max_len) * max_q;
+  const int64_t rows = (int64_t)n_runs(max_len, 1) * max_q;
   return rows < RUN_ROWS ? rows : RUN_ROWS;
 }
 
@@ -155,7 +152,8 @@ __global__ __launch_bounds__(64 * NW) void kv8_attention_kernel(Kv8AttnArgs a) {
   const int runs = n_runs(s.len, s.nq);
   if (run >= runs) return;
   const int each = run_tokens(s.len, runs);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
   // this lane's query, and how many tokens it sees
   const int rho = rt * 16 + c;
@@ -168,20 +166,45 @@ __global__ __launch_bounds__(64 * NW) void kv8_attention_kernel(Kv8AttnArgs a) {
   const long t_begin = (long)run * each;
   const int t_end = (int)min((long)most, t_begin + each);
 
+  // The next tile's keys are fetched as soon as a tile's scores have taken theirs, its values behind the products
+  // with this tile's, its page numbers a tile before and its scales before its keys: loads are in flight all the
+  // time, in one tile's registers, and what is waited for is always older than they are (no load is in a branch, or the
+  // compiler would count on none and wait for all; the last tile is a copy without loads).  Lane (c, g) holds scores and values of tokens
+  // t0 + 16 g .. + 16, and loads keys of tokens t0 + 16 (c / 4) + 4 i + c % 4, i < 4.
   constexpr int STEP = NW * TILE;
-  long t0 = t_begin + wave * TILE;
+  int t0 = (int)t_begin + wave * TILE;
   const int page_mask = (1 << a.c.page_shift) - 1;
   const int* table = a.pages + (long)r * a.max_pages;
   uint4 kw[4][DX], vw[DB];
   float ks, vs;
   int pv, pk;    // pages of the tokens whose scores and values the lane holds, and of those whose keys it loads
   bool there;    // pv is one
-  const auto find = [&](long t0) {
-    const long tv = t0 + 16 * g, tk = t0 + 16 * (c >> 2);
-    pv = tv < t_end ? table[tv >> a.c.page_shift] : -1;   // t_end <= len <= what the table holds
-    pk = tk < t_end ? table[tk >> a.c.page_shift] : -1;
+  const auto find = [&](int t) {   // behind the last token its page again (nothing of it is seen)
+    pv = table[min(t + 16 * g, t_end - 1) >> a.c.page_shift];
+    pk = table[min(t + 16 * (c >> 2), t_end - 1) >> a.c.page_shift];
   };
-  find(t0);
+  const auto held_page = [&](int page) { return page >= 0 && page < a.c.n_pages; };
+  const auto block_of = [&](int page) { return (long)(held_page(page) ? page : 0) * a.c.kv_heads + kvh; };
+  const auto load_k = [&](int t, int page) {
+    const int tk = t + 16 * (c >> 2);
+    const uint8_t* kp = a.c.k + ((block_of(page) << a.c.page_shift) + (tk & page_mask) + (c & 3)) * D + 16 * g;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int x = 0; x < DX; ++x) kw[i][x] = *reinterpret_cast<const uint4*>(kp + 4 * i * D + 64 * x);
+  };
+  const auto load_v = [&](int t, int page) {
+    const int tv = t + 16 * g;
+    const uint8_t* vp = a.c.v + ((block_of(page) * D + c) << a.c.page_shift) + (tv & page_mask);
+#pragma unroll
+    for (int i = 0; i < DB; ++i) vw[i] = *reinterpret_cast<const uint4*>(vp + ((long)16 * i << a.c.page_shift));
+  };
+  const auto load_scales = [&](int page) {
+    const long block = block_of(page);
+    ks = a.c.k_scale[block];
+    vs = a.c.v_scale[block];
+  };
+  if (t0 < t_end) find(t0);
   Tx8 qv[2 * DX];
   {
     const T* q = static_cast<const T*>(a.q) + (s.row0 + qi) * a.qs.row + h * a.qs.head + 16 * g;
@@ -216,42 +239,17 @@ __global__ __launch_bounds__(64 * NW) void kv8_attention_kernel(Kv8AttnArgs a) {
   for (int i = 0; i < DB; ++i) o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   float m = -INFINITY, mv = -INFINITY, l = 0.0f;
 
-  // The next tile's keys are fetched as soon as a tile's scores have taken theirs, its values behind the products
-  // with this tile's, its page numbers a tile before: loads are in flight all the time, in one tile's registers.
-  // Lane (c, g) holds scores and values of tokens t0 + 16 g .. + 16, and loads keys of tokens
-  // t0 + 16 (c / 4) + 4 i + c % 4, i < 4.
-  const auto load_k = [&](long t0) {
-    const int tk = (int)t0 + 16 * (c >> 2);
-    const long block = (long)(pk >= 0 && pk < a.c.n_pages ? pk : 0) * a.c.kv_heads + kvh;
-    const uint8_t* kp = a.c.k + ((block << a.c.page_shift) + (tk & page_mask) + (c & 3)) * D + 16 * g;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int x = 0; x < DX; ++x) kw[i][x] = *reinterpret_cast<const uint4*>(kp + 4 * i * D + 64 * x);
-  };
-  const auto load_v = [&](long t0, int page) {
-    const int tv = (int)t0 + 16 * g;
-    const long block = (long)(page >= 0 && page < a.c.n_pages ? page : 0) * a.c.kv_heads + kvh;
-    const uint8_t* vp = a.c.v + (((block * D) + c) << a.c.page_shift) + (tv & page_mask);
-#pragma unroll
-    for (int i = 0; i < DB; ++i) vw[i] = *reinterpret_cast<const uint4*>(vp + ((long)16 * i << a.c.page_shift));
-  };
-  const auto load_scales = [&](float* k, float* v) {
-    const long block = (long)(pv >= 0 && pv < a.c.n_pages ? pv : 0) * a.c.kv_heads + kvh;
-    *k = a.c.k_scale[block];
-    *v = a.c.v_scale[block];
-  };
-
   if (t0 < t_end) {
-    load_k(t0);
-    load_scales(&ks, &vs);
-    load_v(t0, pv);
-    there = pv >= 0 && pv < a.c.n_pages;
+    const int pv0 = pv, pk0 = pk;
+    there = held_page(pv0);
     find(t0 + STEP);
+    load_scales(pv0);
+    load_k(t0, pk0);
+    load_v(t0, pv0);
   }
-  for (; t0 < t_end; t0 += STEP) {
-    const int tv = (int)t0 + 16 * g;
-    const bool more = t0 + STEP < t_end;
+  const auto tile = [&](auto last) {
+    constexpr bool MORE = !decltype(last)::value;
+    const int tv = t0 + 16 * g;
     // scores of tokens tv + 4 i + e of this lane's query
     f32x4 sc[4];
 #pragma unroll
@@ -269,12 +267,12 @@ __global__ __launch_bounds__(64 * NW) void kv8_attention_kernel(Kv8AttnArgs a) {
     const float f = vs > 0.0f ? (float)((int)(__float_as_uint(vs) >> 23) - 127) : -INFINITY;
     const int left = there ? sees - tv : 0;       // of the lane's 16 tokens, those its query sees
     const int held = there ? s.len - tv : 0;      // places behind the last token may hold anything
-    const int page_next = pv;
-    there = pv >= 0 && pv < a.c.n_pages;
-    if (more) {
-      load_k(t0 + STEP);
-      load_scales(&ks, &vs);
+    const int pv1 = pv, pk1 = pk;
+    if constexpr (MORE) {
+      there = held_page(pv1);
       find(t0 + 2 * STEP);
+      load_scales(pv1);
+      load_k(t0 + STEP, pk1);
     }
     // in log2 units
     float x[16];
@@ -306,17 +304,21 @@ __global__ __launch_bounds__(64 * NW) void kv8_attention_kernel(Kv8AttnArgs a) {
       l += e;
       p[i >> 3][i & 7] = (f16)(e * weight);
     }
-    const bool ragged = __any(held < 16);
+    if (__any(held < 16)) {
+#pragma unroll
+      for (int i = 0; i < DB; ++i) vw[i] = first_bytes(vw[i], held);
+    }
 #pragma unroll
     for (int i = 0; i < DB; ++i) {
-      if (ragged) vw[i] = first_bytes(vw[i], held);
       f16x8 v0, v1;
       codes_to_f16<FORMAT>(vw[i], &v0, &v1);
       o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[0], o[i], 0, 0, 0);
       o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[1], o[i], 0, 0, 0);
     }
-    if (more) load_v(t0 + STEP, page_next);
-  }
+    if constexpr (MORE) load_v(t0 + STEP, pv1);
+  };
+  for (; t0 + STEP < t_end; t0 += STEP) tile(std::false_type{});
+  if (t0 < t_end) tile(std::true_type{});
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
 
@@ -426,7 +428,7 @@ extern "C" eas_status eas_kv8_attention_workspace(const eas_attn_shape* shape, i
   const eas_status st = check_shape(shape);
   if (st != EAS_OK) return st;
   if (max_q < 0 || max_len < 0 || n_seqs < 0 || !bytes) return EAS_ERR_INVALID_ARG;
-  *bytes = most_runs(max_len) == 1 ? 0 : (int64_t)n_seqs * shape->heads * slots(max_q, max_len) * (shape->head_dim + 1) * 4;
+  *bytes = n_runs(max_len, 1) == 1 ? 0 : (int64_t)n_seqs * shape->heads * slots(max_q, max_len) * (shape->head_dim + 1) * 4;
   return EAS_OK;
 }
 
@@ -460,7 +462,7 @@ extern "C" eas_status eas_kv8_attention(const eas_kv8_cache* cache, const eas_at
   if (!cu_q) a.max_q = max_q;   // a sequence's rows start at multiples of it
   const int64_t held = (int64_t)max_pages * cache->page_tokens;
   a.max_len = max_len < held ? max_len : (int)held;
-  a.runs = most_runs(a.max_len);
+  a.runs = n_runs(a.max_len, 1);
   const bool join = a.runs > 1;
   a.slots = (int)slots(a.max_q, a.max_len);
   if (join) {

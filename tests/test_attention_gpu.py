@@ -293,7 +293,7 @@ def test_binding_refusals():
                 lambda: cache.rows(pages, two, 4), lambda: cache.attention(q, one, pages),
                 lambda: cache.attention(q[:9], two, pages), lambda: cache.attention(q[:, :3], two, pages),
                 lambda: cache.attention(q, two, pages[0]),
-                lambda: cache.attention(q, two, torch.zeros(2, 40, **i32),
+                lambda: cache.attention(q, two, torch.zeros(2, 400, **i32),
                                         workspace=torch.zeros(16, dtype=torch.uint8, device="cuda"))):
         with pytest.raises((ValueError, RuntimeError)):
             bad()
@@ -501,7 +501,7 @@ def check_decode(both, q, lens, table, new, scale, causal, out, lse):
 @pytest.mark.parametrize("page,heads,kv_heads,dim", [(16, 4, 4, 64), (64, 14, 2, 128), (32, 20, 1, 64), (128, 8, 1, 128)])
 def test_decode(form, dtype, page, heads, kv_heads, dim):
     torch, _ = lib()
-    lens = [1, 15, 16, 17, 64, 65, 255, 256, 257, 700, 1100]
+    lens = [1, 15, 16, 17, 64, 65, 255, 256, 257, 700, 1024, 1025, 2300]
     print("[kv8] decode %s %s page %d" % (form, dtype, page), flush=True)
     both, table = filled(form, lens, page, kv_heads, dim, 100)
     q = make(torch, (len(lens), heads, dim), getattr(torch, dtype), 5)
@@ -515,7 +515,7 @@ def test_decode(form, dtype, page, heads, kv_heads, dim):
 def test_decode_several_queries(dtype, heads, kv_heads, dim, form, causal):
     """Ragged numbers of queries, none and more than the tokens among them, lengths past a split."""
     torch, _ = lib()
-    new, lens = [3, 0, 17, 5, 1, 40, 9], [300, 20, 17, 3, 0, 600, 1025]
+    new, lens = [3, 0, 17, 5, 1, 40, 9], [1300, 20, 17, 3, 0, 2600, 1025]
     both, table = filled(form, lens, 16, kv_heads, dim, 110)
     c = cu(new)
     q = make(torch, (c[-1] + 2, heads, dim), getattr(torch, dtype), 6)
