@@ -109,7 +109,8 @@ typedef struct {
 } eas_kv8_cache;
 
 /* The page table of the calls below: device int32 [n_seqs, max_pages]; token t
- * of sequence r lies in page pages[r, t / page_tokens].  An entry outside
+ * of sequence r lies in page pages[r, t / page_tokens]; max_pages * page_tokens
+ * is at most 2^30.  An entry outside
  * [0, n_pages) is a page that is not held: tokens appended to it are dropped,
  * its rows read as zeros, and attention does not see its tokens.  Pages may be
  * shared between sequences for reading.  A page that gets tokens in a call is

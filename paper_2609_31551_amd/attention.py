@@ -108,7 +108,7 @@ def _outputs(q, out, lse, with_lse, index, stream):
         out = _on(stream, lambda: torch.empty_like(q))
     elif out.shape[0] != rows:
         raise ValueError("out has %d rows, q %d" % (out.shape[0], rows))
-    strides = _rows(out, "out", heads, dim, q.dtype, index)
+    strides = _rows(out, "out", heads, dim, q.dtype, index)   # a new one's, too: empty_like keeps q's order
     if lse is None:
         if not with_lse:
             return out, None, strides, None
@@ -185,11 +185,13 @@ class Kv8Cache:
         if k.dim() != 4 or k.dtype not in _FORMAT:
             raise ValueError("k must be int8 or float8_e4m3fn codes [pages, kv_heads, page_tokens, head_dim]")
         (n, h, p, d), codes, index = k.shape, k.dtype, k.get_device()
-        for t, name, shape, dtype in ((k, "k", (n, h, p, d), codes), (v, "v", (n, h, d, p), codes),
-                                      (k_scale, "k_scale", (n, h), torch.float32),
-                                      (v_scale, "v_scale", (n, h), torch.float32)):
-            if t.shape != shape or t.dtype != dtype or t.get_device() != index or not t.is_contiguous():
-                raise ValueError("%s must be a contiguous %s tensor of shape %s on %s" % (name, dtype, shape, k.device))
+        if not (v.shape == (n, h, d, p) and v.dtype == codes and k_scale.shape == v_scale.shape == (n, h)
+                and k_scale.dtype == v_scale.dtype == torch.float32
+                and v.get_device() == k_scale.get_device() == v_scale.get_device() == index
+                and k.is_contiguous() and v.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous()):
+            raise ValueError("wanted contiguous v %s, %s, and k_scale, v_scale %s, float32, on %s: got %s" % (
+                (n, h, d, p), codes, (n, h), k.device,
+                ", ".join("%s %s on %s" % (tuple(t.shape), t.dtype, t.device) for t in (k, v, k_scale, v_scale))))
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.n_pages, self.kv_heads, self.page_tokens, self.head_dim = n, h, p, d
         self.device, self._index = k.device, index

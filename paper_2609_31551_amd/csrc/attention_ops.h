@@ -65,10 +65,10 @@ inline eas_status check_cache(const eas_kv8_cache* c) {
   return EAS_OK;
 }
 
-// The page table and the sizes that every cache call takes.  max_pages * page_tokens stays below 2^31.
+// The page table and the sizes that every cache call takes: at most 2^30 tokens of a sequence.
 inline eas_status check_table(const eas_kv8_cache* c, const int32_t* pages, int32_t max_pages, int32_t n_seqs) {
   if ((!pages && n_seqs > 0) || max_pages <= 0 || n_seqs < 0 || (uintptr_t)pages % 4) return EAS_ERR_INVALID_ARG;
-  return (int64_t)max_pages * c->page_tokens > 0x7fffffff ? EAS_ERR_UNSUPPORTED : EAS_OK;
+  return (int64_t)max_pages * c->page_tokens > (1 << 30) ? EAS_ERR_UNSUPPORTED : EAS_OK;
 }
 
 // ---- the cache's scales and codes (device) -----------------------------------

@@ -39,14 +39,14 @@ constexpr int RUN_ROWS = 256;    // runs * queries of a sequence that is split
 // short ones (one of 4,096: 11.3 and 13.8 us).
 constexpr int SHORTEST_RUN = 1024;
 __host__ __device__ inline int n_runs(int len, int nq) {
-  const int by_len = (int)(((int64_t)len + SHORTEST_RUN - 1) / SHORTEST_RUN);
+  const int by_len = (int)(((unsigned)len + SHORTEST_RUN - 1) / SHORTEST_RUN);   // len <= 2^30: 32 bits hold all sums here
   int most = nq > 0 ? RUN_ROWS / nq : 1;
   most = most < 1 ? 1 : most > MAX_RUNS ? MAX_RUNS : most;
   return by_len < 1 ? 1 : by_len < most ? by_len : most;
 }
 __host__ __device__ inline int run_tokens(int len, int runs) {
-  constexpr int step = NW * TILE;
-  return (int)(((int64_t)len + (int64_t)runs * step - 1) / ((int64_t)runs * step)) * step;
+  const unsigned all = (unsigned)runs * (NW * TILE);
+  return (int)(((unsigned)len + all - 1) / all) * (NW * TILE);
 }
 // Workspace slots per sequence and head: at least n_runs * nq for every nq <= max_q, len <= max_len
 // of a sequence that is split
@@ -140,12 +140,12 @@ __global__ __launch_bounds__(64 * NW) void kv8_attention_kernel(Kv8AttnArgs a) {
   __shared__ float o_part[NW][16][D];
   __shared__ float m_part[NW][16], mv_part[NW][16], l_part[NW][16];
 
-  int b = blockIdx.x;
-  const int run = b % a.runs;
-  b /= a.runs;
-  const int rt = b % a.row_tiles;
-  b /= a.row_tiles;
-  const int kvh = b % a.c.kv_heads, r = b / a.c.kv_heads;
+  unsigned b = blockIdx.x;
+  const int run = b % (unsigned)a.runs;
+  b /= (unsigned)a.runs;
+  const int rt = b % (unsigned)a.row_tiles;
+  b /= (unsigned)a.row_tiles;
+  const int kvh = b % (unsigned)a.c.kv_heads, r = b / (unsigned)a.c.kv_heads;
   const Seq s = find_seq(a, r);
   const int group = a.heads / a.c.kv_heads;
   if ((long)rt * 16 >= (long)s.nq * group) return;
@@ -158,7 +158,7 @@ __global__ __launch_bounds__(64 * NW) void kv8_attention_kernel(Kv8AttnArgs a) {
   // this lane's query, and how many tokens it sees
   const int rho = rt * 16 + c;
   const bool real = rho < s.nq * group;
-  const int qi = real ? rho / group : 0, h = kvh * group + (real ? rho % group : 0);
+  const int qi = real ? (unsigned)rho / (unsigned)group : 0, h = kvh * group + (real ? rho - qi * group : 0);
   const int sees = !real ? 0 : a.causal ? max(0, min(s.len, s.len - s.nq + qi + 1)) : s.len;
   // the tile's last query sees most
   const int last = min(rt * 16 + 15, s.nq * group - 1) / group;
@@ -348,7 +348,7 @@ __global__ __launch_bounds__(64 * NW) void kv8_attention_kernel(Kv8AttnArgs a) {
     }
     const float inv = L == 0.0f ? 0.0f : 1.0f / L;
     const float lse2 = L == 0.0f ? -INFINITY : M0 + __log2f(L);
-    const int q = rr / group, head = kvh * group + rr % group;
+    const int q = (unsigned)rr / (unsigned)group, head = kvh * group + rr - q * group;
     if (runs == 1) {
       const long orow = s.row0 + q;
       typedef T Tx4 __attribute__((ext_vector_type(4)));

@@ -152,7 +152,7 @@ def test_cache_calls_refuse_caches(over, status):
 
 
 TABLE_REFUSALS = [(dict(pages=None), BAD), (dict(max_pages=0), BAD), (dict(n=-1), BAD), (dict(pages=PTR + 1), BAD),
-                  (dict(max_pages=1 << 25), UNSUPPORTED)]
+                  (dict(max_pages=(1 << 24) + 1), UNSUPPORTED)]
 
 
 @pytest.mark.parametrize("call", [append, rows, attend])
