@@ -1,13 +1,20 @@
 // Attention over packed prompts, causal or full, with grouped heads
 // (include/eas_attention.h).
 //
-// One pass over the keys with the running maximum and sum of the softmax.  A
-// workgroup of 4 waves owns 128 queries of one (sequence, head), each wave 32 of
-// them; keys and values stream through LDS in tiles of 64, anchored at the sequence's
+// One pass over the keys with the running maximum and sum of the softmax.  A workgroup owns 128 or 256 queries of one
+// (sequence, head), a wave 32 of them; keys and values stream through LDS in tiles of 64, anchored at the sequence's
 // first key, so a query's result does not depend on where its sequence lies.
-//   S^T = K Q^T (v_mfma_f32_32x32x16: keys are rows, so a lane holds 16 scores of one
-//   query), softmax in fp32 on exp2, O^T += V^T P^T with P rounded to the element type.
-// Bound by the matrix units: 4 * head_dim flops for each visible (query, key) pair.
+//   S^T = K Q^T (v_mfma_f32_32x32x16: keys are rows, so a lane holds 16 scores of one query), softmax in fp32 on exp2,
+//   O^T += V^T P^T with P rounded to the element type: by 2^-8 (bf16) or 2^-11 (fp16) of each weight at most, as the
+//   result itself.
+// The tiles come by DMA, two of each kind in LDS, while the tile before is worked on; a wave's softmax stands between
+// the MFMAs of the next tile's scores and of its own values, step by step.
+//
+// Bound by the matrix units: 4 * head_dim flops for each visible (query, key) pair.  16,484 causal tokens of 32 heads
+// of 128 take 1,912 us, 1,164 TFLOP/s; 8,192 with all keys 926 us, 1,187 (a matrix product of 8,192^3 from the library
+// reaches 1,175 here: the board's power, not the instruction's rate, is the limit; with the MFMAs and the DMA alone the
+// full 8,192 take 692 us).  Short prompts are bound by the queries' loads and the results' stores, 15 - 20% of eight
+// prompts of 97 to 2,309 tokens, which nothing of the same workgroup runs beside.
 #include <type_traits>
 
 #include "attention_ops.h"
@@ -21,9 +28,9 @@ constexpr int MAX_RUNS = 16;         // runs that a sequence's keys are split in
 
 // Runs of keys that each query tile of a sequence is split into, a workgroup each: of 4,096 keys at least, where the
 // sequence alone leaves CUs without a workgroup.  A call waits for its longest walk: 128 queries over 32,896 keys of 32
-// heads 86 us, in one walk 471; 512 over 8,704 91 and 134; chunks of 700 - 1,024 queries over 1,535 - 9,916 keys of 16
-// heads 104 and 126.  A batch that fills the chip anyway pays for the runs' sums: eight chunks of 512 over 9,512 keys
-// 620 and 551.  By a sequence's own sizes only: the join rounds otherwise, and a result must not depend on the batch.
+// heads 90 us, in one walk 472; 512 over 8,704 93 and 138; chunks of 700 - 1,024 queries over 1,535 - 9,916 keys of 16
+// heads 105 and 124.  A batch that fills the chip anyway pays for the runs' sums: eight chunks of 512 over 9,512 keys
+// 631 and 570.  By a sequence's own sizes only: the join rounds otherwise, and a result must not depend on the batch.
 __host__ __device__ inline int n_runs(int lq, int lk, int heads) {
   if ((int64_t)((lq + 127) / 128) * heads > 256) return 1;
   const int runs = lk / 4096;
@@ -277,6 +284,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
     return u.v;
   };
   const f32x16 zero = {};
+  constexpr float TOP = std::is_same_v<T, f16> ? 15.0f : 0.0f;
   // The scores of tile t, keys 32 .. in s[1].
   const auto scores = [&](int t, f32x16* s) {
 #pragma unroll
@@ -284,9 +292,10 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
       s[i & 1] = Mfma<T>::go(read_k(t, i), qf[i >> 1], i < 2 ? zero : s[i & 1]);
   };
   // Tile t: the online softmax of its scores s and O^T += V^T P^T, and beside them the next tile's scores n.  One
-  // FMA turns a score into x = s c - m, in log2 units over the maximum m.  m is raised lazily, when some x exceeds
-  // 8, so p = 2^x <= 256 and O is rarely scaled; O and l share m, so O / l is the same.  The first tile always
-  // sets it.  The matrix unit takes 32 cycles an MFMA, in which the wave issues some 8 other instructions: the
+  // FMA turns a score into x = s c - m, in log2 units over m, the maximum less TOP - 8.  m is raised lazily, when some x
+  // exceeds TOP, so p = 2^x <= 2^TOP and O is rarely scaled; O and l share m, so O / l is the same.  The first tile
+  // always sets it.  TOP keeps bf16's sums from overflow where a softmax's do not, and fp16's small weights from
+  // vanishing: what is lost below 2^-24 is 2^-32 of the largest weight.  The matrix unit takes 32 cycles an MFMA, in which the wave issues some 8 other instructions: the
   // softmax's are dealt out behind the MFMAs by hand, in steps that nothing is moved across, each with the operands
   // of the MFMA four steps on.  (Left to the compiler they come in blocks, and both waves of a SIMD wait for the
   // same unit: matrix units 53% busy.)
@@ -319,9 +328,9 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
       const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
       mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
     }
-    const bool need = t == 0 ? mx > -INFINITY : mx > 8.0f;   // a query that sees nothing keeps m = 0, l = 0
+    const bool need = t == 0 ? mx > -INFINITY : mx > TOP;   // a query that sees nothing keeps m = 0, l = 0
     if (__any(need)) {
-      const float d = need ? mx : 0.0f;
+      const float d = need ? mx - (TOP - 8.0f) : 0.0f;
       const float alpha = t == 0 ? 0.0f : __builtin_amdgcn_exp2f(-d);
       m += d;
       l *= alpha;
@@ -516,10 +525,10 @@ int64_t key_tiles(int64_t lq, int64_t lk, int64_t t, int qt, int causal) {
 }
 
 // Queries per workgroup.  256 share each key and value tile among twice the queries, which halves the DMA per score:
-// 3-6% faster where both fill the chip (16,484 causal tokens of 32 heads 2,049 us against 2,129; 8,192 full 984
-// against 1,055).  128 leave less of a workgroup idle behind a sequence's end and at the diagonal, spread few
-// queries over more CUs, and put two workgroups on a CU, one's loads and stores beside the other's products: eight
-// image prompts of 97 to 2,309 tokens 130 us against 140, 64 prompts of 256 125 against 138.  So 256 where they
+// 2-5% faster where both fill the chip (16,484 causal tokens of 32 heads 1,917 us against 1,966; 8,192 full 927
+// against 975).  128 leave less of a workgroup idle behind a sequence's end and at the diagonal, spread few queries
+// over more CUs, and put two workgroups on a CU, one's loads and stores beside the other's products: eight image
+// prompts of 97 to 2,309 tokens 119 us against 125, 64 prompts of 256 106 against 123.  So 256 where they
 // take at most 8% more key tiles per query, walk 16 at least, and two workgroups a CU remain.  A query's arithmetic
 // is the same in both.
 int query_tile(const PromptWork& w, int heads, int causal) {

@@ -5,8 +5,8 @@ Tolerances.  With u the element type's half step (bf16 2^-8, fp16 2^-11 relative
 good to delta (fp32 sums of head_dim exact products: head_dim * 2^-24 * scale * |q| max |k| by Cauchy-Schwarz), the
 result is off by at most u |out| for its own rounding, u A for that of the weights, 2 delta A and the hardware
 exponential's 2^-21 A.  Weights are rounded to fp16 over the cache whatever the element type, and in fp16 a weight
-below 2^-14 is rounded by up to 2^-25 of the largest one instead: 2^-25 sum |v| (over the cache: of the largest
-weight times 127 or 448 steps of its block)."""
+below 2^-14 is rounded by up to 2^-25 instead.  The largest weight is 2^7 at least: 2^-32 sum |v|; over the cache it
+is 2^15: 2^-40 of it times 127 or 448 steps of its block, for each token."""
 import numpy as np
 import pytest
 
@@ -83,7 +83,7 @@ def run_prompt(q, k, v, cu_q, cu_k, causal, scale=None, check_bounds=True):
         u = HALF[str(q.dtype)[6:]]
         size, delta, total, count = prompt_bounds(Q, K, V, cu_q, cu_k, s, causal, u)
         check(f64(out)[:n], f64(lse)[:n], ref, ref_lse, size, delta, total, count, u,
-              2.0 ** -25 if q.dtype == torch.float16 else 0.0)
+              2.0 ** -32 if q.dtype == torch.float16 else 0.0)
     return out, lse
 
 
@@ -261,6 +261,30 @@ def test_prompt_attention_keys_behind_four_gib():
     got, _ = A.prompt_attention(q, k, v, [0, 130], [0, 700])
     want, _ = A.prompt_attention(q, k.contiguous(), v.contiguous(), [0, 130], [0, 700])
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_small_weights_count(dtype, dim, causal):
+    """4,095 keys of 2^-25.3 of the first key's weight each, whose value is 0: the result is made of them alone."""
+    torch, _ = lib()
+    n, dt = 4096, getattr(torch, dtype)
+    k, v = torch.zeros(n, 1, dim, dtype=dt, device="cuda"), torch.ones(n, 1, dim, dtype=dt, device="cuda")
+    k[0], v[0] = 16.0, 0.0
+    q = torch.zeros(40, 1, dim, dtype=dt, device="cuda")
+    q[:, :, 0] = 1.0
+    run_prompt(q, k, v, [0, 40], [0, n], causal, scale=float(np.float32(25.3 * np.log(2.0) / 16)))
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_large_values_do_not_overflow(causal):
+    """Values up to 2^122: sums of 70 of them with weights of 1 at most are finite."""
+    torch, _ = lib()
+    q, k = make(torch, (70, 2, 64), torch.bfloat16, 60), make(torch, (70, 2, 64), torch.bfloat16, 61)
+    v = torch.full((70, 2, 64), 2.0 ** 120, dtype=torch.bfloat16, device="cuda")
+    v[:, :, ::2] *= -4.0
+    run_prompt(q, k, v, [0, 70], None, causal)
 
 
 def test_binding_refusals():
@@ -484,7 +508,7 @@ def check_decode(both, q, lens, table, new, scale, causal, out, lse):
         # weights are rounded to fp16 (2^-11) whatever the element type
         tol_u = 2.0 ** -11
         got = f64(out)[a]
-        tol = u * np.abs(ref) + tol_u * size + (2 * delta[..., None] + 2.0 ** -21) * size + 2.0 ** -25 * total + 2.0 ** -25
+        tol = u * np.abs(ref) + tol_u * size + (2 * delta[..., None] + 2.0 ** -21) * size + 2.0 ** -40 * total + 2.0 ** -25
         bad = ~(np.abs(got - ref) <= tol)
         assert not bad.any(), "sequence %d: %d of %d off, worst %.3g of its tolerance" % (
             r, bad.sum(), bad.size, np.nanmax(np.abs(got - ref) / tol))
@@ -524,6 +548,22 @@ def test_decode_several_queries(dtype, heads, kv_heads, dim, form, causal):
                                   scale=0.2, out=out, with_lse=True)
     assert (out[c[-1]:] == 9.0).all()
     check_decode(both, q, lens, table, new, 0.2, causal, out, lse)
+
+
+@pytest.mark.parametrize("form", FORMATS)
+def test_decode_small_weights_count(form):
+    """As above, over the cache: 1,023 tokens of 2^-25.3 of the first's weight each, in the first's runs of tiles."""
+    torch, A = lib()
+    both = Both(form, 64, 1, 16, 128)
+    k, v = torch.zeros(1024, 1, 128, device="cuda").bfloat16(), torch.ones(1024, 1, 128, device="cuda").bfloat16()
+    k[0], v[0] = 16.0, 0.0
+    table = np.arange(64)[None]
+    both.append(k, v, [0, 1024], [0], table)
+    q = torch.zeros(1, 2, 128, device="cuda").bfloat16()
+    q[:, 0, 0] = 1.0                       # the other head's scores are all 0
+    scale = float(np.float32(25.3 * np.log(2.0) / 16))
+    out, lse = both.gpu.attention(q, i32(torch, [1024]), i32(torch, table), scale=scale, with_lse=True)
+    check_decode(both, q, [1024], table, [1], scale, True, out, lse)
 
 
 def test_decode_over_absent_pages():
