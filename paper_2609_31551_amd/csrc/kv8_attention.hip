@@ -23,7 +23,7 @@
 // and a second kernel joins them in order.
 //
 // Bound by HBM, a byte of codes for each 2 (queries * group) multiply-adds: 16 sequences of 32,768 tokens, 8 heads of
-// 128, 1,068 MB in 201 us, 5.3 TB/s.  32 sequences of 1 - 4,096 tokens, 71 MB, take 23 us: 14 of bytes, a wave's first
+// 128, 1,068 MB in 201 us, 5.3 TB/s.  32 sequences of 1 - 8,192 tokens, 4 heads, 71 MB, take 23 us: 14 of bytes, a wave's first
 // loads one after the other (lengths, pages, scales, codes) and the join, 4 us.
 #include <type_traits>
 
@@ -136,45 +136,58 @@ __device__ __forceinline__ float column_max(float v) {
   return fmaxf(v, __shfl_xor(v, 32, 64));
 }
 
-template <class T, int FORMAT, int D>
+// C: tiles of 16 rows that a workgroup takes.  Two share what is loaded and turned to fp16, but a wave walks for
+// both: see columns().
+template <class T, int FORMAT, int D, int C>
 __global__ __launch_bounds__(64 * NW) void kv8_attention_kernel(Kv8AttnArgs a) {
   typedef T Tx8 __attribute__((ext_vector_type(8)));
   constexpr int DX = D / 64;   // 64-dimension parts of a key
   constexpr int DB = D / 16;   // 16-dimension blocks of the output
-  __shared__ float o_part[NW][16][D];
-  __shared__ float m_part[NW][16], mv_part[NW][16], l_part[NW][16];
+  constexpr int ROWS = 16 * C;
+  __shared__ float o_part[NW][ROWS][D];
+  __shared__ float m_part[NW][ROWS], mv_part[NW][ROWS], l_part[NW][ROWS];
 
-  unsigned b = blockIdx.x;
+  // Workgroups go to the 8 XCDs in turn.  The row tiles of one run, which read the same codes, are 8 apart, on one
+  // XCD: 32 sequences of 2,048 tokens, 3 queries of 28 heads over 4, 27.2 us, dealt out in turn 32.5; 8 of 4,096, 16
+  // queries of 32 heads over 8, 47.6 and 54.3; short ragged ones pay for the uneven load: 8 of 333 - 9,000, 5 of 16
+  // over 4, 15.4 and 14.2.
+  unsigned b = blockIdx.x / 8;
+  const int rt = b % (unsigned)a.row_tiles;
+  b = b / (unsigned)a.row_tiles * 8 + blockIdx.x % 8;
   const int run = b % (unsigned)a.runs;
   b /= (unsigned)a.runs;
-  const int rt = b % (unsigned)a.row_tiles;
-  b /= (unsigned)a.row_tiles;
-  const int kvh = b % (unsigned)a.c.kv_heads, r = b / (unsigned)a.c.kv_heads;
+  const int kvh = b % (unsigned)a.c.kv_heads, rb = b / (unsigned)a.c.kv_heads, r = min(rb, a.n_seqs - 1);
   const Seq s = find_seq(a, r);
   const int group = a.heads / a.c.kv_heads;
-  if ((long)rt * 16 >= (long)s.nq * group) return;
+  if (rb != r || (long)rt * ROWS >= (long)s.nq * group) return;
   const int runs = n_runs(s.len, s.nq);
   if (run >= runs) return;
   const int each = run_tokens(s.len, runs);
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  // this lane's query, and how many tokens it sees
-  const int rho = rt * 16 + c;
-  const bool real = rho < s.nq * group;
-  const int qi = real ? (unsigned)rho / (unsigned)group : 0, h = kvh * group + (real ? rho - qi * group : 0);
-  const int sees = !real ? 0 : a.causal ? max(0, min(s.len, s.len - s.nq + qi + 1)) : s.len;
-  // the tile's last query sees most
-  const int last = min(rt * 16 + 15, s.nq * group - 1) / group;
+  // this lane's queries, and how many tokens they see
+  int sees[C];
+  const T* q[C];
+#pragma unroll
+  for (int j = 0; j < C; ++j) {
+    const int rho = rt * ROWS + 16 * j + c;
+    const bool real = rho < s.nq * group;
+    const int qi = real ? (unsigned)rho / (unsigned)group : 0, h = kvh * group + (real ? rho - qi * group : 0);
+    sees[j] = !real ? 0 : a.causal ? max(0, min(s.len, s.len - s.nq + qi + 1)) : s.len;
+    q[j] = static_cast<const T*>(a.q) + (s.row0 + qi) * a.qs.row + h * a.qs.head + 16 * g;
+  }
+  // the last query sees most
+  const int last = min(rt * ROWS + ROWS - 1, s.nq * group - 1) / group;
   const int most = a.causal ? max(0, min(s.len, s.len - s.nq + last + 1)) : s.len;
   const long t_begin = (long)run * each;
   const int t_end = (int)min((long)most, t_begin + each);
 
-  // The next tile's keys are fetched as soon as a tile's scores have taken theirs, its values behind the products
-  // with this tile's, its page numbers a tile before and its scales before its keys: loads are in flight all the
-  // time, in one tile's registers, and what is waited for is always older than they are (no load is in a branch, or the
-  // compiler would count on none and wait for all; the last tile is a copy without loads).  Lane (c, g) holds scores and values of tokens
-  // t0 + 16 g .. + 16, and loads keys of tokens t0 + 16 (c / 4) + 4 i + c % 4, i < 4.
+  // The next tile's keys are fetched as soon as a tile's scores have taken theirs, its values behind the products with
+  // this tile's, its page numbers a tile before and its scales before its keys: loads are in flight all the time, in one
+  // tile's registers, and what is waited for is always older than they are (no load is in a branch, or the compiler
+  // would count on none and wait for all; the last tile is a copy without loads).  Lane (c, g) holds scores and values
+  // of tokens t0 + 16 g .. + 16, and loads keys of tokens t0 + 16 (c / 4) + 4 i + c % 4, i < 4.
   constexpr int STEP = NW * TILE;
   int t0 = (int)t_begin + wave * TILE;
   const int page_mask = (1 << a.c.page_shift) - 1;
@@ -209,39 +222,43 @@ __global__ __launch_bounds__(64 * NW) void kv8_attention_kernel(Kv8AttnArgs a) {
     vs = a.c.v_scale[block];
   };
   if (t0 < t_end) find(t0);
-  Tx8 qv[2 * DX];
-  {
-    const T* q = static_cast<const T*>(a.q) + (s.row0 + qi) * a.qs.row + h * a.qs.head + 16 * g;
+  Tx8 qv[C][2 * DX];
+#pragma unroll
+  for (int j = 0; j < C; ++j)
 #pragma unroll
     for (int x = 0; x < DX; ++x)
 #pragma unroll
-      for (int y = 0; y < 2; ++y) qv[2 * x + y] = *reinterpret_cast<const Tx8*>(q + 64 * x + 8 * y);
-  }
+      for (int y = 0; y < 2; ++y) qv[j][2 * x + y] = *reinterpret_cast<const Tx8*>(q[j] + 64 * x + 8 * y);
 
   // queries times a power of two that brings the row's largest to [2^14, 2^15)
-  f16x8 qf[2 * DX];
-  float q_scale;
-  {
+  f16x8 qf[C][2 * DX];
+  float q_scale[C];
+#pragma unroll
+  for (int j = 0; j < C; ++j) {
     float top = 0.0f;
 #pragma unroll
     for (int i = 0; i < 2 * DX; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)qv[i][e]));
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)qv[j][i][e]));
     top = column_max(top);
     // 2^(14 - floor(log2 top)), kept in the normal range
     const int e = min(max((int)(__float_as_uint(top) >> 23), 15), 254);
     const float up = __uint_as_float((uint32_t)min(268 - e, 254) << 23);
-    q_scale = a.scale_log2 * __uint_as_float((uint32_t)max(e - 14, 0) << 23);
+    q_scale[j] = a.scale_log2 * __uint_as_float((uint32_t)max(e - 14, 0) << 23);
 #pragma unroll
     for (int i = 0; i < 2 * DX; ++i)
 #pragma unroll
-      for (int e8 = 0; e8 < 8; ++e8) qf[i][e8] = (f16)((float)qv[i][e8] * up);
+      for (int e8 = 0; e8 < 8; ++e8) qf[j][i][e8] = (f16)((float)qv[j][i][e8] * up);
   }
 
-  f32x4 o[DB];
+  f32x4 o[C][DB];
+  float m[C], mv[C], l[C];
 #pragma unroll
-  for (int i = 0; i < DB; ++i) o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  float m = -INFINITY, mv = -INFINITY, l = 0.0f;
+  for (int j = 0; j < C; ++j) {
+#pragma unroll
+    for (int i = 0; i < DB; ++i) o[j][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    m[j] = mv[j] = -INFINITY, l[j] = 0.0f;
+  }
 
   if (t0 < t_end) {
     const int pv0 = pv, pk0 = pk;
@@ -254,23 +271,27 @@ __global__ __launch_bounds__(64 * NW) void kv8_attention_kernel(Kv8AttnArgs a) {
   const auto tile = [&](auto last) {
     constexpr bool MORE = !decltype(last)::value;
     const int tv = t0 + 16 * g;
-    // scores of tokens tv + 4 i + e of this lane's query
-    f32x4 sc[4];
+    // scores of tokens tv + 4 i + e of this lane's queries
+    f32x4 sc[C][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      sc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int j = 0; j < C; ++j) sc[j][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int d = 0; d < DX; ++d) {
         f16x8 k0, k1;
         codes_to_f16<FORMAT>(kw[i][d], &k0, &k1);
-        sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, qf[2 * d], sc[i], 0, 0, 0);
-        sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, qf[2 * d + 1], sc[i], 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+          sc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, qf[j][2 * d], sc[j][i], 0, 0, 0);
+          sc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, qf[j][2 * d + 1], sc[j][i], 0, 0, 0);
+        }
       }
     }
-    const float ck = q_scale * ks;
+    const float k_scale = ks;
     const float f = vs > 0.0f ? (float)((int)(__float_as_uint(vs) >> 23) - 127) : -INFINITY;
-    const int left = there ? sees - tv : 0;       // of the lane's 16 tokens, those its query sees
-    const int held = there ? s.len - tv : 0;      // places behind the last token may hold anything
+    const bool was = there;
+    const int held = was ? s.len - tv : 0;        // places behind the last token may hold anything
     const int pv1 = pv, pk1 = pk;
     if constexpr (MORE) {
       there = held_page(pv1);
@@ -278,35 +299,40 @@ __global__ __launch_bounds__(64 * NW) void kv8_attention_kernel(Kv8AttnArgs a) {
       load_scales(pv1);
       load_k(t0 + STEP, pk1);
     }
-    // in log2 units
-    float x[16];
+    f16x8 p[C][2];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = i < left ? sc[i >> 2][i & 3] * ck : -INFINITY;
-    float top = x[0];
+    for (int j = 0; j < C; ++j) {
+      const int left = was ? sees[j] - tv : 0;    // of the lane's 16 tokens, those its query sees
+      const float ck = q_scale[j] * k_scale;
+      // in log2 units
+      float x[16];
 #pragma unroll
-    for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
-    const float top_m = column_max(top), top_v = column_max(top + f) - 15.0f;
-    if (__any(top_m > m)) {
-      const float up = fmaxf(m, top_m);
-      l *= up == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - up);
-      m = up;
-    }
-    if (__any(top_v > mv)) {
-      const float up = fmaxf(mv, top_v);
-      const float alpha = up == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(mv - up);
-      mv = up;
+      for (int i = 0; i < 16; ++i) x[i] = i < left ? sc[j][i >> 2][i & 3] * ck : -INFINITY;
+      float top = x[0];
 #pragma unroll
-      for (int i = 0; i < DB; ++i) o[i] *= alpha;
-    }
-    // p = 2^(x - m); a code's weight is p 2^(m + f - m')
-    const float m0 = m == -INFINITY ? 0.0f : m, mv0 = mv == -INFINITY ? 0.0f : mv;
-    const float weight = f == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(fminf(m0 + f - mv0, 126.0f));
-    f16x8 p[2];
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
+      const float top_m = column_max(top), top_v = column_max(top + f) - 15.0f;
+      if (__any(top_m > m[j])) {
+        const float up = fmaxf(m[j], top_m);
+        l[j] *= up == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[j] - up);
+        m[j] = up;
+      }
+      if (__any(top_v > mv[j])) {
+        const float up = fmaxf(mv[j], top_v);
+        const float alpha = up == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(mv[j] - up);
+        mv[j] = up;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float e = __builtin_amdgcn_exp2f(x[i] - m0);
-      l += e;
-      p[i >> 3][i & 7] = (f16)(e * weight);
+        for (int i = 0; i < DB; ++i) o[j][i] *= alpha;
+      }
+      // p = 2^(x - m); a code's weight is p 2^(m + f - m')
+      const float m0 = m[j] == -INFINITY ? 0.0f : m[j], mv0 = mv[j] == -INFINITY ? 0.0f : mv[j];
+      const float weight = f == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(fminf(m0 + f - mv0, 126.0f));
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float e = __builtin_amdgcn_exp2f(x[i] - m0);
+        l[j] += e;
+        p[j][i >> 3][i & 7] = (f16)(e * weight);
+      }
     }
     if (__any(held < 16)) {
 #pragma unroll
@@ -316,27 +342,32 @@ __global__ __launch_bounds__(64 * NW) void kv8_attention_kernel(Kv8AttnArgs a) {
     for (int i = 0; i < DB; ++i) {
       f16x8 v0, v1;
       codes_to_f16<FORMAT>(vw[i], &v0, &v1);
-      o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[0], o[i], 0, 0, 0);
-      o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[1], o[i], 0, 0, 0);
+#pragma unroll
+      for (int j = 0; j < C; ++j) {
+        o[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[j][0], o[j][i], 0, 0, 0);
+        o[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[j][1], o[j][i], 0, 0, 0);
+      }
     }
     if constexpr (MORE) load_v(t0 + STEP, pv1);
   };
   for (; t0 + STEP < t_end; t0 += STEP) tile(std::false_type{});
   if (t0 < t_end) tile(std::true_type{});
-  l += __shfl_xor(l, 16, 64);
-  l += __shfl_xor(l, 32, 64);
-
-  // the four waves' sums: lane (c, g) holds dimensions 16 i + 4 g .. + 4 of query c
-  if (g == 0) {
-    m_part[wave][c] = m;
-    mv_part[wave][c] = mv;
-    l_part[wave][c] = l;
-  }
+  // the four waves' sums: lane (c, g) holds dimensions 16 i + 4 g .. + 4 of query c of each column tile
 #pragma unroll
-  for (int i = 0; i < DB; ++i) *reinterpret_cast<f32x4*>(&o_part[wave][c][16 * i + 4 * g]) = o[i];
+  for (int j = 0; j < C; ++j) {
+    l[j] += __shfl_xor(l[j], 16, 64);
+    l[j] += __shfl_xor(l[j], 32, 64);
+    if (g == 0) {
+      m_part[wave][16 * j + c] = m[j];
+      mv_part[wave][16 * j + c] = mv[j];
+      l_part[wave][16 * j + c] = l[j];
+    }
+#pragma unroll
+    for (int i = 0; i < DB; ++i) *reinterpret_cast<f32x4*>(&o_part[wave][16 * j + c][16 * i + 4 * g]) = o[j][i];
+  }
   __syncthreads();
-  for (int i = threadIdx.x; i < 16 * (D / 4); i += 64 * NW) {
-    const int row = i / (D / 4), d = i % (D / 4) * 4, rr = rt * 16 + row;
+  for (int i = threadIdx.x; i < ROWS * (D / 4); i += 64 * NW) {
+    const int row = i / (D / 4), d = i % (D / 4) * 4, rr = rt * ROWS + row;
     if (rr >= s.nq * group) break;
     float M = m_part[0][row];
 #pragma unroll
@@ -412,13 +443,35 @@ __global__ __launch_bounds__(64 * NW) void kv8_join_kernel(Kv8AttnArgs a) {
   if (lane == 0 && a.lse) a.lse[(s.row0 + q) * a.heads + h] = W == 0.0f ? -INFINITY : (M0 + __log2f(W)) * kLn2;
 }
 
+// Workgroups that take `tiles` row tiles of all runs and heads
+int64_t workgroups(const Kv8AttnArgs& a, int64_t tiles) {
+  return ((int64_t)a.runs * a.c.kv_heads * a.n_seqs + 7) / 8 * 8 * tiles;
+}
+
+// Tiles of 16 rows per workgroup.  Two where they leave two workgroups a CU, the most that fit: 8 sequences of 4,096
+// tokens, 8 key heads of 128, 64 queries of 32 heads 110 us against 138; 64 of 300, 5 queries 16.3 against 20.2.  With
+// fewer a call waits for a wave's walk, which two make longer: one sequence, 5 queries 19.2 against 14.5.  Heads of 64,
+// whose waves keep less, gain nothing up to 16 queries of 16 heads over 4 (30.3 and 29.5).  A row's result is the same.
+template <int D>
+int columns(const Kv8AttnArgs& a, int64_t rows) {
+  return D == 128 && workgroups(a, (rows + 31) / 32) >= 2l * device_cus() ? 2 : 1;
+}
+
 template <class T, int FORMAT, int D>
-eas_status launch(const Kv8AttnArgs& a, unsigned blocks, bool join, hipStream_t s) {
-  hipLaunchKernelGGL((kv8_attention_kernel<T, FORMAT, D>), dim3(blocks), dim3(64 * NW), 0, s, a);
+eas_status launch(Kv8AttnArgs& a, int64_t rows, bool join, hipStream_t s) {
+  const int C = rows > 16 ? columns<D>(a, rows) : 1;
+  const int64_t tiles = (rows + 16 * C - 1) / (16 * C), blocks = workgroups(a, tiles);
+  if (tiles > 0x7fffffff || blocks > 0x7fffffff || (int64_t)a.n_seqs * a.max_q * a.heads > 0x7fffffff)
+    return EAS_ERR_UNSUPPORTED;
+  a.row_tiles = (int)tiles;
+  if constexpr (D == 128) {
+    if (C == 2) hipLaunchKernelGGL((kv8_attention_kernel<T, FORMAT, D, 2>), dim3(blocks), dim3(64 * NW), 0, s, a);
+  }
+  if (C == 1) hipLaunchKernelGGL((kv8_attention_kernel<T, FORMAT, D, 1>), dim3(blocks), dim3(64 * NW), 0, s, a);
   if (hipGetLastError() != hipSuccess) return EAS_ERR_HIP;
   if (!join) return EAS_OK;
-  const int64_t rows = (int64_t)a.n_seqs * a.max_q * a.heads;
-  hipLaunchKernelGGL((kv8_join_kernel<T, D>), dim3((unsigned)((rows + NW - 1) / NW)), dim3(64 * NW), 0, s, a);
+  const int64_t joined = (int64_t)a.n_seqs * a.max_q * a.heads;
+  hipLaunchKernelGGL((kv8_join_kernel<T, D>), dim3((unsigned)((joined + NW - 1) / NW)), dim3(64 * NW), 0, s, a);
   return hipGetLastError() == hipSuccess ? EAS_OK : EAS_ERR_HIP;
 }
 
@@ -477,14 +530,10 @@ extern "C" eas_status eas_kv8_attention(const eas_kv8_cache* cache, const eas_at
     a.part_lse = a.part + parts * shape->head_dim;
   }
   const int group = a.heads / a.c.kv_heads;
-  const int64_t tiles = ((int64_t)(a.max_q < n_rows ? a.max_q : n_rows) * group + 15) / 16;
-  const int64_t blocks = tiles * a.runs * a.c.kv_heads * n_seqs;
-  if (tiles > 0x7fffffff || blocks > 0x7fffffff || (int64_t)n_seqs * a.max_q * a.heads > 0x7fffffff)
-    return EAS_ERR_UNSUPPORTED;
-  a.row_tiles = (int)tiles;
+  const int64_t rows = (int64_t)(a.max_q < n_rows ? a.max_q : n_rows) * group;
 #define EAS_KV8_CASE(DT, T, F, D)                                                   \
   if (shape->dtype == DT && cache->format == F && shape->head_dim == D) \
-    return launch<T, F, D>(a, (unsigned)blocks, join, (hipStream_t)stream)
+    return launch<T, F, D>(a, rows, join, (hipStream_t)stream)
   EAS_KV8_CASE(EAS_BF16, bf16, EAS_KV_INT8, 64);
   EAS_KV8_CASE(EAS_BF16, bf16, EAS_KV_INT8, 128);
   EAS_KV8_CASE(EAS_BF16, bf16, EAS_KV_E4M3, 64);

@@ -292,13 +292,13 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
       s[i & 1] = Mfma<T>::go(read_k(t, i), qf[i >> 1], i < 2 ? zero : s[i & 1]);
   };
   // Tile t: the online softmax of its scores s and O^T += V^T P^T, and beside them the next tile's scores n.  One
-  // FMA turns a score into x = s c - m, in log2 units over m, the maximum less TOP - 8.  m is raised lazily, when some x
-  // exceeds TOP, so p = 2^x <= 2^TOP and O is rarely scaled; O and l share m, so O / l is the same.  The first tile
+  // FMA turns a score into x = s c - m, in log2 units over m, the maximum less TOP - 8.  m is raised lazily, when some
+  // x exceeds TOP, so p = 2^x <= 2^TOP and O is rarely scaled; O and l share m, so O / l is the same.  The first tile
   // always sets it.  TOP keeps bf16's sums from overflow where a softmax's do not, and fp16's small weights from
-  // vanishing: what is lost below 2^-24 is 2^-32 of the largest weight.  The matrix unit takes 32 cycles an MFMA, in which the wave issues some 8 other instructions: the
-  // softmax's are dealt out behind the MFMAs by hand, in steps that nothing is moved across, each with the operands
-  // of the MFMA four steps on.  (Left to the compiler they come in blocks, and both waves of a SIMD wait for the
-  // same unit: matrix units 53% busy.)
+  // vanishing: what is lost below 2^-24 is 2^-32 of the largest weight.  The matrix unit takes 32 cycles an MFMA, in
+  // which the wave issues some 8 other instructions: the softmax's are dealt out behind the MFMAs by hand, in steps
+  // that nothing is moved across, each with the operands of the MFMA four steps on.  (Left to the compiler they come in
+  // blocks, and both waves of a SIMD wait for the same unit: matrix units 53% busy.)
   const auto step = [&](int t, f32x16* s, f32x16* n, auto masked, auto next) {
     constexpr bool MASKED = decltype(masked)::value, NEXT = decltype(next)::value;
     const int k0 = (tb + t) * KT;

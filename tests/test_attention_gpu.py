@@ -551,6 +551,29 @@ def test_decode_several_queries(dtype, heads, kv_heads, dim, form, causal):
 
 
 @pytest.mark.parametrize("form", FORMATS)
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("page,causal", [(16, True), (128, False)])
+def test_decode_full_batch(form, dtype, page, causal):
+    """Several queries of so many sequences that a workgroup takes two row tiles: right, and each as when alone."""
+    torch, _ = lib()
+    rng = np.random.default_rng(7)
+    lens = [0, 1, 2, 1025, 2100, 17, 1, 1500] + [int(n) for n in rng.integers(1, 400, 56)]
+    new = [3, 9, 2, 9, 5, 0, 1, 8] + [int(n) for n in rng.integers(0, 10, 56)]
+    both, table = filled(form, lens, page, 8, 128, 120)
+    c = cu(new)
+    q = make(torch, (c[-1], 32, 128), getattr(torch, dtype), 8)
+    out, lse = both.gpu.attention(q, i32(torch, lens), i32(torch, table), cu_q=i32(torch, c), max_q=9, causal=causal,
+                                  with_lse=True)
+    check_decode(both, q[:c[12]], lens[:12], table, new[:12], 128 ** -0.5, causal, out, lse)
+    for r, n in enumerate(new):
+        if n:
+            rows = slice(c[r], c[r + 1])
+            alone, alone_lse = both.gpu.attention(q[rows], i32(torch, lens[r:r + 1]), i32(torch, table[r:r + 1]),
+                                                  causal=causal, with_lse=True)
+            assert torch.equal(out[rows], alone) and torch.equal(lse[rows], alone_lse), "sequence %d" % r
+
+
+@pytest.mark.parametrize("form", FORMATS)
 def test_decode_small_weights_count(form):
     """As above, over the cache: 1,023 tokens of 2^-25.3 of the first's weight each, in the first's runs of tiles."""
     torch, A = lib()
