@@ -72,7 +72,7 @@ typedef struct {
  * k and v may hold anything, NaN included, outside the sequences' keys.
  * workspace: device, 16-byte aligned, at least the bytes that
  * eas_prompt_attention_workspace gives for the same arguments (0: NULL is
- * fine), which is more than 0 only where few queries see 8,192 keys or more; calls
+ * fine), which is more than 0 only where few queries see 2,048 keys or more; calls
  * that may overlap, captured ones included, need one each.  Nothing in it has
  * to be set before, or is kept from call to call.
  * Errors: INVALID_ARG, SHAPE (cu_q, cu_k), CAPACITY (n_seqs, the workspace),

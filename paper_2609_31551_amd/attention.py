@@ -16,7 +16,7 @@ from .eas import EAS_MAX_SEQS, EAS_OK, LIB, EasError  # noqa: F401  (EAS_MAX_SEQ
 P, I32, I64, VP = ctypes.POINTER, ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p
 EAS_FP32, EAS_BF16, EAS_FP16 = range(3)
 EAS_KV_INT8, EAS_KV_E4M3 = range(2)
-SPLIT_KEYS, SPLIT_TOKENS = 8192, 1024   # calls below / up to these need no workspace
+SPLIT_KEYS, SPLIT_TOKENS = 2048, 1024   # calls below / up to these need no workspace
 _DTYPE = {torch.float32: EAS_FP32, torch.bfloat16: EAS_BF16, torch.float16: EAS_FP16}
 _FORMAT = {torch.int8: EAS_KV_INT8, torch.float8_e4m3fn: EAS_KV_E4M3}
 

@@ -26,14 +26,18 @@ constexpr int KT = 64;               // keys per tile
 constexpr int kMaxRows = 1 << 30;    // queries or keys of a call
 constexpr int MAX_RUNS = 16;         // runs that a sequence's keys are split into
 
-// Runs of keys that each query tile of a sequence is split into, a workgroup each: of 4,096 keys at least, where the
-// sequence alone leaves CUs without a workgroup.  A call waits for its longest walk: 128 queries over 32,896 keys of 32
-// heads 90 us, in one walk 472; 512 over 8,704 93 and 138; chunks of 700 - 1,024 queries over 1,535 - 9,916 keys of 16
-// heads 105 and 124.  A batch that fills the chip anyway pays for the runs' sums: eight chunks of 512 over 9,512 keys
-// 631 and 570.  By a sequence's own sizes only: the join rounds otherwise, and a result must not depend on the batch.
+// Runs of keys that each query tile of a sequence is split into, a workgroup each, where the sequence alone leaves CUs
+// without one: of 4,096 keys at least, or fewer where it has less than 128 workgroups without, down to 1,024 with 32.
+// A call waits for its longest walk: 128 queries over 32,896 keys of 32 heads 92 us, in one walk 472; 64 over 5,064 31
+// and in runs of 4,096 79; 300 over 6,300 64 and 100; 512 over 8,704 93 and in one 138; chunks of 700 - 1,024 queries
+// over 1,535 - 9,916 keys of 16 heads 102 and 124.  A batch that fills the chip anyway pays for the runs' sums: sixteen
+// chunks of 64 over 8,256 keys 276, in runs of 4,096 244; eight of 512 over 9,512 keys 631, in one 570, in runs of
+// 1,024 838.  By a sequence's own sizes only: the join rounds otherwise, and a result must not depend on the batch.
 __host__ __device__ inline int n_runs(int lq, int lk, int heads) {
-  if ((int64_t)((lq + 127) / 128) * heads > 256) return 1;
-  const int runs = lk / 4096;
+  const int64_t alone = ((int64_t)lq + 127) / 128 * heads;   // workgroups of one run
+  if (alone > 256) return 1;
+  const int shortest = alone <= 32 ? 1024 : alone >= 128 ? 4096 : 32 * (int)alone;
+  const int runs = lk / shortest;
   return runs < 1 ? 1 : runs < MAX_RUNS ? runs : MAX_RUNS;
 }
 

@@ -94,6 +94,7 @@ LENS = {
     "few_keys": ([50, 5, 130, 3], [20, 0, 64, 1]),                       # first queries see nothing
     "long": ([300, 517], [700, 517]),
     "runs": ([5, 33, 0, 2, 129], [13000, 8193, 9000, 8192, 130]),        # few queries over keys in several runs
+    "short_runs": ([1, 60, 128, 129, 40], [2047, 2048, 2049, 4100, 1100]),
 }
 
 
