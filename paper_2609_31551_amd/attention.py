@@ -35,7 +35,8 @@ class Kv8CacheStruct(ctypes.Structure):
                 ("k", VP), ("v", VP), ("k_scale", VP), ("v_scale", VP)]
 
 
-_pack_shape = struct.Struct("5if8q").pack   # AttnShape's fields; made field by field it takes 0.8 us more
+# the structures' fields: made one by one, a structure takes 0.3 - 0.8 us more
+_pack_shape, _pack_cache = struct.Struct("5if8q").pack, struct.Struct("5i4x4P").pack
 _SIG = {
     "eas_prompt_attention": [P(AttnShape), VP, VP, VP, VP, VP, I32, VP, VP, VP, I64, VP],
     "eas_prompt_attention_workspace": [P(AttnShape), VP, VP, I32, P(I64)],
@@ -209,8 +210,8 @@ class Kv8Cache:
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.n_pages, self.kv_heads, self.page_tokens, self.head_dim = n, h, p, d
         self.device, self._index = k.device, index
-        self._c = Kv8CacheStruct(_FORMAT[codes], h, d, p, n, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(),
-                                 v_scale.data_ptr())
+        self._c = Kv8CacheStruct.from_buffer_copy(_pack_cache(_FORMAT[codes], h, d, p, n, k.data_ptr(), v.data_ptr(),
+                                                              k_scale.data_ptr(), v_scale.data_ptr()))
 
     @classmethod
     def empty(cls, n_pages, kv_heads, head_dim, page_tokens=64, dtype=torch.int8, device="cuda"):
@@ -222,12 +223,13 @@ class Kv8Cache:
                    new((n_pages, kv_heads), torch.float32), new((n_pages, kv_heads), torch.float32))
 
     def _table(self, pages):
-        if pages.dim() != 2:
-            raise ValueError("pages must be [n_seqs, max_pages]")
+        shape = pages.shape
+        if len(shape) != 2 or pages.dtype != torch.int32 or not pages.is_contiguous():
+            raise ValueError("pages must be a contiguous int32 tensor [n_seqs, max_pages], got %s %s"
+                             % (pages.dtype, tuple(shape)))
         if _device(pages) != self._index:
             raise ValueError("pages on %s, the cache on %s" % (pages.device, self.device))
-        n, max_pages = pages.shape
-        return _ints(pages, "pages", self._index, (n, max_pages)), max_pages, n
+        return pages.data_ptr(), shape[1], shape[0]
 
     def _split(self, cu, most, rows, n, name):
         """(pointer to the prefix sums or None, the most rows of a sequence)"""
@@ -264,13 +266,19 @@ class Kv8Cache:
         table, max_pages, n = self._table(pages)
         index, code = self._index, _dtype(dtype)
         shape = (int(n_rows), self.kv_heads, self.head_dim)
+        row = self.kv_heads * self.head_dim
+
         def new():
-            row = self.kv_heads * self.head_dim
             return torch.empty_strided(shape, (row, self.head_dim, 1), dtype=dtype, device=self.device)
-        k = _on(stream, new) if k is None else k
-        v = _on(stream, new) if v is None else v
-        ks = _rows(k, "k", self.kv_heads, self.head_dim, dtype, index)
-        vs = _rows(v, "v", self.kv_heads, self.head_dim, dtype, index)
+        ks = vs = row, self.head_dim
+        if k is None:
+            k = _on(stream, new)
+        else:
+            ks = _rows(k, "k", self.kv_heads, self.head_dim, dtype, index)
+        if v is None:
+            v = _on(stream, new)
+        else:
+            vs = _rows(v, "v", self.kv_heads, self.head_dim, dtype, index)
         if k.shape[0] != shape[0] or v.shape[0] != shape[0]:
             raise ValueError("k has %d rows, v %d, wanted %d" % (k.shape[0], v.shape[0], shape[0]))
         _check(LIB.eas_kv8_rows(self._c, code, table, max_pages, n, _ints(cu_rows, "cu_rows", index, (n + 1,)),
