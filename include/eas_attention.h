@@ -69,12 +69,14 @@ typedef struct {
  * softmax's sum of exponentials, -inf where no key is seen.
  * Rows of out and lse outside [0, cu_q[n_seqs]) are not touched.  A sequence's
  * result does not depend on the others, to the bit.
- * k and v may hold anything, NaN included, outside the sequences' keys.
+ * k and v may hold anything, NaN included, outside the sequences' keys.  What
+ * a query sees of infinities and NaN makes its result infinite or NaN, and
+ * nobody else's.
  * workspace: device, 16-byte aligned, at least the bytes that
  * eas_prompt_attention_workspace gives for the same arguments (0: NULL is
- * fine), which is more than 0 only where few queries see 2,048 keys or more; calls
- * that may overlap, captured ones included, need one each.  Nothing in it has
- * to be set before, or is kept from call to call.
+ * fine), which is more than 0 only where few queries see 2,048 keys or more;
+ * calls that may overlap, captured ones included, need one each.  Nothing in it
+ * has to be set before, or is kept from call to call.
  * Errors: INVALID_ARG, SHAPE (cu_q, cu_k), CAPACITY (n_seqs, the workspace),
  * UNSUPPORTED (element type, head_dim, strides, more than 2^30 queries or keys,
  * more than 2^31 - 1 work items). */
@@ -158,10 +160,12 @@ eas_status eas_kv8_rows(const eas_kv8_cache* cache, int32_t dtype, const int32_t
  * cut to [0, max_pages * page_tokens]; rows outside [0, n_rows) are not
  * touched.  A query that sees no token gets zeros and lse -inf.
  * lse: device fp32 [n_rows, heads] or NULL.
+ * Products of q with the codes are exact, sums and the softmax are held in
+ * fp32, weights are rounded to fp16 for the product with the values' codes.
  * workspace: device, 16-byte aligned, at least the bytes that
  * eas_kv8_attention_workspace gives for the same arguments (0, up to a max_len
- * of 1,024: NULL is fine); calls that may overlap, captured ones included, need one each.  Nothing in
- * it has to be set before, or is kept from call to call.
+ * of 1,024: NULL is fine); calls that may overlap, captured ones included, need
+ * one each.  Nothing in it has to be set before, or is kept from call to call.
  * A sequence's result does not depend on the other sequences, on max_q, on
  * max_len or on which pages hold its tokens, to the bit. */
 eas_status eas_kv8_attention(const eas_kv8_cache* cache, const eas_attn_shape* shape, const void* q, int32_t n_rows,
