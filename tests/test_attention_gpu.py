@@ -288,6 +288,17 @@ def test_large_values_do_not_overflow(causal):
     run_prompt(q, k, v, [0, 70], None, causal)
 
 
+@pytest.mark.parametrize("scale", [1e39, float("inf"), float("nan"), "x"])
+def test_binding_refuses_scales_that_are_no_float32(scale):
+    torch, A = lib()
+    q = make(torch, (10, 2, 64), torch.bfloat16, 1)
+    cache = A.Kv8Cache.empty(4, 2, 64, 16)
+    pages, lens = torch.zeros(2, 2, dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    for bad in (lambda: A.prompt_attention(q, q, q, [0, 10], scale=scale), lambda: cache.attention(q, lens, pages, scale=scale)):
+        with pytest.raises((ValueError, RuntimeError)):
+            bad()
+
+
 def test_binding_refusals():
     torch, A = lib()
     q = make(torch, (10, 4, 64), torch.bfloat16, 1)
@@ -759,6 +770,31 @@ def test_other_stream():
         s.synchronize()
         for a, b in zip(got, want):
             assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_calls_with_runs_on_two_streams_at_once():
+    """Their workspaces are their own: calls that overlap give what they give alone."""
+    torch, A = lib()
+    both, table = filled("e4m3", [5000, 3100], 64, 2, 128, 195)
+    table, lens = i32(torch, table), i32(torch, [5000, 3100])
+    q = make(torch, (40, 8, 128), torch.bfloat16, 196)
+    k, v = make(torch, (6000, 2, 128), torch.bfloat16, 197), make(torch, (6000, 2, 128), torch.bfloat16, 198)
+
+    def calls(x, stream=None):
+        return (*A.prompt_attention(x, k, v, [0, 40], [0, 6000], with_lse=True, stream=stream),
+                *both.gpu.attention(x[:6], lens, table, with_lse=True, stream=stream))
+    queries = [q, q.flip(0).contiguous()]
+    want = [calls(x) for x in queries]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for i in range(2):
+            got[i].append(calls(queries[i], streams[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for one in got[i]:
+            assert all(torch.equal(x, y) for x, y in zip(one, want[i]))
 
 
 @pytest.mark.parametrize("form", FORMATS)
