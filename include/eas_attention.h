@@ -69,9 +69,13 @@ typedef struct {
  * softmax's sum of exponentials, -inf where no key is seen.
  * Rows of out and lse outside [0, cu_q[n_seqs]) are not touched.  A sequence's
  * result does not depend on the others, to the bit.
- * k and v may hold anything, NaN included, outside the sequences' keys.  What
- * a query sees of infinities and NaN makes its result infinite or NaN, and
- * nobody else's.
+ * k and v may hold anything, NaN included, outside the sequences' keys, and
+ * what a query does not see never reaches its result.  A key whose score is
+ * -inf (an infinite dimension, or products that overflow fp32) weighs nothing;
+ * a query whose scores are all -inf gets zeros and lse -inf, as one that sees no
+ * key.  A score of NaN or +inf makes a query's result and lse NaN; a value of
+ * NaN or infinity makes that dimension of the result of who sees it infinite or
+ * NaN, whatever its weight.
  * workspace: device, 16-byte aligned, at least the bytes that
  * eas_prompt_attention_workspace gives for the same arguments (0: NULL is
  * fine), which is more than 0 only where few queries see 2,048 keys or more;
@@ -158,7 +162,8 @@ eas_status eas_kv8_rows(const eas_kv8_cache* cache, int32_t dtype, const int32_t
  * max_q, max_len: host, at least the queries and tokens of every sequence
  * (queries beyond are not computed, tokens beyond are not seen).  Lengths are
  * cut to [0, max_pages * page_tokens]; rows outside [0, n_rows) are not
- * touched.  A query that sees no token gets zeros and lse -inf.
+ * touched.  A query that sees no token gets zeros and lse -inf.  Scores of -inf,
+ * +inf and NaN do what they do in eas_prompt_attention.
  * lse: device fp32 [n_rows, heads] or NULL.
  * Products of q with the codes are exact, sums and the softmax are held in
  * fp32, weights are rounded to fp16 for the product with the values' codes.

@@ -273,6 +273,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[hb][e] = 0.0f;
   float m = 0.0f, l = 0.0f;
+  bool unset = true;   // no score above -inf yet; the same in both lanes of a query, as m is
 
   constexpr int NK = 2 * C::KS, NV = 4 * C::HB;   // MFMAs of a tile's scores, and of its products with the values
   // A operand of score MFMA i: keys 32 (i % 2) .. of k-step i / 2; of value MFMA j: block j % HB, keys 16 (j / HB) ..
@@ -297,9 +298,9 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
   };
   // Tile t: the online softmax of its scores s and O^T += V^T P^T, and beside them the next tile's scores n.  One
   // FMA turns a score into x = s c - m, in log2 units over m, the maximum less TOP - 8.  m is raised lazily, when some
-  // x exceeds TOP, so p = 2^x <= 2^TOP and O is rarely scaled; O and l share m, so O / l is the same.  The first tile
-  // always sets it.  TOP keeps bf16's sums from overflow where a softmax's do not, and fp16's small weights from
-  // vanishing: what is lost below 2^-24 is 2^-32 of the largest weight.  The matrix unit takes 32 cycles an MFMA, in
+  // x exceeds TOP, so p = 2^x <= 2^TOP and O is rarely scaled; O and l share m, so O / l is the same.  The first score
+  // above -inf sets it, in whichever tile that is: until then O and l are 0.  TOP keeps bf16's sums from overflow where
+  // a softmax's do not, and fp16's small weights from vanishing: what is lost below 2^-24 is 2^-32 of the largest weight.  The matrix unit takes 32 cycles an MFMA, in
   // which the wave issues some 8 other instructions: the softmax's are dealt out behind the MFMAs by hand, in steps
   // that nothing is moved across, each with the operands of the MFMA four steps on.  (Left to the compiler they come in
   // blocks, and both waves of a SIMD wait for the same unit: matrix units 53% busy.)
@@ -332,10 +333,11 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
       const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
       mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
     }
-    const bool need = t == 0 ? mx > -INFINITY : mx > TOP;   // a query that sees nothing keeps m = 0, l = 0
+    const bool need = mx > (unset ? -INFINITY : TOP);   // a query that sees nothing keeps m = 0, l = 0
     if (__any(need)) {
       const float d = need ? mx - (TOP - 8.0f) : 0.0f;
-      const float alpha = t == 0 ? 0.0f : __builtin_amdgcn_exp2f(-d);
+      const float alpha = unset ? 0.0f : __builtin_amdgcn_exp2f(-d);
+      unset = unset && !need;
       m += d;
       l *= alpha;
 #pragma unroll
