@@ -41,6 +41,9 @@ __host__ __device__ inline int n_runs(int lq, int lk, int heads) {
   return runs < 1 ? 1 : runs < MAX_RUNS ? runs : MAX_RUNS;
 }
 
+// Key tiles of each run, the last ones' fewer or none
+__host__ __device__ inline int run_tiles(int lk, int runs) { return ((lk + KT - 1) / KT + runs - 1) / runs; }
+
 // Work list: the query tiles of all sequences, a run each, those with most keys first where they are few enough to be
 // listed (when they are many, what the last ones leave idle is little).
 constexpr int LISTED = 768;
@@ -224,8 +227,9 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
   auto seen = [&](int q) { return a.causal ? max(0, min(lk, lk - lq + min(q, lq - 1) + 1)) : lk; };
   const int qw = q0 + wave * 32, qi = qw + l32;
   const int sees = seen(qi), fewest = seen(qw), most = qw < lq ? seen(qw + 31) : 0;
-  // key tiles of the query tile, from tb on those of the run, and of these the wave's
-  const int all = (seen(q0 + C::QT - 1) + KT - 1) / KT, each = (all + runs - 1) / runs, tb = run * each;
+  // key tiles of the query tile, from tb on those of the run, and of these the wave's; the runs' borders go by the
+  // sequence's keys alone, so that they are the same for 128 and 256 queries a workgroup
+  const int all = (seen(q0 + C::QT - 1) + KT - 1) / KT, each = run_tiles(lk, runs), tb = run * each;
   const int nt = max(0, min(each, all - tb)), nt_w = max(0, min(nt, (most + KT - 1) / KT - tb));
 
   x8 qf[C::KS];
@@ -579,8 +583,11 @@ int64_t list_tiles(PromptWork* w, int heads, int qt, int causal) {
     for (int r = 0; r < w->n; ++r)
       for (int64_t t = 0; t * qt < queries(r); ++t) {
         const int n = runs(r);
-        const int c = (int)(CLASSES - 1 - key_tiles(queries(r), keys(r), t, qt, causal) / n * CLASSES / top);
-        for (int k = 0; k < n; ++k) f(r, (int)t * n + k, c);
+        const int64_t walk = key_tiles(queries(r), keys(r), t, qt, causal), each = run_tiles((int)keys(r), n);
+        for (int k = 0; k < n; ++k) {
+          const int64_t left = walk - k * each, own = left < 0 ? 0 : left < each ? left : each;
+          f(r, (int)t * n + k, (int)(CLASSES - 1 - own * CLASSES / top));
+        }
       }
   };
   every([&](int, int, int c) { ++at[c + 1]; });
