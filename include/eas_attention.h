@@ -162,7 +162,8 @@ eas_status eas_kv8_rows(const eas_kv8_cache* cache, int32_t dtype, const int32_t
  * max_q, max_len: host, at least the queries and tokens of every sequence
  * (queries beyond are not computed, tokens beyond are not seen).  Lengths are
  * cut to [0, max_pages * page_tokens]; rows outside [0, n_rows) are not
- * touched.  A query that sees no token gets zeros and lse -inf.  Scores of -inf,
+ * touched.  Queries and tokens that are left out so leave the others' places i
+ * and j, Lq and lens[r] as they are.  A query that sees no token gets zeros and lse -inf.  Scores of -inf,
  * +inf and NaN do what they do in eas_prompt_attention.
  * lse: device fp32 [n_rows, heads] or NULL.
  * Products of q with the codes are exact, sums and the softmax are held in

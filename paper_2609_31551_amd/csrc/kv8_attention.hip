@@ -71,29 +71,37 @@ struct Kv8AttnArgs {
   float* part;          // [n_seqs, heads, slots, D] results of runs, then [n_seqs, heads, slots] their log2 sums
   float* part_lse;
   float scale_log2;     // scale * log2(e)
-  int heads, causal, n_rows, max_q, max_len, max_pages, n_seqs, slots, row_tiles, runs;
+  int heads, causal, n_rows, max_len, max_pages, n_seqs, slots, row_tiles, runs;
+  int max_q, most_q;    // the caller's, and a bound of the queries of a sequence that are computed
 };
 
 struct Seq {
-  long row0;   // first query's row
-  int nq, len;
+  long row0;     // row of the first query that is computed
+  int before;    // tokens before that query's own, where causal: it sees before + 1
+  int nq, len;   // queries that are computed, tokens that may be seen
 };
 
+// A sequence's queries without those beyond max_q and those of rows outside [0, n_rows): the others keep their places.
+// Prefix sums that do not fit may wrap; what is computed lies in [0, n_rows) whatever they hold.
 __device__ __forceinline__ Seq find_seq(const Kv8AttnArgs& a, int r) {
   Seq s;
-  long n;
+  unsigned lq = a.max_q;
+  s.row0 = (long)r * a.max_q;
   if (a.cu_q) {
     s.row0 = a.cu_q[r];
-    n = (long)a.cu_q[r + 1] - s.row0;
-  } else {
-    s.row0 = (long)r * a.max_q;
-    n = a.max_q;
+    lq = (unsigned)a.cu_q[r + 1] - (unsigned)a.cu_q[r];
   }
-  n = min(n, (long)a.max_q);
-  if (s.row0 < 0 || s.row0 + n > a.n_rows) n = s.row0 < 0 ? 0 : a.n_rows - s.row0;
-  s.nq = (int)max(n, 0l);
-  s.len = max(0, min(a.lens[r], min(a.max_len, a.max_pages << a.c.page_shift)));
+  const int len = max(0, min(a.lens[r], a.max_pages << a.c.page_shift));
+  const int skip = (int)max(-s.row0, 0l) & 0x7fffffff;
+  s.before = (int)((unsigned)len - lq + (unsigned)skip);
+  s.row0 = max(s.row0, 0l);
+  s.nq = (int)max(min((long)(min(max((int)lq, 0), a.max_q) - skip), a.n_rows - s.row0), 0l);
+  s.len = min(len, a.max_len);
   return s;
+}
+// Tokens that computed query i sees
+__device__ __forceinline__ int seen_by(const Kv8AttnArgs& a, const Seq& s, int i) {
+  return a.causal ? max(0, min(s.len, s.before + i + 1)) : s.len;
 }
 
 // 16 codes to fp16, exactly: int8 by building 1024 + (code + 128) and taking 1152 off
@@ -174,12 +182,12 @@ __global__ __launch_bounds__(64 * NW) void kv8_attention_kernel(Kv8AttnArgs a) {
     const int rho = rt * ROWS + 16 * j + c;
     const bool real = rho < s.nq * group;
     const int qi = real ? (unsigned)rho / (unsigned)group : 0, h = kvh * group + (real ? rho - qi * group : 0);
-    sees[j] = !real ? 0 : a.causal ? max(0, min(s.len, s.len - s.nq + qi + 1)) : s.len;
+    sees[j] = real ? seen_by(a, s, qi) : 0;
     q[j] = static_cast<const T*>(a.q) + (s.row0 + qi) * a.qs.row + h * a.qs.head + 16 * g;
   }
   // the last query sees most
   const int last = min(rt * ROWS + ROWS - 1, s.nq * group - 1) / group;
-  const int most = a.causal ? max(0, min(s.len, s.len - s.nq + last + 1)) : s.len;
+  const int most = seen_by(a, s, last);
   const long t_begin = (long)run * each;
   const int t_end = (int)min((long)most, t_begin + each);
 
@@ -405,8 +413,8 @@ template <class T, int D>
 __global__ __launch_bounds__(64 * NW) void kv8_join_kernel(Kv8AttnArgs a) {
   const unsigned row = blockIdx.x * NW + (threadIdx.x >> 6);   // (sequence, query, head), below 2^31
   const int lane = threadIdx.x & 63;
-  const int h = row % (unsigned)a.heads, q = row / (unsigned)a.heads % (unsigned)a.max_q;
-  const int r = row / (unsigned)a.heads / (unsigned)a.max_q;
+  const int h = row % (unsigned)a.heads, q = row / (unsigned)a.heads % (unsigned)a.most_q;
+  const int r = row / (unsigned)a.heads / (unsigned)a.most_q;
   if (r >= a.n_seqs) return;
   const Seq s = find_seq(a, r);
   if (q >= s.nq) return;
@@ -461,7 +469,7 @@ template <class T, int FORMAT, int D>
 eas_status launch(Kv8AttnArgs& a, int64_t rows, bool join, hipStream_t s) {
   const int C = rows > 16 ? columns<D>(a, rows) : 1;
   const int64_t tiles = (rows + 16 * C - 1) / (16 * C), blocks = workgroups(a, tiles);
-  if (tiles > 0x7fffffff || blocks > 0x7fffffff || (int64_t)a.n_seqs * a.max_q * a.heads > 0x7fffffff)
+  if (tiles > 0x7fffffff || blocks > 0x7fffffff || (int64_t)a.n_seqs * a.most_q * a.heads > 0x7fffffff)
     return EAS_ERR_UNSUPPORTED;
   a.row_tiles = (int)tiles;
   if constexpr (D == 128) {
@@ -470,7 +478,7 @@ eas_status launch(Kv8AttnArgs& a, int64_t rows, bool join, hipStream_t s) {
   if (C == 1) hipLaunchKernelGGL((kv8_attention_kernel<T, FORMAT, D, 1>), dim3(blocks), dim3(64 * NW), 0, s, a);
   if (hipGetLastError() != hipSuccess) return EAS_ERR_HIP;
   if (!join) return EAS_OK;
-  const int64_t joined = (int64_t)a.n_seqs * a.max_q * a.heads;
+  const int64_t joined = (int64_t)a.n_seqs * a.most_q * a.heads;
   hipLaunchKernelGGL((kv8_join_kernel<T, D>), dim3((unsigned)((joined + NW - 1) / NW)), dim3(64 * NW), 0, s, a);
   return hipGetLastError() == hipSuccess ? EAS_OK : EAS_ERR_HIP;
 }
@@ -515,13 +523,13 @@ extern "C" eas_status eas_kv8_attention(const eas_kv8_cache* cache, const eas_at
   a.cu_q = cu_q, a.lens = lens, a.pages = pages;
   a.scale_log2 = shape->scale * kLog2e;
   a.heads = shape->heads, a.causal = shape->causal;
-  a.n_rows = n_rows, a.max_q = max_q < n_rows ? max_q : n_rows, a.max_pages = max_pages, a.n_seqs = n_seqs;
-  if (!cu_q) a.max_q = max_q;   // a sequence's rows start at multiples of it
+  a.n_rows = n_rows, a.max_q = max_q, a.most_q = cu_q && n_rows < max_q ? n_rows : max_q;
+  a.max_pages = max_pages, a.n_seqs = n_seqs;
   const int64_t held = (int64_t)max_pages * cache->page_tokens;
   a.max_len = max_len < held ? max_len : (int)held;
   a.runs = n_runs(a.max_len, 1);
   const bool join = a.runs > 1;
-  a.slots = (int)slots(a.max_q, a.max_len);
+  a.slots = (int)slots(a.most_q, a.max_len);
   if (join) {
     const int64_t parts = (int64_t)n_seqs * a.heads * a.slots;
     if (!workspace || !aligned16(workspace)) return EAS_ERR_INVALID_ARG;
@@ -530,7 +538,7 @@ extern "C" eas_status eas_kv8_attention(const eas_kv8_cache* cache, const eas_at
     a.part_lse = a.part + parts * shape->head_dim;
   }
   const int group = a.heads / a.c.kv_heads;
-  const int64_t rows = (int64_t)(a.max_q < n_rows ? a.max_q : n_rows) * group;
+  const int64_t rows = (int64_t)(max_q < n_rows ? max_q : n_rows) * group;
 #define EAS_KV8_CASE(DT, T, F, D)                                                   \
   if (shape->dtype == DT && cache->format == F && shape->head_dim == D) \
     return launch<T, F, D>(a, rows, join, (hipStream_t)stream)

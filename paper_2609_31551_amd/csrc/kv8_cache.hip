@@ -40,11 +40,11 @@ __device__ __forceinline__ bool find_span(const AppendArgs& a, int r, int b, Spa
     row0 = (long)r * a.max_new;
     n = a.max_new;
   }
-  if (row0 < 0) return false;
   n = min(n, min((long)a.max_new, a.n_rows - row0));
-  const long slot = (held >> a.c.page_shift) + (long)b;
-  if (n <= 0 || slot >= a.max_pages) return false;
-  const long lo = max((long)held, slot << a.c.page_shift), hi = min(held + n, (slot + 1) << a.c.page_shift);
+  const long from = held + max(-row0, 0l);   // the first token whose row there is
+  const long slot = (from >> a.c.page_shift) + b;
+  if (slot >= a.max_pages) return false;
+  const long lo = max(from, slot << a.c.page_shift), hi = min(held + n, (slot + 1) << a.c.page_shift);
   if (lo >= hi) return false;
   s->page = a.pages[(long)r * a.max_pages + slot];
   if (s->page < 0 || s->page >= a.c.n_pages) return false;
