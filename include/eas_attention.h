@@ -83,7 +83,7 @@ typedef struct {
  * has to be set before, or is kept from call to call.
  * Errors: INVALID_ARG, SHAPE (cu_q, cu_k), CAPACITY (n_seqs, the workspace),
  * UNSUPPORTED (element type, head_dim, strides, more than 2^30 queries or keys,
- * more than 2^31 - 1 work items). */
+ * more threads than a launch holds, 2^32 - 1: 2 for each query and head). */
 eas_status eas_prompt_attention(const eas_attn_shape* shape, const void* q, const void* k, const void* v,
                                 const int32_t* cu_q, const int32_t* cu_k, int32_t n_seqs, void* out, float* lse,
                                 void* workspace, int64_t workspace_bytes, void* stream);
@@ -120,7 +120,13 @@ typedef struct {
  * [0, n_pages) is a page that is not held: tokens appended to it are dropped,
  * its rows read as zeros, and attention does not see its tokens.  Pages may be
  * shared between sequences for reading.  A page that gets tokens in a call is
- * named once in it: appended to from two places, its codes are undefined. */
+ * named once in it: appended to from two places, its codes are undefined.
+ * The calls launch workgroups of up to 256 threads for what the host's bounds
+ * allow -- every sequence, head and page that max_new tokens, 64 rows of max_rows
+ * or 16 queries of max_q and a run of max_len tokens can touch -- and refuse
+ * bounds that allow 2^32 threads or more over the sequences (append, rows) or
+ * over sequences and heads (attention) with EAS_ERR_UNSUPPORTED: bounds near the
+ * batch's own avoid that. */
 
 /* Appends new keys and values.  k, v: device [n_rows] rows of kv_heads heads.
  * Sequence r's new tokens are rows cu_new[r] .. cu_new[r+1] (device int32

@@ -71,6 +71,9 @@ inline eas_status check_table(const eas_kv8_cache* c, const int32_t* pages, int3
   return (int64_t)max_pages * c->page_tokens > (1 << 30) ? EAS_ERR_UNSUPPORTED : EAS_OK;
 }
 
+// A grid's dimension holds less than 2^32 threads.
+inline bool fits_launch(int64_t workgroups, int threads) { return workgroups <= 0xffffffffll / threads; }
+
 // ---- the cache's scales and codes (device) -----------------------------------
 
 // The cache as the kernels get it.

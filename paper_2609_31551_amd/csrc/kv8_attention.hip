@@ -467,10 +467,11 @@ int columns(const Kv8AttnArgs& a, int64_t rows) {
 
 template <class T, int FORMAT, int D>
 eas_status launch(Kv8AttnArgs& a, int64_t rows, bool join, hipStream_t s) {
+  const int64_t joined = (int64_t)a.n_seqs * a.most_q * a.heads;
+  if (joined > 0x7fffffff || (join && !fits_launch((joined + NW - 1) / NW, 64 * NW))) return EAS_ERR_UNSUPPORTED;
   const int C = rows > 16 ? columns<D>(a, rows) : 1;
   const int64_t tiles = (rows + 16 * C - 1) / (16 * C), blocks = workgroups(a, tiles);
-  if (tiles > 0x7fffffff || blocks > 0x7fffffff || (int64_t)a.n_seqs * a.most_q * a.heads > 0x7fffffff)
-    return EAS_ERR_UNSUPPORTED;
+  if (!fits_launch(blocks, 64 * NW)) return EAS_ERR_UNSUPPORTED;
   a.row_tiles = (int)tiles;
   if constexpr (D == 128) {
     if (C == 2) hipLaunchKernelGGL((kv8_attention_kernel<T, FORMAT, D, 2>), dim3(blocks), dim3(64 * NW), 0, s, a);
@@ -478,7 +479,6 @@ eas_status launch(Kv8AttnArgs& a, int64_t rows, bool join, hipStream_t s) {
   if (C == 1) hipLaunchKernelGGL((kv8_attention_kernel<T, FORMAT, D, 1>), dim3(blocks), dim3(64 * NW), 0, s, a);
   if (hipGetLastError() != hipSuccess) return EAS_ERR_HIP;
   if (!join) return EAS_OK;
-  const int64_t joined = (int64_t)a.n_seqs * a.most_q * a.heads;
   hipLaunchKernelGGL((kv8_join_kernel<T, D>), dim3((unsigned)((joined + NW - 1) / NW)), dim3(64 * NW), 0, s, a);
   return hipGetLastError() == hipSuccess ? EAS_OK : EAS_ERR_HIP;
 }

@@ -217,8 +217,9 @@ __global__ __launch_bounds__(NT) void kv8_rows_kernel(RowsArgs a) {
   constexpr int IV = (SPAN / 4 * C + NT - 1) / NT; // and of values, 4 tokens each
   const int r = blockIdx.x / a.blocks, b = blockIdx.x % a.blocks, h = blockIdx.y, tid = threadIdx.x;
   const int shift = a.c.page_shift, mask = (1 << shift) - 1;
-  const long row0 = a.cu[r], n = min((long)a.cu[r + 1] - row0, (long)a.max_rows);
-  const long first = a.first ? a.first[r] : 0;
+  const long skip = max(-(long)a.cu[r], 0l), row0 = a.cu[r] + skip;   // rows before 0 are not there
+  const long n = min((long)a.cu[r + 1] - a.cu[r], (long)a.max_rows) - skip;
+  const long first = (a.first ? a.first[r] : 0) + skip;
   // tokens of this workgroup; a sequence that starts below 0 has spans below 0 too
   const long base = (first >= 0 ? first / SPAN : -((-first + SPAN - 1) / SPAN)) * SPAN + (long)b * SPAN;
   const long lo = max(first, base), hi = min(first + n, base + SPAN);
@@ -333,6 +334,8 @@ struct LaunchAppend {
     // a decoding step's tokens by one wave each (16 sequences 5.0 us, with 256 threads 5.4); small pages
     // by fewer threads (16,384 tokens in 16-token pages, 8 heads of 64: 17.5 us, with 256 threads 25.6)
     const int pieces = (D << a.c.page_shift) / 8;
+    if (!fits_launch(grid.x, a.max_new <= FEW_TOKENS || pieces <= 256 ? 64 : pieces == 512 ? 128 : 256))
+      return EAS_ERR_UNSUPPORTED;
     if (a.max_new <= FEW_TOKENS)
       hipLaunchKernelGGL((kv8_append_kernel<T, F, D, 64, 1, true>), grid, dim3(64), 0, s, a);
     else if (pieces == 128)
@@ -398,8 +401,8 @@ extern "C" eas_status eas_kv8_rows(const eas_kv8_cache* cache, int32_t dtype, co
   if (n_rows == 0 || max_rows == 0 || n_seqs == 0) return EAS_OK;
   if (!k && !v) return EAS_ERR_INVALID_ARG;
   RowsArgs a = {kv8_args(cache), k, v, k_strides, v_strides, cu_rows, first, pages, n_rows, max_rows, max_pages,
-                touched(max_rows, SPAN, 0x7fffffff)};
-  if ((int64_t)a.blocks * n_seqs > 0x7fffffff) return EAS_ERR_UNSUPPORTED;
+                touched(max_rows < n_rows ? max_rows : n_rows, SPAN, 0x7fffffff)};
+  if (!fits_launch((int64_t)a.blocks * n_seqs, NT)) return EAS_ERR_UNSUPPORTED;
   return by_type<LaunchRows>(dtype, cache->format, cache->head_dim, a,
                              dim3((unsigned)(a.blocks * n_seqs), (unsigned)cache->kv_heads), (hipStream_t)stream);
 }

@@ -661,7 +661,7 @@ eas_status launch_all(const eas_attn_shape* shape, PromptArgs a, PromptWork* w, 
   const int qt = query_tile(*w, shape->heads, shape->causal);
   const int64_t tiles = list_tiles(w, shape->heads, qt, shape->causal);
   const int64_t blocks = workgroups(tiles, shape->heads, shape->kv_heads);
-  if (blocks > 0x7fffffff) return EAS_ERR_UNSUPPORTED;
+  if (!fits_launch(blocks, 2 * qt)) return EAS_ERR_UNSUPPORTED;   // a wave for 32 queries
   a.tiles = (int)tiles;
   const eas_status st = qt == 256 ? launch<T, HD, 8>(a, *w, (unsigned)blocks, s)
                                   : launch<T, HD, 4>(a, *w, (unsigned)blocks, s);

@@ -58,3 +58,19 @@ def test_append_drops_rows_before_the_first(form, page, lo, hi):
     both.gpu.append(k, v, i32(torch, [1]), i32(torch, table), i32(torch, [lo, hi]), max_new=hi - lo)
     both.ref.append(f64(k), f64(v), 1 - lo, list(table[0]))
     both.check_rows([1 - lo + hi], table, torch.bfloat16)
+
+
+def test_rows_of_sequences_that_begin_before_the_first_row():
+    """And bounds far above the batch's: every row there is, is written, and no other."""
+    torch, A = lib()
+    both, table = filled("int8", [200, 90], 32, 2, 64, 330)
+    t, first = i32(torch, table), i32(torch, [10, 3])
+    want = both.gpu.rows(t, i32(torch, [0, 150, 230]), 230, first=first)
+    for most in (230, 100000, 1 << 30):
+        got = [torch.full((140, 2, 64), 5.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        both.gpu.rows(t, i32(torch, [-70, 80, 160]), 140, first=first, max_len=most, k=got[0], v=got[1])
+        for a, b in zip(got, want):
+            assert torch.equal(a, b[70:210])
+    got = torch.full((140, 2, 64), 5.0, dtype=torch.bfloat16, device="cuda")
+    both.gpu.rows(t, i32(torch, [-70, 80, 160]), 140, first=first, max_len=100, k=got)
+    assert torch.equal(got[:30], want[0][70:100]) and (got[30:80] == 5.0).all() and torch.equal(got[80:], want[0][150:210])
