@@ -17,6 +17,7 @@ P, I32, I64, VP = ctypes.POINTER, ctypes.c_int32, ctypes.c_int64, ctypes.c_void_
 EAS_FP32, EAS_BF16, EAS_FP16 = range(3)
 EAS_KV_INT8, EAS_KV_E4M3 = range(2)
 SPLIT_KEYS, SPLIT_TOKENS = 2048, 1024   # calls below / up to these need no workspace
+_INT_MAX = 2 ** 31 - 1
 _DTYPE = {torch.float32: EAS_FP32, torch.bfloat16: EAS_BF16, torch.float16: EAS_FP16}
 _FORMAT = {torch.int8: EAS_KV_INT8, torch.float8_e4m3fn: EAS_KV_E4M3}
 
@@ -87,6 +88,16 @@ def _ints(t, name, index, shape):
         raise ValueError("%s must be a contiguous int32 tensor of shape %s on cuda:%d, got %s %s on %s"
                          % (name, tuple(shape), index, t.dtype, tuple(t.shape), t.device))
     return t.data_ptr()
+
+
+def _count(most, rows, name):
+    """A bound of a batch (None: ``rows``) as a C int: what is more than that holds is as good as its largest."""
+    if rows > _INT_MAX:
+        raise ValueError("%d rows are more than the calls take" % rows)
+    most = rows if most is None else min(int(most), _INT_MAX)
+    if most < 0:
+        raise ValueError("%s must not be negative" % name)
+    return most
 
 
 def _dtype(dtype):
@@ -234,13 +245,13 @@ class Kv8Cache:
     def _split(self, cu, most, rows, n, name):
         """(pointer to the prefix sums or None, the most rows of a sequence)"""
         if cu is not None:
-            return _ints(cu, name, self._index, (n + 1,)), rows if most is None else int(most)
+            return _ints(cu, name, self._index, (n + 1,)), _count(most, rows, "the most rows of a sequence")
         if most is None:
             most = rows // n if n else 0
         if most * n != rows:
             raise ValueError("without %s every sequence has the same number of rows: %d rows, %d sequences of %d"
                              % (name, rows, n, most))
-        return None, int(most)
+        return None, _count(most, rows, "the most rows of a sequence")
 
     def append(self, k, v, held, pages, cu_new=None, max_new=None, stream=None):
         """New tokens' keys and values [rows, kv_heads, head_dim] behind the ``held`` (int32 device [n_seqs]) tokens
@@ -283,7 +294,7 @@ class Kv8Cache:
             raise ValueError("k has %d rows, v %d, wanted %d" % (k.shape[0], v.shape[0], shape[0]))
         _check(LIB.eas_kv8_rows(self._c, code, table, max_pages, n, _ints(cu_rows, "cu_rows", index, (n + 1,)),
                                 None if first is None else _ints(first, "first", index, (n,)),
-                                shape[0] if max_len is None else int(max_len), shape[0], k.data_ptr(),
+                                _count(max_len, shape[0], "max_len"), shape[0], k.data_ptr(),
                                 Strides(*ks), v.data_ptr(), Strides(*vs),
                                 _current_stream(index) if stream is None else stream.cuda_stream),
                "Kv8Cache.rows")
@@ -301,9 +312,7 @@ class Kv8Cache:
         qs = _rows(q, "q", None, dim, dtype, index)
         rows, heads = q.shape[0], q.shape[1]
         cu, most_q = self._split(cu_q, max_q, rows, n, "cu_q")
-        most = max_pages * self.page_tokens
-        if max_len is not None and max_len < most:
-            most = int(max_len)
+        most = min(_count(max_len, max_pages * self.page_tokens, "max_len"), max_pages * self.page_tokens)
         out, lse, strides, lse_ptr = _outputs(q, out, lse, with_lse, index, stream)
         shape = _shape(code, heads, self.kv_heads, dim, causal, scale, qs, (0, 0), (0, 0), strides)
         need = I64()
