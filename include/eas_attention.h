@@ -52,7 +52,7 @@ typedef struct {
                             /* heads is a multiple of kv_heads, at most 1024     */
   int32_t head_dim;         /* 64 or 128                                         */
   int32_t causal;           /* 1 or 0                                            */
-  float scale;              /* finite; multiplies q . k                          */
+  float scale;              /* multiplies q . k; 2.3e38 at most, so that scale * log2(e) is finite */
   eas_strides q, k, v, out;
 } eas_attn_shape;
 

@@ -48,7 +48,9 @@ inline eas_status check_shape(const eas_attn_shape* s) {
   const eas_status st = check_dtype(s->dtype);
   if (st != EAS_OK) return st;
   if (s->heads <= 0 || s->kv_heads <= 0 || s->heads > 1024 || s->heads % s->kv_heads) return EAS_ERR_INVALID_ARG;
-  if ((s->causal != 0 && s->causal != 1) || !std::isfinite(s->scale) || s->head_dim <= 0) return EAS_ERR_INVALID_ARG;
+  // the kernels work on scale * log2(e)
+  if ((s->causal != 0 && s->causal != 1) || !std::isfinite(s->scale * kLog2e) || s->head_dim <= 0)
+    return EAS_ERR_INVALID_ARG;
   return s->head_dim == 64 || s->head_dim == 128 ? EAS_OK : EAS_ERR_UNSUPPORTED;
 }
 

@@ -19,3 +19,16 @@ def test_more_threads_than_a_launch_holds():
     # prompts: 2^22 workgroups of 256 queries for each of two heads
     s = shape(heads=2, kv_heads=2, q=(256, 128), k=(256, 128), v=(256, 128), out=(256, 128))
     assert prompt(s, cu_q=(0, 1 << 30)) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("scale", [2.4e38, -2.4e38, 3.4e38])
+def test_scales_that_are_infinite_in_log2_units(scale):
+    assert prompt(shape(scale=scale)) == BAD
+    assert attend(s=shape(scale=scale)) == BAD
+
+
+def test_the_largest_scales():
+    """The shape passes: the next argument is refused."""
+    for scale in (2.3e38, -2.3e38, 0.0):
+        assert prompt(shape(scale=scale), cu_q=(0, 9), cu_k=(0, (1 << 30) + 1)) == UNSUPPORTED
+        assert attend(cache(page_tokens=16), shape(scale=scale), max_pages=(1 << 26) + 1) == UNSUPPORTED
