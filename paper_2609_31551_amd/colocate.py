@@ -30,6 +30,7 @@ into the 8-bit cache, and a decoding step; ``beside_prefill`` times an encode
 micro-batch and that work alone and side by side on two streams.
 """
 import ctypes
+import math
 import statistics
 import time
 
@@ -223,41 +224,58 @@ class PrefillWork:
 def beside_prefill(run, work, reps=3):
     """Times (ms, medians of ``reps``) of ``run(stream)`` -- one encode micro-batch -- and of one ``work.step``, each
     alone and side by side on two streams: {"encode_alone", "encode_beside", "prefill_alone", "prefill_beside"}.
-    Side by side the prefill stream is given steps enough to outlast the micro-batch."""
+    What is timed is enqueued behind a gate (one reserved CU) that is opened when it is all there, so the host's time
+    is not in it, and both streams begin at once.  Side by side, the steps outlast the micro-batch (or, where it is
+    shorter than a few of them, several in a row), and a step's time is the mean of those that lie wholly within it."""
     import torch
     measure, prefill = _stream("measure"), _stream("prefill")
 
     def event():
         return torch.cuda.Event(enable_timing=True)
 
-    def encode():
-        e0, e1 = event(), event()
-        e0.record(measure)
-        run(measure)
-        e1.record(measure)
-        return e0, e1
+    def timed(batches, steps, queued=256):
+        """Events around the micro-batches, before and after each step, and whether the gate held; up to ``queued``
+        steps wait behind it, which the streams' queues have room for."""
+        e, p = [event(), event()], [event() for _ in range(steps + 1)]
 
-    def steps(n):
-        e0, e1 = event(), event()
-        e0.record(prefill)
-        for _ in range(n):
-            work.step(prefill)
-        e1.record(prefill)
-        return e0, e1
+        def enqueue(some):
+            for i in some:
+                work.step(prefill)
+                p[i + 1].record(prefill)
+        with CuReservation(1, max_s=3.0) as gate:
+            opened = torch.cuda.Event()
+            opened.record(gate.stream)
+            measure.wait_event(opened)
+            prefill.wait_event(opened)
+            e[0].record(measure)
+            for _ in range(batches):
+                run(measure)
+            e[1].record(measure)
+            p[0].record(prefill)
+            enqueue(range(min(steps, queued)))
+        enqueue(range(queued, steps))
+        e[1].synchronize()
+        p[-1].synchronize()
+        return e, p, not gate.lapsed()
 
-    def ms(events, n=1):
-        events[1].synchronize()
-        return events[0].elapsed_time(events[1]) / n
-    torch.cuda.synchronize()
-    ms(encode()), ms(steps(2))   # warm-up
-    alone, each, beside, step_beside = [], [], [], []
+    def side_by_side(batches, steps):
+        """(ms of a micro-batch, mean ms of a step beside it)"""
+        for _ in range(6):
+            e, p, held = timed(batches, steps)
+            beside = [a.elapsed_time(b) for a, b in zip(p, p[1:]) if e[0].elapsed_time(a) >= 0 <= b.elapsed_time(e[1])]
+            if held and beside and e[1].elapsed_time(p[-1]) >= 0:
+                return e[0].elapsed_time(e[1]) / batches, statistics.mean(beside)
+            steps *= 2   # the micro-batch outlasted them
+        raise RuntimeError("%d steps of prefill work do not cover %d micro-batches" % (steps // 2, batches))
+    timed(1, 2)   # warm-up
+    times = {"encode_alone": [], "prefill_alone": [], "encode_beside": [], "prefill_beside": []}
     for _ in range(reps):
-        alone.append(ms(encode()))
-        each.append(ms(steps(8), 8))
-        n = int(3 * alone[-1] / each[-1]) + 4
-        p = steps(n)
-        e = encode()
-        beside.append(ms(e))
-        step_beside.append(ms(p, n))
-    return {k: statistics.median(v) for k, v in (("encode_alone", alone), ("encode_beside", beside),
-                                                 ("prefill_alone", each), ("prefill_beside", step_beside))}
+        e, _, _ = timed(1, 0)
+        alone = e[0].elapsed_time(e[1])
+        _, p, _ = timed(0, 8)
+        each = p[0].elapsed_time(p[-1]) / 8
+        batches = max(1, math.ceil(4 * each / alone))
+        beside, step_beside = side_by_side(batches, int(2 * batches * alone / each) + 4)
+        for k, v in zip(times, (alone, each, beside, step_beside)):
+            times[k].append(v)
+    return {k: statistics.median(v) for k, v in times.items()}
