@@ -172,8 +172,10 @@ eas_status eas_kv8_rows(const eas_kv8_cache* cache, int32_t dtype, const int32_t
  * and j, Lq and lens[r] as they are.  A query that sees no token gets zeros and lse -inf.  Scores of -inf,
  * +inf and NaN do what they do in eas_prompt_attention.
  * lse: device fp32 [n_rows, heads] or NULL.
- * Products of q with the codes are exact, sums and the softmax are held in
- * fp32, weights are rounded to fp16 for the product with the values' codes.
+ * A row's values of q are taken to fp16 relative to its largest, each good to
+ * 2^-39 of that (exactly, where it is 2^-31 of the largest or more); their
+ * products with the codes are exact, sums and the softmax are held in fp32, and
+ * weights are rounded to fp16 for the product with the values' codes.
  * workspace: device, 16-byte aligned, at least the bytes that
  * eas_kv8_attention_workspace gives for the same arguments (0, up to a max_len
  * of 1,024: NULL is fine); calls that may overlap, captured ones included, need

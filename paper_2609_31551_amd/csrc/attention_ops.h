@@ -105,7 +105,7 @@ __device__ __forceinline__ float block_scale(float top) {
   return __uint_as_float((uint32_t)e << 23);
 }
 
-// 1 / scale of a power of two in [2^-126, 2^121], 0 for 0
+// 1 / scale of a power of two in [2^-126, 2^122], 0 for 0 (bf16's largest needs 2^122 in int8)
 __device__ __forceinline__ float inverse_scale(float s) {
   return s > 0.0f ? __uint_as_float(0x7f000000u - __float_as_uint(s)) : 0.0f;
 }

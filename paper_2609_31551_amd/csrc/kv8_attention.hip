@@ -11,12 +11,14 @@
 // the waves' final sums.  The 16 tokens lie in one page, whatever its size, so a lane
 // looks up one scale of each kind.
 //
-// Codes are exact in fp16 (both formats), and so are the queries after a multiplication by
-// a power of two for each row, so the scores are exact products summed in fp32.  With
-// block scales 2^f of the values, x = scale * q . k in log2 units and running maxima m of
-// x and m' of x + f - 15, a lane sums l += 2^(x - m) and O += 2^(x + f - m') * code:
-// whatever the scales, the largest weight of a code is 2^15, so rounding the weights to
-// fp16 costs 2^-11 of each, or of those below fp16's normal range 2^-40 of the largest.
+// Codes are exact in fp16 (both formats).  Queries are multiplied by a power of two for each
+// row that brings its largest value to [2^14, 2^15); in fp16 each is then good to 2^-25, which
+// is 2^-39 of the largest (and exact from 2^-31 of it on, where 8 bits fit above fp16's last).
+// Scores are exact products of such values, summed in fp32.  With block scales 2^f of the
+// values, x = scale * q . k in log2 units and running maxima m of x and m' of x + f - 15, a
+// lane sums l += 2^(x - m) and O += 2^(x + f - m') * code: whatever the scales, the largest
+// weight of a code is 2^15, so rounding the weights to fp16 costs 2^-11 of each, or of those
+// below fp16's normal range 2^-40 of the largest.
 //
 // A sequence's tokens are split into runs by a rule on its own length and queries only,
 // so its result does not depend on the batch; each run's result goes to the workspace

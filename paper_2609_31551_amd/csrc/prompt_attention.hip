@@ -349,10 +349,11 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
   // FMA turns a score into x = s c - m, in log2 units over m, the maximum less TOP - 8.  m is raised lazily, when some
   // x exceeds TOP, so p = 2^x <= 2^TOP and O is rarely scaled; O and l share m, so O / l is the same.  The first score
   // above -inf sets it, in whichever tile that is: until then O and l are 0.  TOP keeps bf16's sums from overflow where
-  // a softmax's do not, and fp16's small weights from vanishing: what is lost below 2^-24 is 2^-32 of the largest weight.  The matrix unit takes 32 cycles an MFMA, in
-  // which the wave issues some 8 other instructions: the softmax's are dealt out behind the MFMAs by hand, in steps
-  // that nothing is moved across, each with the operands of the MFMA four steps on.  (Left to the compiler they come in
-  // blocks, and both waves of a SIMD wait for the same unit: matrix units 53% busy.)
+  // a softmax's do not, and fp16's small weights from vanishing: what is lost below 2^-24 is 2^-32 of the largest
+  // weight.  The matrix unit takes 32 cycles an MFMA, in which the wave issues some 8 other instructions: the softmax's
+  // are dealt out behind the MFMAs by hand, in steps that nothing is moved across, each with the operands of the MFMA
+  // four steps on.  (Left to the compiler they come in blocks, and both waves of a SIMD wait for the same unit: 8,192
+  // tokens with all keys 942 us, so 897.)
   const auto step = [&](int t, f32x16* s, f32x16* n, auto masked, auto next) {
     constexpr bool MASKED = decltype(masked)::value, NEXT = decltype(next)::value;
     const int k0 = (tb + t) * KT;
