@@ -80,7 +80,10 @@ typedef struct {
  * eas_prompt_attention_workspace gives for the same arguments (0: NULL is
  * fine), which is more than 0 only where few queries see 2,048 keys or more;
  * calls that may overlap, captured ones included, need one each.  Nothing in it
- * has to be set before, or is kept from call to call.
+ * has to be set before, or is kept from call to call.  A sequence's share goes by
+ * its own sizes, as its result does: 2^19 * (head_dim + 1) * 4 bytes at most, 258
+ * MiB at heads of 128 (1,024 queries of 32 heads over 65,536 keys), however many
+ * are in the batch.
  * Errors: INVALID_ARG, SHAPE (cu_q, cu_k), CAPACITY (n_seqs, the workspace),
  * UNSUPPORTED (element type, head_dim, strides, more than 2^30 queries or keys,
  * more threads than a launch holds, 2^32 - 1: 2 for each query and head). */
@@ -180,8 +183,13 @@ eas_status eas_kv8_rows(const eas_kv8_cache* cache, int32_t dtype, const int32_t
  * eas_kv8_attention_workspace gives for the same arguments (0, up to a max_len
  * of 1,024: NULL is fine); calls that may overlap, captured ones included, need
  * one each.  Nothing in it has to be set before, or is kept from call to call.
+ * It grows with max_q up to 256 * heads * (head_dim + 1) * 4 bytes a sequence.
  * A sequence's result does not depend on the other sequences, on max_q, on
- * max_len or on which pages hold its tokens, to the bit. */
+ * max_len or on which pages hold its tokens, to the bit.
+ * Made for a few queries of each sequence.  From 128 on, eas_kv8_rows and
+ * eas_prompt_attention over the rows take less time: 8 sequences of 4,096 tokens,
+ * 32 heads of 128 over 8, with 64 queries each 102 us here and 105 there, with
+ * 128 289 and 146, with 512 1,836 and 277. */
 eas_status eas_kv8_attention(const eas_kv8_cache* cache, const eas_attn_shape* shape, const void* q, int32_t n_rows,
                              const int32_t* cu_q, int32_t max_q, const int32_t* lens, int32_t max_len,
                              const int32_t* pages, int32_t max_pages, int32_t n_seqs, void* out, float* lse,

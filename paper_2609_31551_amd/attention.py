@@ -172,7 +172,8 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, *, causal=True, scale=None, out=N
     head_dim] in bfloat16 or float16, any row and head strides; cu_q, cu_k: host prefix sums of the sequences'
     queries and keys (cu_k None: the same).  scale None: head_dim ** -0.5.  Returns (out, lse): out like q, in
     ``out`` where given, rows behind the last sequence untouched; lse [rows, heads] float32 with with_lse or where
-    given, else None.  workspace: a uint8 device tensor to use instead of a new one where one is needed."""
+    given, else None.  workspace: a uint8 device tensor to use instead of a new one where one is needed, for few queries
+    over 2,048 keys or more: up to 258 MiB for such a sequence with heads of 128."""
     index, dtype = _device(q), q.dtype
     code = _dtype(dtype)
     if q.dim() != 3 or k.dim() != 3:
@@ -273,7 +274,8 @@ class Kv8Cache:
     def rows(self, pages, cu_rows, n_rows, first=None, max_len=None, dtype=torch.bfloat16, k=None, v=None, stream=None):
         """Cached tokens back as rows (eas_kv8_rows): rows cu_rows[r] .. cu_rows[r+1] (int32 device [n_seqs + 1]) of
         the ``n_rows`` receive sequence r's tokens from first[r] (int32 device; None: 0) on.  max_len: the most of a
-        sequence (None: n_rows).  Returns (k, v) [n_rows, kv_heads, head_dim]; rows of no sequence are not written."""
+        sequence (None: n_rows); the launch grows with it * n_seqs.  Returns (k, v) [n_rows, kv_heads, head_dim]; rows
+        of no sequence are not written."""
         table, max_pages, n = self._table(pages)
         index, code = self._index, _dtype(dtype)
         shape = (int(n_rows), self.kv_heads, self.head_dim)
@@ -304,8 +306,10 @@ class Kv8Cache:
                   lse=None, with_lse=False, workspace=None, stream=None):
         """Attention of q [rows, heads, head_dim] over the first ``lens`` (int32 device [n_seqs]) tokens of each
         sequence, the queries' own among them (eas_kv8_attention).  cu_q, max_q: as cu_new and max_new of append;
-        max_len: the most tokens of a sequence (None: what the page table holds).  workspace: a uint8 device tensor
-        to use instead of a new one.  Returns (out, lse) as prompt_attention."""
+        max_len: the most tokens of a sequence (None: what the page table holds).  The launch and the workspace grow
+        with max_q * n_seqs and max_len, so give them where cu_q is given.  workspace: a uint8 device tensor to use
+        instead of a new one.  Returns (out, lse) as prompt_attention, which over rows() is faster from 128 queries of
+        a sequence on."""
         table, max_pages, n = self._table(pages)
         index, dtype, dim = self._index, q.dtype, self.head_dim
         code = _dtype(dtype)

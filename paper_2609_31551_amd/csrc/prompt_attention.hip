@@ -11,10 +11,11 @@
 // the MFMAs of the next tile's scores and of its own values, step by step.
 //
 // Bound by the matrix units: 4 * head_dim flops for each visible (query, key) pair.  16,484 causal tokens of 32 heads
-// of 128 take 1,912 us, 1,164 TFLOP/s; 8,192 with all keys 926 us, 1,187 (a matrix product of 8,192^3 from the library
-// reaches 1,175 here: the board's power, not the instruction's rate, is the limit; with the MFMAs and the DMA alone the
-// full 8,192 take 692 us).  Short prompts are bound by the queries' loads and the results' stores, 15 - 20% of eight
-// prompts of 97 to 2,309 tokens, which nothing of the same workgroup runs beside.
+// of 128 take 1,912 - 2,010 us from card to card, 1,107 - 1,164 TFLOP/s, the units 60% busy at 1.76 GHz; 8,192 with all
+// keys 926 - 970 (a matrix product of 8,192^3 from the library reaches 1,175: the board's power, not the instruction's
+// rate, is the limit; with the MFMAs and the DMA alone the full 8,192 take 692 us).  Eight prompts of 97 to 2,309
+// tokens, 104 - 120 us, keep them 38% busy at 2.0 GHz: the queries' loads and the results' stores, which nothing of the
+// same workgroup runs beside, and waves that wait for their workgroup's last.
 #include <type_traits>
 
 #include "attention_ops.h"
