@@ -76,6 +76,42 @@ inline eas_status check_table(const eas_kv8_cache* c, const int32_t* pages, int3
 // A grid's dimension holds less than 2^32 threads.
 inline bool fits_launch(int64_t workgroups, int threads) { return workgroups <= 0xffffffffll / threads; }
 
+// ---- sequences of the calls over a paged cache (device) ----------------------
+
+// A sequence of a call over a paged cache
+struct Seq {
+  long row0;     // row of the first query that is computed
+  int before;    // tokens before that query's own, where causal: it sees before + 1
+  int nq, len;   // queries that are computed, tokens that may be seen
+  int lq;        // its queries, computed or not
+};
+
+// A sequence's queries without those beyond max_q and those of rows outside [0, n_rows): the others keep their places.
+// Prefix sums that do not fit may wrap; what is computed lies in [0, n_rows) whatever they hold.
+template <class Args>
+__device__ __forceinline__ Seq find_seq(const Args& a, int r) {
+  Seq s;
+  unsigned lq = a.max_q;
+  s.row0 = (long)r * a.max_q;
+  if (a.cu_q) {
+    s.row0 = a.cu_q[r];
+    lq = (unsigned)a.cu_q[r + 1] - (unsigned)a.cu_q[r];
+  }
+  const int len = max(0, min(a.lens[r], a.max_pages << a.c.page_shift));
+  const int skip = (int)max(-s.row0, 0l) & 0x7fffffff;
+  s.before = (int)((unsigned)len - lq + (unsigned)skip);
+  s.row0 = max(s.row0, 0l);
+  s.nq = (int)max(min((long)(min(max((int)lq, 0), a.max_q) - skip), a.n_rows - s.row0), 0l);
+  s.len = min(len, a.max_len);
+  s.lq = max((int)lq, 0);
+  return s;
+}
+// Tokens that computed query i sees
+template <class Args>
+__device__ __forceinline__ int seen_by(const Args& a, const Seq& s, int i) {
+  return a.causal ? max(0, min(s.len, s.before + i + 1)) : s.len;
+}
+
 // ---- the cache's scales and codes (device) -----------------------------------
 
 // The cache as the kernels get it.

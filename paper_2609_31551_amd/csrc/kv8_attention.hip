@@ -77,35 +77,6 @@ struct Kv8AttnArgs {
   int max_q, most_q;    // the caller's, and a bound of the queries of a sequence that are computed
 };
 
-struct Seq {
-  long row0;     // row of the first query that is computed
-  int before;    // tokens before that query's own, where causal: it sees before + 1
-  int nq, len;   // queries that are computed, tokens that may be seen
-};
-
-// A sequence's queries without those beyond max_q and those of rows outside [0, n_rows): the others keep their places.
-// Prefix sums that do not fit may wrap; what is computed lies in [0, n_rows) whatever they hold.
-__device__ __forceinline__ Seq find_seq(const Kv8AttnArgs& a, int r) {
-  Seq s;
-  unsigned lq = a.max_q;
-  s.row0 = (long)r * a.max_q;
-  if (a.cu_q) {
-    s.row0 = a.cu_q[r];
-    lq = (unsigned)a.cu_q[r + 1] - (unsigned)a.cu_q[r];
-  }
-  const int len = max(0, min(a.lens[r], a.max_pages << a.c.page_shift));
-  const int skip = (int)max(-s.row0, 0l) & 0x7fffffff;
-  s.before = (int)((unsigned)len - lq + (unsigned)skip);
-  s.row0 = max(s.row0, 0l);
-  s.nq = (int)max(min((long)(min(max((int)lq, 0), a.max_q) - skip), a.n_rows - s.row0), 0l);
-  s.len = min(len, a.max_len);
-  return s;
-}
-// Tokens that computed query i sees
-__device__ __forceinline__ int seen_by(const Kv8AttnArgs& a, const Seq& s, int i) {
-  return a.causal ? max(0, min(s.len, s.before + i + 1)) : s.len;
-}
-
 // 16 codes to fp16, exactly: int8 by building 1024 + (code + 128) and taking 1152 off
 template <int FORMAT>
 __device__ __forceinline__ void codes_to_f16(const uint4& w, f16x8* lo, f16x8* hi) {
