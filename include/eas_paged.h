@@ -131,8 +131,8 @@ eas_status eas_kv16_attention(const eas_kv16_cache* cache, const eas_attn_shape*
                               void* workspace, int64_t workspace_bytes, void* stream);
 
 /* Workspace bytes of eas_kv16_attention (host only, no HIP calls). */
-eas_status eas_kv16_attention_workspace(const eas_attn_shape* shape, int32_t max_q, int32_t max_len, int32_t n_seqs,
-                                        int64_t* bytes);
+eas_status eas_kv16_attention_workspace(const eas_attn_shape* shape, int32_t n_rows, int32_t max_q, int32_t max_len,
+                                        int32_t n_seqs, int64_t* bytes);
 
 #ifdef __cplusplus
 }

@@ -17,42 +17,7 @@ namespace {
 constexpr int TILE = 32;         // tokens per wave and step
 constexpr int NW = 4;            // waves per workgroup
 constexpr int ROWS = 16;         // of a workgroup
-constexpr int MAX_RUNS = 64;     // runs per sequence
-constexpr int RUN_ROWS = 256;    // runs * queries of a sequence that is split
-constexpr int SHORTEST_RUN = 1024;
-
-// Runs that `len` tokens are split into for nq queries, and a run's tokens
-__host__ __device__ inline int n_runs(int len, int nq) {
-  const int by_len = (int)(((unsigned)len + SHORTEST_RUN - 1) / SHORTEST_RUN);   // len <= 2^30: 32 bits hold all sums here
-  int most = nq > 0 ? RUN_ROWS / nq : 1;
-  most = most < 1 ? 1 : most > MAX_RUNS ? MAX_RUNS : most;
-  return by_len < 1 ? 1 : by_len < most ? by_len : most;
-}
-__host__ __device__ inline int run_tokens(int len, int runs) {
-  const unsigned all = (unsigned)runs * (NW * TILE);
-  return (int)(((unsigned)len + all - 1) / all) * (NW * TILE);
-}
-// Workspace slots of a sequence: at least n_runs * nq * heads for every nq <= max_q, len <= max_len of one that is split
-inline int64_t slots(int max_q, int max_len, int heads) {
-  const int64_t rows = (int64_t)n_runs(max_len, 1) * max_q;
-  return heads * (rows < RUN_ROWS ? rows : RUN_ROWS);
-}
-
-struct Kv16AttnArgs {
-  Kv16Args c;
-  const void* q;
-  void* out;
-  float* lse;
-  eas_strides qs, os;
-  const int* cu_q;
-  const int* lens;
-  const int* pages;
-  float* part;          // [n_seqs, slots, D] results of runs, a sequence's as [run, head, query]
-  float* part_lse;      // [n_seqs, slots] their log2 sums
-  float scale_log2;     // scale * log2(e)
-  int heads, causal, n_rows, max_len, max_pages, n_seqs, slots, row_tiles, runs;
-  int max_q, most_q;    // the caller's, and a bound of the queries of a sequence that are computed
-};
+static_assert(FEW_STEP == NW * TILE);
 
 template <class T>
 struct Mfma16;
@@ -90,15 +55,15 @@ __global__ __launch_bounds__(64 * NW) void kv16_tokens_kernel(Kv16AttnArgs a) {
   unsigned b = blockIdx.x;
   const int rt = b % (unsigned)a.row_tiles;
   b /= (unsigned)a.row_tiles;
-  const int run = b % (unsigned)a.runs;
-  b /= (unsigned)a.runs;
+  const int run = b % (unsigned)a.most_runs;
+  b /= (unsigned)a.most_runs;
   const int kvh = b % (unsigned)a.c.kv_heads, r = b / (unsigned)a.c.kv_heads;
   const Seq s = find_seq(a, r);
   const int group = a.heads / a.c.kv_heads;
-  if ((long)rt * ROWS >= (long)s.nq * group) return;
-  const int runs = n_runs(s.len, s.nq);
+  if (!takes_few(a, s) || rt * ROWS >= s.nq * group) return;
+  const int runs = few_runs(s.len, s.nq, a.heads, a.c.kv_heads);
   if (run >= runs) return;
-  const int each = run_tokens(s.len, runs);
+  const int each = few_run_tokens(s.len, runs);
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
@@ -116,14 +81,12 @@ __global__ __launch_bounds__(64 * NW) void kv16_tokens_kernel(Kv16AttnArgs a) {
   const long t_begin = (long)run * each;
   const int t_end = (int)min((long)most, t_begin + each);
   const int* table = a.pages + (long)r * a.max_pages;
-  const int page_mask = (1 << a.c.page_shift) - 1;
-  const auto held = [&](int page) { return page >= 0 && page < a.c.n_pages; };
   // offset of a token's head in the cache, of tokens behind the last that of the last; *there: its page is held
   const auto place = [&](int t, bool* there) {
     t = min(t, t_end - 1);
     const int page = table[t >> a.c.page_shift];
-    *there = held(page);
-    return ((((long)(*there ? page : 0) * a.c.kv_heads + kvh) << a.c.page_shift) + (t & page_mask)) * D;
+    *there = held_page(a, page);
+    return token_offset(a, page, kvh, t, D);
   };
   const T* keys = static_cast<const T*>(a.c.k);
   const T* values = static_cast<const T*>(a.c.v);
@@ -239,7 +202,7 @@ __global__ __launch_bounds__(64 * NW) void kv16_tokens_kernel(Kv16AttnArgs a) {
       *reinterpret_cast<Tx4*>(static_cast<T*>(a.out) + orow * a.os.row + h * a.os.head + d) = y;
       if (d == 0 && a.lse) a.lse[orow * a.heads + h] = lse2 * kLn2;
     } else {
-      const long slot = (long)r * a.slots + ((long)run * a.heads + h) * s.nq + query;
+      const long slot = first_slot(a, s, r) + ((long)run * a.c.kv_heads + kvh) * s.nq * group + rr;
       *reinterpret_cast<f32x4*>(a.part + slot * D + d) = sum * inv;
       if (d == 0) a.part_lse[slot] = lse2;
     }
@@ -248,18 +211,20 @@ __global__ __launch_bounds__(64 * NW) void kv16_tokens_kernel(Kv16AttnArgs a) {
 
 // Joins the runs of the sequences that were split, in order: D / 4 threads for each row.
 template <class T, int D>
-__global__ __launch_bounds__(256) void kv16_join_kernel(Kv16AttnArgs a) {
+__global__ __launch_bounds__(256) void kv16_join_kernel(Kv16AttnArgs a, int join_q) {
   constexpr int EACH = 256 / (D / 4);
-  const unsigned row = blockIdx.x * EACH + threadIdx.x / (D / 4);   // (sequence, head, query), below 2^31
+  const unsigned row = blockIdx.x * EACH + threadIdx.x / (D / 4);   // (sequence, query, head), below 2^31
   const int d = threadIdx.x % (D / 4) * 4;
-  const int i = row % (unsigned)a.most_q, h = row / (unsigned)a.most_q % (unsigned)a.heads;
-  const int r = row / (unsigned)a.most_q / (unsigned)a.heads;
+  const int h = row % (unsigned)a.heads, i = row / (unsigned)a.heads % (unsigned)join_q;
+  const int r = row / (unsigned)a.heads / (unsigned)join_q;
   if (r >= a.n_seqs) return;
   const Seq s = find_seq(a, r);
   if (i >= s.nq) return;
-  const int runs = n_runs(s.len, s.nq);
+  const int runs = runs_of(a, s);
   if (runs == 1) return;
-  const long slot = (long)r * a.slots + (long)h * s.nq + i, step = (long)a.heads * s.nq;   // of run 0, and from run to run
+  const int group = a.heads / a.c.kv_heads, kvh = h / group;
+  const long rows = (long)s.nq * group, step = rows * a.c.kv_heads;   // from run to run
+  const long slot = first_slot(a, s, r) + kvh * rows + (long)i * group + (h - kvh * group);
   float M = -INFINITY;
   for (int k = 0; k < runs; ++k) M = fmaxf(M, a.part_lse[slot + k * step]);
   const float base = M == -INFINITY ? 0.0f : M;
@@ -282,22 +247,51 @@ __global__ __launch_bounds__(256) void kv16_join_kernel(Kv16AttnArgs a) {
   if (d == 0 && a.lse) a.lse[(s.row0 + i) * a.heads + h] = W == 0.0f ? -INFINITY : (M + __log2f(W)) * kLn2;
 }
 
+// The most runs of a sequence within the bounds, and the slots of one that is split: runs * queries * heads.
+int most_runs(int max_q, int max_len, int heads, int kv_heads) {
+  const int group = heads / kv_heads, few = few_runs(max_len, 1, heads, kv_heads);
+  if (few_rows(max_q, group)) return few;
+  const int many = many_runs(max_len, 1, kv_heads);   // fewer rows, more runs
+  return many > few ? many : few;
+}
+// Of sequences that are split, the most queries
+int64_t split_queries(int max_q, int heads) {
+  const int64_t many = MANY_ALONE * 128 / heads, few = FEW_ROWS, most = many > few ? many : few;
+  return max_q < most ? max_q : most;
+}
+int64_t seq_slots(int max_q, int max_len, int heads, int kv_heads) {
+  return split_queries(max_q, heads) * heads * most_runs(max_q, max_len, heads, kv_heads);
+}
+// Slots of a call: for each sequence, or for each row, whichever are fewer
+int64_t all_slots(int64_t n_rows, int64_t n_seqs, int64_t each, int heads, int runs) {
+  const int64_t by_row = n_rows * heads * runs;
+  return n_seqs > by_row / each || n_seqs * each >= by_row ? by_row : n_seqs * each;
+}
+
 template <class T, int D>
-eas_status launch(Kv16AttnArgs& a, int64_t rows, bool join, hipStream_t s) {
-  const int64_t tiles = (rows + ROWS - 1) / ROWS;
-  const int64_t pairs = (int64_t)a.n_seqs * a.c.kv_heads, joined = (int64_t)a.n_seqs * a.most_q;
+eas_status launch(Kv16AttnArgs& a, hipStream_t s) {
+  const int group = a.heads / a.c.kv_heads;
+  const int64_t pairs = (int64_t)a.n_seqs * a.c.kv_heads;
+  const bool many = !few_rows(a.most_q, group), few = a.cu_q || !many;
+  const int64_t rows = (int64_t)a.most_q * group, tiles = ((rows < FEW_ROWS ? rows : FEW_ROWS) + ROWS - 1) / ROWS;
   constexpr int each = 256 / (D / 4);
-  if (pairs > 0x7fffffff || !fits_launch(tiles * a.runs, 64 * NW) || !fits_launch(tiles * a.runs * pairs, 64 * NW))
+  const int64_t join_q = split_queries(a.most_q, a.heads), joined = a.n_seqs * join_q;
+  if (pairs > 0x7fffffff || (few && !fits_launch(tiles * a.most_runs * pairs, 64 * NW))) return EAS_ERR_UNSUPPORTED;
+  if (a.most_runs > 1 && (joined * a.heads > 0x7fffffff || !fits_launch((joined * a.heads + each - 1) / each, 256)))
     return EAS_ERR_UNSUPPORTED;
-  if (join && (joined * a.heads > 0x7fffffff || !fits_launch((joined * a.heads + each - 1) / each, 256)))
-    return EAS_ERR_UNSUPPORTED;
-  const int64_t blocks = tiles * a.runs * pairs;
-  a.row_tiles = (int)tiles;
-  hipLaunchKernelGGL((kv16_tokens_kernel<T, D>), dim3((unsigned)blocks), dim3(64 * NW), 0, s, a);
-  if (hipGetLastError() != hipSuccess) return EAS_ERR_HIP;
-  if (!join) return EAS_OK;
-  hipLaunchKernelGGL((kv16_join_kernel<T, D>), dim3((unsigned)((joined * a.heads + each - 1) / each)),
-                     dim3(256), 0, s, a);
+  if (many) {
+    const eas_status st = launch_kv16_many(a, std::is_same_v<T, bf16> ? EAS_BF16 : EAS_FP16, D, s);
+    if (st != EAS_OK) return st;
+  }
+  if (few) {
+    a.row_tiles = (int)tiles;
+    const int64_t blocks = tiles * a.most_runs * pairs;
+    hipLaunchKernelGGL((kv16_tokens_kernel<T, D>), dim3((unsigned)blocks), dim3(64 * NW), 0, s, a);
+    if (hipGetLastError() != hipSuccess) return EAS_ERR_HIP;
+  }
+  if (a.most_runs == 1) return EAS_OK;
+  hipLaunchKernelGGL((kv16_join_kernel<T, D>), dim3((unsigned)((joined * a.heads + each - 1) / each)), dim3(256), 0, s, a,
+                     (int)join_q);
   return hipGetLastError() == hipSuccess ? EAS_OK : EAS_ERR_HIP;
 }
 
@@ -306,12 +300,17 @@ eas_status launch(Kv16AttnArgs& a, int64_t rows, bool join, hipStream_t s) {
 
 using namespace eas;
 
-extern "C" eas_status eas_kv16_attention_workspace(const eas_attn_shape* shape, int32_t max_q, int32_t max_len,
-                                                   int32_t n_seqs, int64_t* bytes) {
+extern "C" eas_status eas_kv16_attention_workspace(const eas_attn_shape* shape, int32_t n_rows, int32_t max_q,
+                                                   int32_t max_len, int32_t n_seqs, int64_t* bytes) {
   const eas_status st = check_shape(shape);
   if (st != EAS_OK) return st;
-  if (max_q < 0 || max_len < 0 || n_seqs < 0 || !bytes) return EAS_ERR_INVALID_ARG;
-  *bytes = n_runs(max_len, 1) == 1 ? 0 : n_seqs * slots(max_q, max_len, shape->heads) * (shape->head_dim + 1) * 4;
+  if (n_rows < 0 || max_q < 0 || max_len < 0 || n_seqs < 0 || !bytes) return EAS_ERR_INVALID_ARG;
+  const int most_q = max_q < n_rows ? max_q : n_rows;
+  const int runs = most_runs(most_q, max_len, shape->heads, shape->kv_heads);
+  *bytes = 0;
+  if (runs == 1 || most_q == 0 || n_seqs == 0) return EAS_OK;
+  *bytes = all_slots(n_rows, n_seqs, seq_slots(most_q, max_len, shape->heads, shape->kv_heads), shape->heads, runs) *
+           (shape->head_dim + 1) * 4;
   return EAS_OK;
 }
 
@@ -346,19 +345,18 @@ extern "C" eas_status eas_kv16_attention(const eas_kv16_cache* cache, const eas_
   a.max_pages = max_pages, a.n_seqs = n_seqs;
   const int64_t there = (int64_t)max_pages * cache->page_tokens;
   a.max_len = max_len < there ? max_len : (int)there;
-  a.runs = n_runs(a.max_len, 1);
-  const bool join = a.runs > 1;
-  a.slots = (int)slots(a.most_q, a.max_len, a.heads);
-  if (join) {
-    const int64_t parts = (int64_t)n_seqs * a.slots;
+  a.most_runs = most_runs(a.most_q, a.max_len, a.heads, a.c.kv_heads);
+  if (a.most_runs > 1) {
+    a.slots = seq_slots(a.most_q, a.max_len, a.heads, a.c.kv_heads);
+    const int64_t slots = all_slots(n_rows, n_seqs, a.slots, a.heads, a.most_runs);
+    if (slots < (int64_t)n_seqs * a.slots) a.slots = 0;
     if (!workspace || !aligned16(workspace)) return EAS_ERR_INVALID_ARG;
-    if (workspace_bytes < parts * (shape->head_dim + 1) * 4) return EAS_ERR_CAPACITY;
+    if (workspace_bytes / ((shape->head_dim + 1) * 4) < slots) return EAS_ERR_CAPACITY;
     a.part = static_cast<float*>(workspace);
-    a.part_lse = a.part + parts * shape->head_dim;
+    a.part_lse = a.part + slots * shape->head_dim;
   }
-  const int64_t rows = (int64_t)a.most_q * (a.heads / a.c.kv_heads);
 #define EAS_KV16_CASE(DT, T, D) \
-  if (shape->dtype == DT && shape->head_dim == D) return launch<T, D>(a, rows, join, (hipStream_t)stream)
+  if (shape->dtype == DT && shape->head_dim == D) return launch<T, D>(a, (hipStream_t)stream)
   EAS_KV16_CASE(EAS_BF16, bf16, 64);
   EAS_KV16_CASE(EAS_BF16, bf16, 128);
   EAS_KV16_CASE(EAS_FP16, f16, 64);

@@ -1,0 +1,247 @@
+// Attention of chunks of new tokens over the paged 16-bit cache (include/eas_paged.h): sequences with many rows, a row
+// being one query of one head.
+//
+// A workgroup owns 128 or 256 rows of one (sequence, key / value head), a wave 32 of them: queries and the heads of
+// their group side by side, so that a chunk of few tokens fills a wave, and tokens that stand in LDS serve the whole
+// group.  The walk over the tokens is prompt attention's (attention_tiles.h); what differs is where a tile comes from:
+// its 64 tokens lie in one to four pages.  A DMA instruction moves 4 or 8 tokens, which no page's border parts, so its
+// page is one scalar; the page numbers of a tile are one load, a tile ahead of the DMA that goes by them.  Tiles of pages
+// that are not held are masked like tokens behind a query's own (their DMA reads page 0).
+#include "attention_tiles.h"
+#include "paged_ops.h"
+
+namespace eas {
+namespace {
+
+// The sequence and its item of the launch's `item`th: row tiles and runs of all sequences with many rows, in order.
+// Each wave goes over the sequences by itself, 64 at a time.  False where there is none.
+template <int QT>
+__device__ __forceinline__ bool find_item(const Kv16AttnArgs& a, int* item, int* r) {
+  const int lane = threadIdx.x & 63, group = a.heads / a.c.kv_heads;
+  for (int first = 0; first < a.n_seqs; first += 64) {
+    int own = 0;
+    if (first + lane < a.n_seqs) {
+      const Seq s = find_seq(a, first + lane);
+      if (!takes_few(a, s)) {
+        const long rows = (long)s.nq * group;
+        own = (int)((rows + QT - 1) / QT) * many_runs(s.len, rows, a.c.kv_heads);
+      }
+    }
+    int upto = own;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int x = __shfl_up(upto, o, 64);
+      upto += lane >= o ? x : 0;
+    }
+    const unsigned long long behind = __ballot(upto > *item);
+    if (behind) {
+      const int at = __ffsll(behind) - 1;
+      *item -= __builtin_amdgcn_readlane(upto - own, at);
+      *r = first + at;
+      return true;
+    }
+    *item -= __builtin_amdgcn_readlane(upto, 63);
+  }
+  return false;
+}
+
+template <class T, int HD, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void kv16_chunks_kernel(Kv16AttnArgs a) {
+  using C = Cfg<HD, NW>;
+  typedef typename Mfma<T>::x8 x8;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];   // keys x 2, values x 2
+  const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) char*)smem;
+
+  int kvh, item, r;
+  place(a.c.kv_heads, a.c.kv_heads, &kvh, &item);
+  if (item >= a.items || !find_item<C::QT>(a, &item, &r)) return;
+  item = __builtin_amdgcn_readfirstlane(item), r = __builtin_amdgcn_readfirstlane(r);
+  const Seq s = find_seq(a, r);
+  const int group = a.heads / a.c.kv_heads, rows = s.nq * group;
+  const int runs = many_runs(s.len, rows, a.c.kv_heads), run = item % runs;
+  const int tile = (rows + C::QT - 1) / C::QT - 1 - item / runs;   // the last rows, which see most, first
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, l32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rw = tile * C::QT + wave * 32;
+
+  // this lane's row, and tokens that rows see: the lane's, the wave's fewest and most, the workgroup's most
+  const auto query = [&](int row) { return (int)((unsigned)min(row, rows - 1) / (unsigned)group); };
+  const auto head_of = [&](int row, int i) { return kvh * group + min(row, rows - 1) - i * group; };
+  const int sees = seen_by(a, s, query(rw + l32)), fewest = seen_by(a, s, query(rw)), most = rw < rows ? seen_by(a, s, query(rw + 31)) : 0;
+  // token tiles of the workgroup, from tb on those of the run, and of these the wave's
+  const int all = (seen_by(a, s, query((tile + 1) * C::QT - 1)) + KT - 1) / KT, each = many_run_tiles(s.len, runs);
+  const int tb = run * each;
+  const int nt = max(0, min(each, all - tb)), nt_w = max(0, min(nt, (most + KT - 1) / KT - tb));
+
+  x8 qf[C::KS];
+  {
+    const int i = query(rw + l32);
+    const T* qp = static_cast<const T*>(a.q) + (s.row0 + i) * a.qs.row + head_of(rw + l32, i) * a.qs.head;
+#pragma unroll
+    for (int ks = 0; ks < C::KS; ++ks) qf[ks] = *reinterpret_cast<const x8*>(qp + ks * 16 + g * 8);
+  }
+
+  // A tile's DMA: instruction n = wave + NW j fills LDS slots 64 n + lane; slot i is chunk i % R of row i / R
+  constexpr int ROWS = 64 / C::R;   // of an instruction
+  const int lrow = lane / C::R;
+  const int dcol = C::logical(wave * ROWS + lrow, lane % C::R) * 16;   // the same for all j: a row's place goes by row % 16
+  const int last = s.len - 1;
+  const int* table = a.pages + (long)r * a.max_pages;
+  // in lane p (of every four), the page of tokens 16 p .. of tile t; behind the last token, the last one's
+  const auto pages_of = [&](int t) { return table[min((tb + t) * KT + 16 * (lane & 3), last) >> a.c.page_shift]; };
+  const auto held_parts = [&](int pages) { return (int)(__ballot(held_page(a, pages)) & 15); };
+  const auto fetch = [&](const void* base, int t, int pages, int lds_off) {
+#pragma unroll
+    for (int j = 0; j < C::NDMA; ++j) {
+      const int n = wave + NW * j, row = n * ROWS, first = min((tb + t) * KT + row, last);
+      const long at = token_offset(a, __builtin_amdgcn_readlane(pages, row / 16), kvh, first, HD);
+      // rows behind the last token read it again
+      dma16(lds0 + lds_off + n * 1024, (unsigned)min(lrow, last - first) * (HD * 2) + dcol, static_cast<const T*>(base) + at);
+    }
+  };
+  const auto fetch_k = [&](int t, int pages) { fetch(a.c.k, t, pages, (t & 1) * C::TILE); };
+  const auto fetch_v = [&](int t, int pages) { fetch(a.c.v, t, pages, (2 + (t & 1)) * C::TILE); };
+
+  TileWalk<T, HD, NW> walk(smem, qf, a.scale_log2);
+  constexpr std::integral_constant<bool, true> yes{};
+  constexpr std::integral_constant<bool, false> no{};
+  // Waits until the wave's own DMA has landed and its LDS reads are done, and for the other waves to be as far.  One
+  // asm: no read may move up between the wait and the barrier.  Every wave passes it once a tile, from whichever of
+  // the loops below it is in.
+  const auto meet = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+  int pages_v = 0, pages_k = 0;        // of tiles t + 1 and t + 2
+  int parts = 0, parts1 = 0, parts2 = 0;   // which of the parts of tiles t, t + 1 and t + 2 are held
+  const auto arrive = [&](int t) {
+    meet();   // keys t + 1 and values t are there, keys t and values t - 1 read by all
+    if (t + 2 < nt) fetch_k(t + 2, pages_k);
+    if (t + 1 < nt) fetch_v(t + 1, pages_v);
+    parts = parts1, parts1 = parts2, parts2 = held_parts(pages_k);
+    pages_v = pages_k;
+    pages_k = pages_of(t + 3);
+  };
+  const auto hidden = [&](int t) {   // of tile t's weights
+    int upto[4];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) upto[p] = (parts >> p & 1 ? sees : 0) - (tb + t) * KT;
+    return [=](int v) { return key_of(v, g) >= upto[(v >> 4) * 2 + (v & 15) / 8]; };
+  };
+  if (nt > 0) {
+    f32x16 sa[2], sb[2];
+    const int pages0 = pages_of(0);
+    pages_v = pages_of(1), pages_k = pages_of(2);
+    parts1 = held_parts(pages0), parts2 = held_parts(pages_v);   // of tiles 0 and 1
+    fetch_k(0, pages0);
+    fetch_v(0, pages0);
+    if (nt > 1) fetch_k(1, pages_v);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    // the queries are taken here, so that no wait for them is left to the loop, where it would wait for a tile
+#pragma unroll
+    for (int ks = 0; ks < C::KS; ++ks) asm volatile("" ::"v"(qf[ks]));
+    meet();
+    int t = 0;
+    if (nt_w > 0) {
+      walk.scores(0, sa);
+      // tiles that all the wave's queries see whole, in pairs, up to a page that is not held; those at the border, or
+      // from that page on; the last one
+      for (const int whole = min(fewest / KT - tb, nt_w - 1); t + 2 <= whole && (parts1 & parts2) == 15; t += 2) {
+        arrive(t);
+        walk.step(t, sa, sb, hidden(t), no, yes);
+        arrive(t + 1);
+        walk.step(t + 1, sb, sa, hidden(t + 1), no, yes);
+      }
+      for (; t + 1 < nt_w; ++t) {
+        arrive(t);
+        walk.step(t, sa, sb, hidden(t), yes, yes);
+        sa[0] = sb[0];
+        sa[1] = sb[1];
+      }
+      arrive(t);
+      walk.step(t, sa, sb, hidden(t), yes, no);
+      ++t;
+    }
+    for (; t < nt; ++t) arrive(t);
+  }
+
+  // every wave is past its last read
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __syncthreads();
+  int row0 = rw;
+  asm("" : "+s"(row0));   // rows' queries and heads are taken anew: no register holds them over the walk
+  if (row0 >= rows) return;
+  const int ri = row0 + l32, qi = query(ri);
+  char* stage = smem + wave * 32 * HD * 2;
+  f32x16* o = walk.o;
+  float m = walk.m, l = walk.l;
+  if (any_not_finite<C::HB>(o)) {
+    const auto page_of = [&](int i) { return table[i >> a.c.page_shift]; };
+    careful_rows<T, HD>(
+        qf, [&](long i) { return static_cast<const T*>(a.c.k) + token_offset(a, page_of((int)i), kvh, (int)i, HD); },
+        [&](long i) { return static_cast<const T*>(a.c.v) + token_offset(a, page_of((int)i), kvh, (int)i, HD); },
+        [&](int i) { return i >= sees || !held_page(a, page_of(i)); },
+        [&](int t) {
+          bool whole = (t + 1) * KT <= fewest;
+          for (int p = 0; p < 4; ++p) whole = whole && held_page(a, page_of(t * KT + 16 * p));
+          return whole;
+        },
+        s.len, tb, tb + nt_w, a.scale_log2, stage, o, &m, &l);
+  }
+  l += __shfl_xor(l, 32, 64);
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l, lse2 = l == 0.0f ? -INFINITY : m + __log2f(l);
+  if (runs > 1) {
+    const long slot = first_slot(a, s, r) + ((long)run * a.c.kv_heads + kvh) * rows + ri;   // a wave's are consecutive
+    if (ri < rows) {
+#pragma unroll
+      for (int hb = 0; hb < C::HB; ++hb)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4)
+          *reinterpret_cast<float4*>(a.part + slot * HD + hb * 32 + e * 2 + g * 4) =
+              make_float4(o[hb][e] * inv, o[hb][e + 1] * inv, o[hb][e + 2] * inv, o[hb][e + 3] * inv);
+      if (g == 0) a.part_lse[slot] = lse2;
+    }
+    return;
+  }
+  if (a.lse && g == 0 && ri < rows) a.lse[(s.row0 + qi) * a.heads + head_of(ri, qi)] = lse2 * kLn2;
+  // the tiles' memory stages each wave's 32 x HD results, chunks of row r rotated by r, so that the stores are of
+  // whole rows
+#pragma unroll
+  for (int hb = 0; hb < C::HB; ++hb)
+#pragma unroll
+    for (int e4 = 0; e4 < 4; ++e4) {
+      union { uint2 u; T e[4]; } st;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) st.e[e] = (T)(o[hb][e4 * 4 + e] * inv);
+      *reinterpret_cast<uint2*>(stage + l32 * HD * 2 + (hb * 4 + e4 + l32) % C::R * 16 + g * 8) = st.u;
+    }
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+  for (int k = 0; k < C::R / 2; ++k) {
+    const int c = lane + 64 * k, row = c / C::R, ch = c % C::R, i = query(row0 + row);
+    const uint4 x = *reinterpret_cast<const uint4*>(stage + row * HD * 2 + (ch + row) % C::R * 16);
+    if (row0 + row < rows)
+      *reinterpret_cast<uint4*>(static_cast<T*>(a.out) + (s.row0 + i) * a.os.row + head_of(row0 + row, i) * a.os.head +
+                                ch * 8) = x;
+  }
+}
+
+template <class T, int HD, int NW>
+eas_status launch(Kv16AttnArgs a, hipStream_t s) {
+  using C = Cfg<HD, NW>;
+  const int group = a.heads / a.c.kv_heads;
+  // row tiles of all sequences, and their runs: of each either by its length's bound or what is split at most
+  const int64_t tiles = ((int64_t)a.n_rows * group + C::QT - 1) / C::QT + (a.n_seqs < a.n_rows ? a.n_seqs : a.n_rows);
+  const int runs = many_runs(a.max_len, 1, a.c.kv_heads);
+  const int64_t items = tiles * runs, blocks = tile_workgroups(items, a.c.kv_heads, a.c.kv_heads);
+  if (items > 0x7fffffff || !fits_launch(blocks, 64 * NW)) return EAS_ERR_UNSUPPORTED;
+  a.items = (int)items;
+  hipLaunchKernelGGL((kv16_chunks_kernel<T, HD, NW>), dim3((unsigned)blocks), dim3(64 * NW), 4 * C::TILE, s, a);
+  return hipGetLastError() == hipSuccess ? EAS_OK : EAS_ERR_HIP;
+}
+
+}  // namespace
+
+eas_status launch_kv16_many(const Kv16AttnArgs& a, int32_t dtype, int dim, hipStream_t s) {
+  if (dtype == EAS_BF16) return dim == 128 ? launch<bf16, 128, 4>(a, s) : launch<bf16, 64, 4>(a, s);
+  return dim == 128 ? launch<f16, 128, 4>(a, s) : launch<f16, 64, 4>(a, s);
+}
+
+}  // namespace eas

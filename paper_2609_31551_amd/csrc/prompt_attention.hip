@@ -16,14 +16,11 @@
 // rate, is the limit; with the MFMAs and the DMA alone the full 8,192 take 692 us).  Eight prompts of 97 to 2,309
 // tokens, 104 - 120 us, keep them 38% busy at 2.0 GHz: the queries' loads and the results' stores, which nothing of the
 // same workgroup runs beside, and waves that wait for their workgroup's last.
-#include <type_traits>
-
-#include "attention_ops.h"
+#include "attention_tiles.h"
 
 namespace eas {
 namespace {
 
-constexpr int KT = 64;               // keys per tile
 constexpr int kMaxRows = 1 << 30;    // queries or keys of a call
 constexpr int MAX_RUNS = 16;         // runs that a sequence's keys are split into
 
@@ -71,177 +68,6 @@ struct PromptArgs {
   float* part_lse;   // and their softmax's log2 sums [slots]
 };
 
-template <class T>
-struct Mfma;
-template <>
-struct Mfma<bf16> {
-  typedef bf16x8 x8;
-  __device__ static f32x16 go(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-};
-template <>
-struct Mfma<f16> {
-  typedef f16x8 x8;
-  __device__ static f32x16 go(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
-};
-
-// Key of a wave's weight v (of 32) in a tile; the other lane of the query, g ^ 1, has the others
-__device__ __forceinline__ int key_of(int v, int g) { return (v >> 4) * 32 + (v & 15) / 4 * 8 + g * 4 + (v & 3); }
-
-// The wave's queries over key tiles from .. to again, into O, m and l, in the layout that the loop leaves them in; no
-// value reaches a query that does not see it.  Only for results that the loop, in which a hidden value is multiplied by
-// a weight of 0, leaves infinite or NaN.  Tiles that all the wave's queries see whole go through the matrix units,
-// straight from memory; at the border values are taken key by key, by the queries that see them, the weights from
-// `stage`, 4 KB of LDS for each wave.  4,096 tokens of 8 heads that all come this way take 0.49 ms, without a NaN 0.084.
-template <class T, int HD, class X8>
-__device__ __forceinline__ void careful_rows(const X8* qf, const T* kp, long k_row, const T* vp, long v_row, int lk,
-                                             int from, int to, int fewest, int sees, float scale_log2, char* stage,
-                                             f32x16* o, float* m_out, float* l_out) {
-  constexpr int KS = HD / 16, HB = HD / 32;
-  constexpr float TOP = std::is_same_v<T, f16> ? 15.0f : 0.0f;   // log2 of the largest weight, as in the loop
-  typedef T Tx4 __attribute__((ext_vector_type(4)));
-  const int lane = threadIdx.x & 63, g = lane >> 5, l32 = lane & 31;
-  const f32x16 zero = {};
-  float m = -INFINITY, l = 0.0f;
-#pragma unroll
-  for (int hb = 0; hb < HB; ++hb) o[hb] = zero;
-  for (int t = from; t < to; ++t) {
-    const int k0 = t * KT;
-    f32x16 s[2] = {zero, zero};
-#pragma unroll
-    for (int i = 0; i < 2 * KS; ++i) {
-      const long row = min(k0 + 32 * (i & 1) + l32, lk - 1);
-      s[i & 1] = Mfma<T>::go(*reinterpret_cast<const X8*>(kp + row * k_row + (i >> 1) * 16 + g * 8), qf[i >> 1], s[i & 1]);
-    }
-    float top = -INFINITY;
-#pragma unroll
-    for (int v = 0; v < 32; ++v) {
-      float x = s[v >> 4][v & 15] * scale_log2;
-      if (k0 + key_of(v, g) >= sees) x = -INFINITY;
-      top = fmaxf(top, x);
-      s[v >> 4][v & 15] = x;
-    }
-    top = fmaxf(m, fmaxf(top, __shfl_xor(top, 32, 64)));
-    const float base = top == -INFINITY ? 0.0f : top, alpha = __builtin_amdgcn_exp2f(m - base);
-    m = top;
-    l *= alpha;
-#pragma unroll
-    for (int hb = 0; hb < HB; ++hb) o[hb] *= alpha;
-#pragma unroll
-    for (int v = 0; v < 32; ++v) {
-      const float p = __builtin_amdgcn_exp2f(s[v >> 4][v & 15] - base + TOP);
-      l += p;
-      s[v >> 4][v & 15] = p;
-    }
-    if (k0 + KT <= fewest) {
-#pragma unroll 1
-      for (int c = 0; c < 4; ++c) {   // 16 keys
-        X8 p;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = (T)(c == 0 ? s[0][e] : c == 1 ? s[0][8 + e] : c == 2 ? s[1][e] : s[1][8 + e]);
-#pragma unroll
-        for (int hb = 0; hb < HB; ++hb) {
-          X8 v;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = vp[(k0 + key_of(8 * c + e, g)) * v_row + hb * 32 + l32];
-          o[hb] = Mfma<T>::go(v, p, o[hb]);
-        }
-      }
-    } else {
-      float* w = reinterpret_cast<float*>(stage) + l32 * 32;   // of 32 keys
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-#pragma unroll
-        for (int v = 0; v < 16; ++v) w[key_of(v, g)] = s[kb][v];
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-#pragma unroll 1
-        for (int i = 0; i < 32; ++i) {
-          const int key = k0 + kb * 32 + i;
-          if (key < sees) {
-            const float p = w[i];
-#pragma unroll
-            for (int hb = 0; hb < HB; ++hb)
-#pragma unroll
-              for (int e4 = 0; e4 < 4; ++e4) {
-                const Tx4 x = *reinterpret_cast<const Tx4*>(vp + key * v_row + hb * 32 + e4 * 8 + g * 4);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[hb][e4 * 4 + e] = fmaf(p, (float)x[e], o[hb][e4 * 4 + e]);
-              }
-          }
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      }
-    }
-  }
-  *m_out = m - TOP;
-  *l_out = l;
-}
-
-// Whether any of n floats is infinite or NaN in any lane
-template <int N>
-__device__ __forceinline__ bool any_not_finite(const f32x16* o) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < N; ++i)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) top = max(top, __float_as_uint(o[i][e]) & 0x7fffffffu);
-  return __any(top >= 0x7f800000u);
-}
-
-#pragma clang diagnostic ignored "-Winline-asm"
-// 64 lanes' 16-byte pieces at base + voff, to 1 KB of LDS in lane order
-__device__ __forceinline__ void dma16(unsigned lds_addr, unsigned voff, const void* base) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n"
-               :: "s"(lds_addr), "v"(voff), "s"(base) : "memory", "m0");
-}
-
-typedef short v4i16 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
-
-template <int HD, int NW_>
-struct Cfg {
-  static constexpr int NW = NW_;                 // waves per workgroup, 32 queries each
-  static constexpr int QT = 32 * NW;             // queries per workgroup
-  static constexpr int R = HD / 8;               // 16-byte chunks per row
-  static constexpr int KS = HD / 16;             // 16-wide steps of q . k
-  static constexpr int HB = HD / 32;             // 32-row blocks of O^T
-  static constexpr int TILE = KT * HD * 2;       // bytes of a key or value tile
-  static constexpr int NDMA = TILE / 1024 / NW;  // DMA instructions per wave and tile
-  // Chunk L of a tile's row is stored at chunk (L + rot) % R.  A key read takes one chunk of 16 consecutive
-  // rows at a time, a transposing value read 64 bytes of 4 consecutive rows: both hit all banks once.
-  __device__ static int rot(int row) {
-    return R == 16 ? 4 * (row & 3) + ((row >> 2) & 3) : 2 * (row & 3) + ((row >> 2) & 1);
-  }
-  __device__ static int phys(int row, int L) { return (L + rot(row)) % R; }
-  __device__ static int logical(int row, int p) { return (p + R - rot(row)) % R; }
-};
-
-// The head and query tile of a workgroup.  Workgroups go to the 8 XCDs in turn, each with an L2 of its own, so the
-// query heads of one key / value head, which read the same keys, are kept on one XCD (of 8 or more heads a whole
-// number each; 1, 2 or 4 heads get 8, 4 or 2 XCDs each); other numbers are dealt out as they come.  All heads of a
-// query tile, then those of the next.
-__device__ __forceinline__ bool place(const PromptArgs& a, int* h, int* tile) {
-  const int b = blockIdx.x, xcd = b & 7, i = b >> 3, kv_heads = a.heads / a.group;
-  if (kv_heads % 8 == 0) {
-    const int each = a.heads / 8;
-    *h = xcd * each + i % each;
-    *tile = i / each;
-  } else if (8 % kv_heads == 0) {
-    const int xcds = 8 / kv_heads, item = i * xcds + xcd % xcds;
-    *h = xcd / xcds * a.group + item % a.group;
-    *tile = item / a.group;
-  } else {
-    *h = b % a.heads;
-    *tile = b / a.heads;
-  }
-  return *tile < a.tiles;
-}
-// Workgroups that place() spreads `tiles` tiles of all heads over
-int64_t workgroups(int64_t tiles, int heads, int kv_heads) {
-  if (kv_heads % 8 == 0 || 8 % kv_heads) return tiles * heads;
-  const int64_t xcds = 8 / kv_heads;
-  return (tiles * (heads / kv_heads) + xcds - 1) / xcds * 8;
-}
-
 template <class T, int HD, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, PromptWork w) {
   using C = Cfg<HD, NW>;
@@ -251,7 +77,8 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
   const unsigned lds0 = (unsigned)(size_t)lds;
 
   int h, tile;
-  if (!place(a, &h, &tile)) return;
+  place(a.heads, a.heads / a.group, &h, &tile);
+  if (tile >= a.tiles) return;
   int r = 0, item;
   if (w.listed) {
     r = w.tile[tile] & 63;
@@ -302,141 +129,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
   auto fetch_k = [&](int t) { fetch(kp, a.ks.row, t, (t & 1) * C::TILE); };
   auto fetch_v = [&](int t) { fetch(vp, a.vs.row, t, (2 + (t & 1)) * C::TILE); };
 
-  int kofs[C::KS];
-#pragma unroll
-  for (int ks = 0; ks < C::KS; ++ks) kofs[ks] = l32 * HD * 2 + C::phys(l32, 2 * ks + g) * 16;
-  // V^T operand: lane 16 q + 4 e + t reads row 16 (..) + 8 half + 4 g + e, columns 32 hb + 16 (q % 2) + 4 t .. + 4
-  int vofs[C::HB][2];
-#pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    const int row = 8 * half + 4 * g + ((lane >> 2) & 3);
-#pragma unroll
-    for (int hb = 0; hb < C::HB; ++hb) {
-      const int col = hb * 32 + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-      vofs[hb][half] = row * HD * 2 + C::phys(row, col >> 3) * 16 + (col & 7) * 2;
-    }
-  }
-
-  f32x16 o[C::HB];
-#pragma unroll
-  for (int hb = 0; hb < C::HB; ++hb)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) o[hb][e] = 0.0f;
-  float m = 0.0f, l = 0.0f;
-  bool unset = true;   // no score above -inf yet; the same in both lanes of a query, as m is
-
-  constexpr int NK = 2 * C::KS, NV = 4 * C::HB;   // MFMAs of a tile's scores, and of its products with the values
-  // A operand of score MFMA i: keys 32 (i % 2) .. of k-step i / 2; of value MFMA j: block j % HB, keys 16 (j / HB) ..
-  const auto read_k = [&](int t, int i) {
-    return *reinterpret_cast<const x8*>(smem + (t & 1) * C::TILE + (i & 1) * 32 * HD * 2 + kofs[i >> 1]);
-  };
-  const auto read_v = [&](int t, int j) {
-    union { x8 v; v4i16 h[2]; } u;
-#pragma unroll
-    for (int half = 0; half < 2; ++half)
-      u.h[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (lds_v4i16*)(lds + (2 + (t & 1)) * C::TILE + j / C::HB * 16 * HD * 2 + vofs[j % C::HB][half]));
-    return u.v;
-  };
-  const f32x16 zero = {};
-  constexpr float TOP = std::is_same_v<T, f16> ? 15.0f : 0.0f;
-  // The scores of tile t, keys 32 .. in s[1].
-  const auto scores = [&](int t, f32x16* s) {
-#pragma unroll
-    for (int i = 0; i < NK; ++i)
-      s[i & 1] = Mfma<T>::go(read_k(t, i), qf[i >> 1], i < 2 ? zero : s[i & 1]);
-  };
-  // Tile t: the online softmax of its scores s and O^T += V^T P^T, and beside them the next tile's scores n.  One
-  // FMA turns a score into x = s c - m, in log2 units over m, the maximum less TOP - 8.  m is raised lazily, when some
-  // x exceeds TOP, so p = 2^x <= 2^TOP and O is rarely scaled; O and l share m, so O / l is the same.  The first score
-  // above -inf sets it, in whichever tile that is: until then O and l are 0.  TOP keeps bf16's sums from overflow where
-  // a softmax's do not, and fp16's small weights from vanishing: what is lost below 2^-24 is 2^-32 of the largest
-  // weight.  The matrix unit takes 32 cycles an MFMA, in which the wave issues some 8 other instructions: the softmax's
-  // are dealt out behind the MFMAs by hand, in steps that nothing is moved across, each with the operands of the MFMA
-  // four steps on.  (Left to the compiler they come in blocks, and both waves of a SIMD wait for the same unit: 8,192
-  // tokens with all keys 942 us, so 897.)
-  const auto step = [&](int t, f32x16* s, f32x16* n, auto masked, auto next) {
-    constexpr bool MASKED = decltype(masked)::value, NEXT = decltype(next)::value;
-    const int k0 = (tb + t) * KT;
-    x8 kf[4], vf[4], p[4];
-    if constexpr (NEXT) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) kf[i] = read_k(t + 1, i);
-    }
-    float mx = -INFINITY;
-    constexpr int H = NK / 2, E = 32 / H;   // steps of the first part, and scores of each
-#pragma unroll
-    for (int i = 0; i < H; ++i) {
-      if constexpr (NEXT) {
-        n[i & 1] = Mfma<T>::go(kf[i & 3], qf[i >> 1], i < 2 ? zero : n[i & 1]);
-        kf[i & 3] = read_k(t + 1, i + 4);
-      }
-#pragma unroll
-      for (int v = E * i; v < E * i + E; ++v) {
-        float x = fmaf(s[v >> 4][v & 15], a.scale_log2, -m);
-        if (MASKED && k0 + (v >> 4) * 32 + (v & 15) / 4 * 8 + g * 4 + (v & 3) >= sees) x = -INFINITY;
-        mx = fmaxf(mx, x);
-        s[v >> 4][v & 15] = x;
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    {   // the query's other half of the keys is in lane ^ 32
-      const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-      mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
-    }
-    const bool need = mx > (unset ? -INFINITY : TOP);   // a query that sees nothing keeps m = 0, l = 0
-    if (__any(need)) {
-      const float d = need ? mx - (TOP - 8.0f) : 0.0f;
-      const float alpha = unset ? 0.0f : __builtin_amdgcn_exp2f(-d);
-      unset = unset && !need;
-      m += d;
-      l *= alpha;
-#pragma unroll
-      for (int hb = 0; hb < C::HB; ++hb)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[hb][e] *= alpha;
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[kb][e] -= d;
-    }
-    float sum[4];
-    const auto weigh = [&](int v) {
-      const float x = __builtin_amdgcn_exp2f(s[v >> 4][v & 15]);
-      sum[v >> 3] = v & 7 ? sum[v >> 3] + x : x;
-      p[v >> 3][v & 7] = (T)x;
-    };
-    __builtin_amdgcn_sched_barrier(0);
-    if constexpr (!NEXT) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) vf[i] = read_v(t, i);
-    }
-    constexpr int W = 16 / H;   // weights of the first 32 keys, a step
-#pragma unroll
-    for (int i = H; i < NK; ++i) {
-      if constexpr (NEXT) {
-        n[i & 1] = Mfma<T>::go(kf[i & 3], qf[i >> 1], n[i & 1]);
-        if (i + 4 < NK)
-          kf[i & 3] = read_k(t + 1, i + 4);
-        else
-          vf[i + 4 - NK] = read_v(t, i + 4 - NK);
-      }
-#pragma unroll
-      for (int v = W * (i - H); v < W * (i - H) + W; ++v) weigh(v);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    constexpr int Y = 32 / NV;   // of the others, beside the products with the first half's values
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      o[j % C::HB] = Mfma<T>::go(vf[j & 3], p[j / C::HB], o[j % C::HB]);
-      if (j + 4 < NV) vf[j & 3] = read_v(t, j + 4);
-      if (j < NV / 2)
-#pragma unroll
-        for (int v = 16 + Y * j; v < 16 + Y * j + Y; ++v) weigh(v);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-  };
+  TileWalk<T, HD, NW> walk(smem, qf, a.scale_log2);
   constexpr std::integral_constant<bool, true> yes{};
   constexpr std::integral_constant<bool, false> no{};
   // Waits until the wave's own DMA has landed and its LDS reads are done, and for the other waves to be as far.  One
@@ -447,6 +140,9 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
     meet();   // keys t + 1 and values t are there, keys t and values t - 1 read by all
     if (t + 2 < nt) fetch_k(t + 2);
     if (t + 1 < nt) fetch_v(t + 1);
+  };
+  const auto hidden = [&](int t) {   // of tile t's weights
+    return [&, k0 = (tb + t) * KT](int v) { return k0 + key_of(v, g) >= sees; };
   };
   if (nt > 0) {
     f32x16 sa[2], sb[2];
@@ -461,22 +157,22 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
     meet();
     int t = 0;
     if (nt_w > 0) {
-      scores(0, sa);
+      walk.scores(0, sa);
       // tiles that all the wave's queries see whole, in pairs; those at the border; the last one
       for (const int whole = min(fewest / KT - tb, nt_w - 1); t + 2 <= whole; t += 2) {
         arrive(t);
-        step(t, sa, sb, no, yes);
+        walk.step(t, sa, sb, hidden(t), no, yes);
         arrive(t + 1);
-        step(t + 1, sb, sa, no, yes);
+        walk.step(t + 1, sb, sa, hidden(t + 1), no, yes);
       }
       for (; t + 1 < nt_w; ++t) {
         arrive(t);
-        step(t, sa, sb, yes, yes);
+        walk.step(t, sa, sb, hidden(t), yes, yes);
         sa[0] = sb[0];
         sa[1] = sb[1];
       }
       arrive(t);
-      step(t, sa, sb, yes, no);
+      walk.step(t, sa, sb, hidden(t), yes, no);
       ++t;
     }
     for (; t < nt; ++t) arrive(t);
@@ -487,8 +183,13 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
   __syncthreads();
   if (qw >= lq) return;
   char* stage = smem + wave * 32 * HD * 2;
+  f32x16* o = walk.o;
+  float m = walk.m, l = walk.l;
   if (a.causal && any_not_finite<C::HB>(o))
-    careful_rows<T, HD>(qf, kp, a.ks.row, vp, a.vs.row, lk, tb, tb + nt_w, fewest, sees, a.scale_log2, stage, o, &m, &l);
+    careful_rows<T, HD>(
+        qf, [&](long i) { return kp + i * a.ks.row; }, [&](long i) { return vp + i * a.vs.row; },
+        [&](int i) { return i >= sees; }, [&](int t) { return (t + 1) * KT <= fewest; }, lk, tb, tb + nt_w, a.scale_log2,
+        stage, o, &m, &l);
   l += __shfl_xor(l, 32, 64);
   const float inv = l == 0.0f ? 0.0f : 1.0f / l, lse2 = l == 0.0f ? -INFINITY : m + __log2f(l);
   if (runs > 1) {
@@ -662,7 +363,7 @@ template <class T, int HD>
 eas_status launch_all(const eas_attn_shape* shape, PromptArgs a, PromptWork* w, const JoinWork& j, hipStream_t s) {
   const int qt = query_tile(*w, shape->heads, shape->causal);
   const int64_t tiles = list_tiles(w, shape->heads, qt, shape->causal);
-  const int64_t blocks = workgroups(tiles, shape->heads, shape->kv_heads);
+  const int64_t blocks = tile_workgroups(tiles, shape->heads, shape->kv_heads);
   if (!fits_launch(blocks, 2 * qt)) return EAS_ERR_UNSUPPORTED;   // a wave for 32 queries
   a.tiles = (int)tiles;
   const eas_status st = qt == 256 ? launch<T, HD, 8>(a, *w, (unsigned)blocks, s)

@@ -33,7 +33,7 @@ _SIG = {
     "eas_kv16_append": [P(Kv16CacheStruct), P(RotaryStruct), VP, I64, VP, Strides, I32, VP, Strides, VP, Strides, VP,
                         Strides, I32, VP, I32, VP, VP, I32, I32, VP],
     "eas_kv16_attention": [P(Kv16CacheStruct), P(AttnShape), VP, I32, VP, I32, VP, I32, VP, I32, I32, VP, VP, VP, I64, VP],
-    "eas_kv16_attention_workspace": [P(AttnShape), I32, I32, I32, P(I64)],
+    "eas_kv16_attention_workspace": [P(AttnShape), I32, I32, I32, I32, P(I64)],
 }
 for _name, _args in _SIG.items():
     _fn = getattr(LIB, _name)
@@ -226,7 +226,7 @@ class Kv16Cache:
         shape = _shape(self._code, heads, self.kv_heads, dim, causal, scale, qs, (0, 0), (0, 0), strides)
         need = I64()
         if most > SPLIT_TOKENS:
-            _check(LIB.eas_kv16_attention_workspace(shape, most_q, most, n, need), "Kv16Cache.attention")
+            _check(LIB.eas_kv16_attention_workspace(shape, rows, most_q, most, n, need), "Kv16Cache.attention")
         workspace, ws_ptr, ws_bytes = _workspace(workspace, need.value, index, self.device, stream)
         _check(LIB.eas_kv16_attention(self._c, shape, q.data_ptr(), rows, cu, most_q, _ints(lens, "lens", index, (n,)),
                                       most, table, max_pages, n, out.data_ptr(), lse_ptr, ws_ptr, ws_bytes,

@@ -216,25 +216,31 @@ def test_calls_with_nothing_to_do():
     assert append(n=0, held=None, pages=None) == attend(n=0, lens=None, pages=None) == eas.EAS_OK
 
 
-def workspace(max_q, max_len, n, s=None):
+def workspace(max_q, max_len, n, s=None, rows=None):
+    """rows: of the batch; None: max_q of each sequence."""
     b = ctypes.c_int64(-1)
-    assert eas.LIB.eas_kv16_attention_workspace(ctypes.byref(s or shape()), max_q, max_len, n, ctypes.byref(b)) == 0
+    rows = min(max_q * n, (1 << 31) - 1) if rows is None else rows
+    assert eas.LIB.eas_kv16_attention_workspace(ctypes.byref(s or shape()), rows, max_q, max_len, n, ctypes.byref(b)) == 0
     return b.value
 
 
-def test_workspace_sizes_grow_with_queries_and_tokens_up_to_a_bound():
+def test_workspace_sizes_grow_with_rows_and_tokens_up_to_a_bound():
     assert workspace(1, 64, 3) == 0                        # short: nothing is split
     one = workspace(1, 4000, 1)
     assert one > 0 and workspace(1, 4000, 5) == 5 * one
     assert workspace(1, 1 << 20, 1) >= workspace(1, 9000, 1) >= one
-    assert workspace(1 << 20, 1 << 30, 1) == workspace(1 << 21, 1 << 30, 1) <= 300 << 20
+    assert workspace(1 << 20, 1 << 30, 1) == workspace(1 << 21, 1 << 30, 1) <= 1200 << 20
+    # single tokens beside one chunk: by the rows there are
+    assert workspace(500, 8000, 64, rows=563) < workspace(500, 8000, 64) / 4
+    assert workspace(0, 8000, 4) == workspace(5, 8000, 0) == 0
     assert attend(ws_bytes=workspace(1, 4000, 2) - 1) == CAPACITY
     b = ctypes.c_int64()
     call = eas.LIB.eas_kv16_attention_workspace
-    assert call(None, 1, 1, 1, ctypes.byref(b)) == BAD
-    assert call(ctypes.byref(shape()), -1, 1, 1, ctypes.byref(b)) == BAD
-    assert call(ctypes.byref(shape()), 1, 1, 1, None) == BAD
-    assert call(ctypes.byref(shape(head_dim=80)), 1, 1, 1, ctypes.byref(b)) == UNSUPPORTED
+    assert call(None, 1, 1, 1, 1, ctypes.byref(b)) == BAD
+    assert call(ctypes.byref(shape()), 1, -1, 1, 1, ctypes.byref(b)) == BAD
+    assert call(ctypes.byref(shape()), -1, 1, 1, 1, ctypes.byref(b)) == BAD
+    assert call(ctypes.byref(shape()), 1, 1, 1, 1, None) == BAD
+    assert call(ctypes.byref(shape(head_dim=80)), 1, 1, 1, 1, ctypes.byref(b)) == UNSUPPORTED
 
 
 def test_the_binding_knows_where_no_workspace_is_needed():
