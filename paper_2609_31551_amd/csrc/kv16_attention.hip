@@ -1,14 +1,15 @@
-// Attention of new tokens over the paged 16-bit cache (include/eas_paged.h).
+// Attention of new tokens over the paged 16-bit cache (include/eas_paged.h): the call, sequences with few rows, and the
+// join of runs.  Sequences with many rows go to kv16_chunks.hip.
 //
 // A row is one query of one head; the rows of a sequence that share a key / value head (its queries times the
-// group's heads) are taken 16 at a time, as the columns of MFMA products whose rows are the cache's tokens and
-// dimensions:
+// group's heads) are the columns, 16 or 32 of them, of MFMA products whose rows are the cache's tokens and dimensions:
 //   S^T = K Q^T,  O^T += V^T P^T   (v_mfma_f32_16x16x32),
-// with one pass over the tokens, the running maximum and sum of the softmax in fp32, and P rounded to the element type.
-// The four waves of a workgroup take tiles of 32 tokens in turn and are joined at the end; a sequence's tokens are
-// split into runs by a rule on its own sizes, and the runs joined in order by a second kernel.
-#include <type_traits>
-
+// with one pass over the tokens, the running maximum and sum of the softmax in fp32, and P rounded to the element type
+// (2^-8 or 2^-11 of each weight at most, as the result itself).
+// The four waves of a workgroup take a quarter of its run's tokens each, 32 at a time, without a barrier between them.
+// Keys go from memory to the registers that the products take them from, two tiles ahead.  Values have to be turned:
+// they go by DMA to LDS, two tiles a wave, and are read by transposing reads.
+#include "attention_tiles.h"
 #include "paged_ops.h"
 
 namespace eas {
@@ -16,7 +17,6 @@ namespace {
 
 constexpr int TILE = 32;         // tokens per wave and step
 constexpr int NW = 4;            // waves per workgroup
-constexpr int ROWS = 16;         // of a workgroup
 static_assert(FEW_STEP == NW * TILE);
 
 template <class T>
@@ -32,153 +32,304 @@ struct Mfma16<f16> {
   __device__ static f32x4 go(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
 
-// maximum and sum over the four lanes that hold one query (lane, lane ^ 16, ^ 32, ^ 48)
+// maximum and sum over the four lanes that hold one row (lane, lane ^ 16, ^ 32, ^ 48)
 __device__ __forceinline__ float column_max(float v) {
-  v = fmaxf(v, __shfl_xor(v, 16, 64));
-  return fmaxf(v, __shfl_xor(v, 32, 64));
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 __device__ __forceinline__ float column_sum(float v) {
-  v += __shfl_xor(v, 16, 64);
-  return v + __shfl_xor(v, 32, 64);
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-template <class T, int D>
-__global__ __launch_bounds__(64 * NW) void kv16_tokens_kernel(Kv16AttnArgs a) {
+// Sizes of a tile of values in LDS.  Chunk L (16 bytes) of a token's row is stored at chunk L ^ rot: a transposing read
+// takes 32 bytes of tokens 8 g + 4 half + e, e and g = 0 .. 3, and hits all banks once for each eight of them.
+template <int D>
+struct Values {
+  static constexpr int R = D / 8;               // chunks per row
+  static constexpr int BYTES = TILE * D * 2;
+  static constexpr int NDMA = BYTES / 1024;     // DMA instructions per tile
+  static constexpr int TOKENS = 64 / R;         // of an instruction
+  __device__ static int rot(int row) {
+    return R == 16 ? 2 * (row & 3) + 8 * (row >> 3 & 1) : 2 * (row >> 1 & 1) + 4 * (row >> 3 & 1);
+  }
+};
+
+// C: columns of 16 rows that a workgroup takes
+template <class T, int D, int C>
+__global__ __launch_bounds__(64 * NW, 2) void kv16_tokens_kernel(Kv16AttnArgs a) {
   typedef typename Mfma16<T>::x8 x8;
   typedef T Tx4 __attribute__((ext_vector_type(4)));
+  using V = Values<D>;
+  constexpr int ROWS = 16 * C;
   constexpr int KS = D / 32;   // 32-dimension steps of q . k
   constexpr int DB = D / 16;   // 16-dimension blocks of the output
+  constexpr int NK = 2 * KS;   // loads of a tile's keys
+  constexpr int SETS = C * D <= 128 ? 2 : 1;   // tiles of keys in registers: two beside 32 rows of 128 spill 54 of them
   constexpr float TOP = std::is_same_v<T, f16> ? 15.0f : 0.0f;   // log2 of the largest weight
-  __shared__ float o_part[NW][ROWS][D];
+  constexpr int RING = NW * 2 * V::BYTES, PARTS = NW * ROWS * D * 4;
+  __shared__ __attribute__((aligned(1024))) char smem[RING > PARTS ? RING : PARTS];   // values, then the waves' sums
   __shared__ float m_part[NW][ROWS], l_part[NW][ROWS];
 
   unsigned b = blockIdx.x;
-  const int rt = b % (unsigned)a.row_tiles;
-  b /= (unsigned)a.row_tiles;
   const int run = b % (unsigned)a.most_runs;
   b /= (unsigned)a.most_runs;
   const int kvh = b % (unsigned)a.c.kv_heads, r = b / (unsigned)a.c.kv_heads;
   const Seq s = find_seq(a, r);
-  const int group = a.heads / a.c.kv_heads;
-  if (!takes_few(a, s) || rt * ROWS >= s.nq * group) return;
+  const int group = a.heads / a.c.kv_heads, rows = s.nq * group;
+  if (!takes_few(a, s) || rows == 0) return;
   const int runs = few_runs(s.len, s.nq, a.heads, a.c.kv_heads);
   if (run >= runs) return;
   const int each = few_run_tokens(s.len, runs);
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  // this lane's query, and how many tokens it sees
-  const int rho = rt * ROWS + c;
-  const bool real = rho < s.nq * group;
-  const int qi = real ? (unsigned)rho / (unsigned)group : 0, head = kvh * group + (real ? rho - qi * group : 0);
-  const int sees = real ? seen_by(a, s, qi) : 0;
-  const T* q = static_cast<const T*>(a.q) + (s.row0 + qi) * a.qs.row + head * a.qs.head;
-  x8 qf[KS];
-#pragma unroll
-  for (int i = 0; i < KS; ++i) qf[i] = *reinterpret_cast<const x8*>(q + 32 * i + 8 * g);
-  // the last query sees most
-  const int most = seen_by(a, s, min(rt * ROWS + ROWS - 1, s.nq * group - 1) / group);
+  // the last query sees most; the run's tokens, and of these the wave's
   const long t_begin = (long)run * each;
-  const int t_end = (int)min((long)most, t_begin + each);
+  const int t_end = (int)min((long)seen_by(a, s, s.nq - 1), t_begin + each);
+  const long w_begin = t_begin + wave * (each / NW);
+  const int w0 = (int)min(w_begin, (long)t_end), w1 = (int)min((long)t_end, w_begin + each / NW), last = w1 - 1;
+  const int tiles = (w1 - w0 + TILE - 1) / TILE;
   const int* table = a.pages + (long)r * a.max_pages;
-  // offset of a token's head in the cache, of tokens behind the last that of the last; *there: its page is held
-  const auto place = [&](int t, bool* there) {
-    t = min(t, t_end - 1);
-    const int page = table[t >> a.c.page_shift];
-    *there = held_page(a, page);
-    return token_offset(a, page, kvh, t, D);
-  };
-  const T* keys = static_cast<const T*>(a.c.k);
-  const T* values = static_cast<const T*>(a.c.v);
+  // lane p: page of the tokens 16 p .. of the 32 tiles from tile t on
+  const auto pages_of = [&](int t) { return table[min(w0 + t * TILE + 16 * lane, last) >> a.c.page_shift]; };
+  int pages = 0;   // renewed by whichever of a tile's keys and values is asked for first
+  if (tiles > 0) pages = pages_of(0);
 
-  f32x4 o[DB];
-  float m, l;
-  // The wave's tiles.  Row 4 g + e of score block i is token 8 g + 4 i + e, so that a lane ends with the scores of 8
-  // consecutive tokens, 8 g .. + 8, of one query: as the products with the values want them.
-  const auto walk = [&](auto careful) {
-    m = -INFINITY, l = 0.0f;
+  // this lane's rows, and how many tokens they see
+  int sees[C];
+  x8 qf[C][KS];
 #pragma unroll
-    for (int i = 0; i < DB; ++i) o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int t0 = (int)t_begin + wave * TILE; t0 < t_end; t0 += NW * TILE) {
-      f32x4 sc[2];
-      bool there;
+  for (int j = 0; j < C; ++j) {
+    const int rho = 16 * j + c;
+    const bool real = rho < rows;
+    const int qi = real ? (unsigned)rho / (unsigned)group : 0, head = kvh * group + (real ? rho - qi * group : 0);
+    sees[j] = real ? seen_by(a, s, qi) : 0;
+    const T* q = static_cast<const T*>(a.q) + (s.row0 + qi) * a.qs.row + head * a.qs.head;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const T* kp = keys + place(t0 + 8 * (c >> 2) + 4 * i + (c & 3), &there) + 8 * g;
-        sc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int i = 0; i < KS; ++i) qf[j][i] = *reinterpret_cast<const x8*>(q + 32 * i + 8 * g);
+  }
+
+  f32x4 o[C][DB];
+  float m[C], l[C];
+  const auto clear = [&] {
 #pragma unroll
-        for (int k = 0; k < KS; ++k) sc[i] = Mfma16<T>::go(*reinterpret_cast<const x8*>(kp + 32 * k), qf[k], sc[i]);
-      }
-      const T* vp = values + place(t0 + 8 * g, &there);   // 8 tokens lie in one page
-      const int left = there ? sees - (t0 + 8 * g) : 0;   // of the lane's 8 tokens, those that its query sees
-      float x[8], top = -INFINITY;
+    for (int j = 0; j < C; ++j) {
+      m[j] = -INFINITY, l[j] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < DB; ++i) o[j][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+  };
+  // Weights x of a tile's scores, in place; left: of the lane's 8 tokens, those that its row may see at most
+  const auto weigh = [&](f32x4 (*sc)[2], int t0, bool there, float (*x)[8]) {
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+      const int left = there ? sees[j] - (t0 + 8 * g) : 0;
+      float top = -INFINITY;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        x[i] = i < left ? sc[i >> 2][i & 3] * a.scale_log2 : -INFINITY;
-        top = fmaxf(top, x[i]);
+        x[j][i] = i < left ? sc[j][i >> 2][i & 3] * a.scale_log2 : -INFINITY;
+        top = fmaxf(top, x[j][i]);
       }
       top = column_max(top);
-      const float up = fmaxf(m, top), base = up == -INFINITY ? 0.0f : up;
-      const float alpha = __builtin_amdgcn_exp2f(m - base);
-      m = up;
-      l *= alpha;
+      if (__any(top > m[j])) {
+        const float up = fmaxf(m[j], top), alpha = up == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[j] - up);
+        m[j] = up;
+        l[j] *= alpha;
 #pragma unroll
-      for (int i = 0; i < DB; ++i) o[i] *= alpha;
+        for (int i = 0; i < DB; ++i) o[j][i] *= alpha;
+      }
+      const float base = m[j] == -INFINITY ? 0.0f : m[j];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        x[i] = __builtin_amdgcn_exp2f(x[i] - base + TOP);
-        l += x[i];
-      }
-      if constexpr (!decltype(careful)::value) {
-        x8 p;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = (T)x[i];
-        const int last = min(t0 + 8 * g + 7, t_end - 1) - min(t0 + 8 * g, t_end - 1);
-#pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          x8 v;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = vp[min(i, last) * D + 16 * d + c];
-          o[d] = Mfma16<T>::go(v, p, o[d]);
-        }
-      } else {
-        // token by token, by the queries that see it
-        for (int from = 0; from < 4; ++from)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int t = t0 + 8 * from + i;
-            const float p = __shfl(x[i], 16 * from + c, 64);
-            const long at = place(t, &there);
-            if (t < sees && there)
-#pragma unroll
-              for (int d = 0; d < DB; ++d) {
-                const Tx4 v = *reinterpret_cast<const Tx4*>(values + at + 16 * d + 4 * g);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[d][e] = fmaf(p, (float)v[e], o[d][e]);
-              }
-          }
+        x[j][i] = __builtin_amdgcn_exp2f(x[j][i] - base + TOP);
+        l[j] += x[j][i];
       }
     }
   };
-  walk(std::false_type{});
-  // A hidden value went into the products with weight 0: where it is infinite or NaN it shows, and the tiles are walked
-  // again without.
+  const T* keys = static_cast<const T*>(a.c.k);
+  const T* values = static_cast<const T*>(a.c.v);
+  const int page_mask = (1 << a.c.page_shift) - 1;
+
+  // Row 4 g + e of score block i is token 8 g + 4 i + e, so that a lane ends with the scores of 8 consecutive tokens, 8 g
+  // .. + 8, of its rows: as the products with the values want them.
+  const int ktok = 8 * (c >> 2) + (c & 3);   // + 4 i: the token whose key the lane loads for block i
+  x8 kf[SETS][2][KS];
+  int parts[SETS];   // which halves of a tile lie in pages that are held
+  const auto block_of = [&](int t, int half) {   // elements before the head's block in the half's page
+    const int page = __builtin_amdgcn_readlane(pages, (2 * t + half) & 63);
+    return ((long)(held_page(a, page) ? page : 0) * a.c.kv_heads + kvh) * D << a.c.page_shift;
+  };
+  const auto load_k = [&](int t, int set) {
+    if (SETS == 2 && t > 0 && (t & 31) == 0) pages = pages_of(t);
+    const unsigned long long held = __ballot(held_page(a, pages));
+    parts[set] = (int)(held >> (2 * t & 63) & 3);
+    const long block = c < 8 ? block_of(t, 0) : block_of(t, 1);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int at = min(w0 + t * TILE + ktok + 4 * i, last) & page_mask;   // behind the last token it again
+      const T* kp = keys + block + at * D + 8 * g;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) kf[set][i][k] = *reinterpret_cast<const x8*>(kp + 32 * k);
+    }
+  };
+  const unsigned ring = (unsigned)(size_t)(__attribute__((address_space(3))) char*)smem + wave * 2 * V::BYTES;
+  const int vrow = lane / V::R, vcol = lane % V::R;
+  const auto fetch_v = [&](int t) {
+    if (SETS == 1 && t > 0 && (t & 31) == 0) pages = pages_of(t);   // asked for before its keys
+#pragma unroll
+    for (int n = 0; n < V::NDMA; ++n) {
+      const int row = n * V::TOKENS, first = min(w0 + t * TILE + row, last);
+      const long at = block_of(t, row / 16) + (long)(first & page_mask) * D;
+      const int chunk = vcol ^ V::rot(row + vrow);
+      dma16(ring + (t & 1) * V::BYTES + n * 1024, (unsigned)min(vrow, last - first) * (D * 2) + chunk * 16, values + at);
+    }
+  };
+  // V^T operand: lane 16 g + 4 e + i reads token 8 g + 4 half + e, dimensions 16 d + 4 i .. + 4
+  const int vtok = 8 * g + (lane >> 2 & 3);
+  const unsigned vat = vtok * D * 2 + (V::rot(vtok) + (lane >> 1 & 1)) * 16 + (lane & 1) * 8;   // rot is even, at most R - 2
+  const auto read_v = [&](int t, int d) {
+    union { x8 v; v4i16 h[2]; } u;
+    const unsigned at = ring + (t & 1) * V::BYTES + (vat ^ d * 32);
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+      u.h[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(size_t)(at + half * 4 * D * 2));
+    return u.v;
+  };
+  // Tile t, whose keys are in kf[set]; MORE: how many tiles follow, 2 or more as 2.  Memory operations complete in order:
+  // when the values of tile t are waited for, what was asked for after them may be on its way.
+  const auto tile = [&](int t, int set, auto more) {
+    constexpr int MORE = decltype(more)::value;
+    f32x4 sc[C][2];
+#pragma unroll
+    for (int j = 0; j < C; ++j)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        sc[j][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int k = 0; k < KS; ++k) sc[j][i] = Mfma16<T>::go(kf[set][i][k], qf[j][k], sc[j][i]);
+      }
+    const bool there = parts[set] >> (g >> 1) & 1;
+    if constexpr (MORE >= SETS) load_k(t + SETS, set);
+    float x[C][8];
+    weigh(sc, w0 + t * TILE, there, x);
+    x8 p[C];
+#pragma unroll
+    for (int j = 0; j < C; ++j)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[j][i] = (T)x[j][i];
+    // keys t + 1, values t + 1 and keys t + 2; values t + 1 and keys t + 1
+    constexpr int AFTER = MORE == 0 ? 0 : V::NDMA + NK * (SETS == 2 ? MORE : 1);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(AFTER) : "memory");
+#pragma unroll
+    for (int d = 0; d < DB; ++d) {
+      const x8 v = read_v(t, d);
+#pragma unroll
+      for (int j = 0; j < C; ++j) o[j][d] = Mfma16<T>::go(v, p[j], o[j][d]);
+    }
+    if constexpr (MORE == 2) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the tile's reads are done
+      fetch_v(t + 2);
+    }
+  };
+  clear();
+  if (tiles > 0) {
+    load_k(0, 0);
+    fetch_v(0);
+    if (tiles > 1) {
+      if constexpr (SETS == 2) load_k(1, 1);
+      fetch_v(1);
+    }
+    int t = 0;
+    for (; t + 3 < tiles; t += 2) {
+      tile(t, 0, std::integral_constant<int, 2>{});
+      tile(t + 1, SETS - 1, std::integral_constant<int, 2>{});
+    }
+    if (t + 2 < tiles) {
+      tile(t, 0, std::integral_constant<int, 2>{});
+      tile(t + 1, SETS - 1, std::integral_constant<int, 1>{});
+      tile(t + 2, 0, std::integral_constant<int, 0>{});
+    } else if (t + 1 < tiles) {
+      tile(t, 0, std::integral_constant<int, 1>{});
+      tile(t + 1, SETS - 1, std::integral_constant<int, 0>{});
+    } else {
+      tile(t, 0, std::integral_constant<int, 0>{});
+    }
+  }
+  // A hidden value went into the products with weight 0: where it is infinite or NaN it shows, and the wave's tokens are
+  // walked again, value by value, by the rows that see them.
   uint32_t size = 0;
 #pragma unroll
-  for (int i = 0; i < DB; ++i)
+  for (int j = 0; j < C; ++j)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) size = max(size, __float_as_uint(o[i][e]) & 0x7fffffffu);
-  if (__any(size >= 0x7f800000u)) walk(std::true_type{});
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) size = max(size, __float_as_uint(o[j][i][e]) & 0x7fffffffu);
+  if (__any(size >= 0x7f800000u)) {
+    const auto place = [&](int t, bool* there) {
+      t = min(t, last);
+      const int page = table[t >> a.c.page_shift];
+      *there = held_page(a, page);
+      return token_offset(a, page, kvh, t, D);
+    };
+    clear();
+    for (int t0 = w0; t0 < w1; t0 += TILE) {
+      f32x4 sc[C][2];
+      bool there;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const T* kp = keys + place(t0 + ktok + 4 * i, &there) + 8 * g;
+#pragma unroll
+        for (int j = 0; j < C; ++j) sc[j][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          const x8 kk = *reinterpret_cast<const x8*>(kp + 32 * k);
+#pragma unroll
+          for (int j = 0; j < C; ++j) sc[j][i] = Mfma16<T>::go(kk, qf[j][k], sc[j][i]);
+        }
+      }
+      place(t0 + 8 * g, &there);
+      float x[C][8];
+      weigh(sc, t0, there, x);
+#pragma unroll 1
+      for (int from = 0; from < 4; ++from)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int t = t0 + 8 * from + i;
+          const T* vp = values + place(t, &there) + 4 * g;
+#pragma unroll
+          for (int j = 0; j < C; ++j) {
+            const float p = __shfl(x[j][i], 16 * from + c, 64);
+            if (t < sees[j] && there)
+#pragma unroll
+              for (int d = 0; d < DB; ++d) {
+                const Tx4 v = *reinterpret_cast<const Tx4*>(vp + 16 * d);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[j][d][e] = fmaf(p, (float)v[e], o[j][d][e]);
+              }
+          }
+        }
+    }
+  }
 
-  // the four waves' sums: lane (c, g) holds dimensions 16 i + 4 g .. + 4 of query c
-  l = column_sum(l);
-  if (g == 0) m_part[wave][c] = m, l_part[wave][c] = l;
+  // the four waves' sums: lane (c, g) holds dimensions 16 i + 4 g .. + 4 of its rows
+  __syncthreads();   // the values are read
+  float (*o_part)[ROWS][D] = reinterpret_cast<float (*)[ROWS][D]>(smem);
 #pragma unroll
-  for (int i = 0; i < DB; ++i) *reinterpret_cast<f32x4*>(&o_part[wave][c][16 * i + 4 * g]) = o[i];
+  for (int j = 0; j < C; ++j) {
+    l[j] = column_sum(l[j]);
+    if (g == 0) m_part[wave][16 * j + c] = m[j], l_part[wave][16 * j + c] = l[j];
+#pragma unroll
+    for (int i = 0; i < DB; ++i) *reinterpret_cast<f32x4*>(&o_part[wave][16 * j + c][16 * i + 4 * g]) = o[j][i];
+  }
   __syncthreads();
   for (int i = threadIdx.x; i < ROWS * (D / 4); i += 64 * NW) {
-    const int row = i / (D / 4), d = i % (D / 4) * 4, rr = rt * ROWS + row;
-    if (rr >= s.nq * group) break;
+    const int row = i / (D / 4), d = i % (D / 4) * 4;
+    if (row >= rows) break;
     float M = m_part[0][row];
 #pragma unroll
     for (int w = 1; w < NW; ++w) M = fmaxf(M, m_part[w][row]);
@@ -193,8 +344,8 @@ __global__ __launch_bounds__(64 * NW) void kv16_tokens_kernel(Kv16AttnArgs a) {
     }
     const float inv = L == 0.0f ? 0.0f : 1.0f / L;
     const float lse2 = L == 0.0f ? -INFINITY : M0 + __log2f(L) - TOP;
-    const int query = (unsigned)rr / (unsigned)group, h = kvh * group + rr - query * group;
     if (runs == 1) {
+      const int query = (unsigned)row / (unsigned)group, h = kvh * group + row - query * group;
       const long orow = s.row0 + query;
       Tx4 y;
 #pragma unroll
@@ -202,7 +353,7 @@ __global__ __launch_bounds__(64 * NW) void kv16_tokens_kernel(Kv16AttnArgs a) {
       *reinterpret_cast<Tx4*>(static_cast<T*>(a.out) + orow * a.os.row + h * a.os.head + d) = y;
       if (d == 0 && a.lse) a.lse[orow * a.heads + h] = lse2 * kLn2;
     } else {
-      const long slot = first_slot(a, s, r) + ((long)run * a.c.kv_heads + kvh) * s.nq * group + rr;
+      const long slot = first_slot(a, s, r) + ((long)run * a.c.kv_heads + kvh) * rows + row;
       *reinterpret_cast<f32x4*>(a.part + slot * D + d) = sum * inv;
       if (d == 0) a.part_lse[slot] = lse2;
     }
@@ -273,10 +424,9 @@ eas_status launch(Kv16AttnArgs& a, hipStream_t s) {
   const int group = a.heads / a.c.kv_heads;
   const int64_t pairs = (int64_t)a.n_seqs * a.c.kv_heads;
   const bool many = !few_rows(a.most_q, group), few = a.cu_q || !many;
-  const int64_t rows = (int64_t)a.most_q * group, tiles = ((rows < FEW_ROWS ? rows : FEW_ROWS) + ROWS - 1) / ROWS;
   constexpr int each = 256 / (D / 4);
   const int64_t join_q = split_queries(a.most_q, a.heads), joined = a.n_seqs * join_q;
-  if (pairs > 0x7fffffff || (few && !fits_launch(tiles * a.most_runs * pairs, 64 * NW))) return EAS_ERR_UNSUPPORTED;
+  if (pairs > 0x7fffffff || (few && !fits_launch(a.most_runs * pairs, 64 * NW))) return EAS_ERR_UNSUPPORTED;
   if (a.most_runs > 1 && (joined * a.heads > 0x7fffffff || !fits_launch((joined * a.heads + each - 1) / each, 256)))
     return EAS_ERR_UNSUPPORTED;
   if (many) {
@@ -284,9 +434,11 @@ eas_status launch(Kv16AttnArgs& a, hipStream_t s) {
     if (st != EAS_OK) return st;
   }
   if (few) {
-    a.row_tiles = (int)tiles;
-    const int64_t blocks = tiles * a.most_runs * pairs;
-    hipLaunchKernelGGL((kv16_tokens_kernel<T, D>), dim3((unsigned)blocks), dim3(64 * NW), 0, s, a);
+    const dim3 blocks((unsigned)(a.most_runs * pairs));
+    if ((int64_t)a.most_q * group <= 16)
+      hipLaunchKernelGGL((kv16_tokens_kernel<T, D, 1>), blocks, dim3(64 * NW), 0, s, a);
+    else
+      hipLaunchKernelGGL((kv16_tokens_kernel<T, D, 2>), blocks, dim3(64 * NW), 0, s, a);
     if (hipGetLastError() != hipSuccess) return EAS_ERR_HIP;
   }
   if (a.most_runs == 1) return EAS_OK;

@@ -52,7 +52,7 @@ struct Kv16AttnArgs {
   int max_q, most_q;    // the caller's, and a bound of the queries of a sequence that are computed
   long slots;           // of a sequence; 0: most_runs for each row and head instead
   int most_runs;        // of any sequence within the bounds
-  int row_tiles, items; // of the launch
+  int items;            // of the launch: row tiles and runs of all sequences with many rows
 };
 
 // ---- which kernel takes a sequence, and in how many runs of its tokens: by the sequence's own sizes alone, as runs
