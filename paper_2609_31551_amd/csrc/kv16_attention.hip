@@ -7,8 +7,9 @@
 // with one pass over the tokens, the running maximum and sum of the softmax in fp32, and P rounded to the element type
 // (2^-8 or 2^-11 of each weight at most, as the result itself).
 // The four waves of a workgroup take a quarter of its run's tokens each, 32 at a time, without a barrier between them.
-// Keys go from memory to the registers that the products take them from, two tiles ahead.  Values have to be turned:
-// they go by DMA to LDS, two tiles a wave, and are read by transposing reads.
+// Keys and values are on their way some tiles ahead, into registers, in loads that no branch stands around, so that
+// each is waited for alone.  Keys are taken by the products as they come; values have to be turned: a wave stores its tile
+// to LDS of its own and reads it back by transposing reads.
 #include "attention_tiles.h"
 #include "paged_ops.h"
 
@@ -46,14 +47,14 @@ __device__ __forceinline__ float column_sum(float v) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// Sizes of a tile of values in LDS.  Chunk L (16 bytes) of a token's row is stored at chunk L ^ rot: a transposing read
-// takes 32 bytes of tokens 8 g + 4 half + e, e and g = 0 .. 3, and hits all banks once for each eight of them.
+// A tile of values.  Chunk L (16 bytes) of a token's row is stored at chunk L ^ rot: a transposing read takes 32 bytes
+// of tokens 8 g + 4 half + e, e and g = 0 .. 3, and hits all banks once for each eight of them.
 template <int D>
 struct Values {
   static constexpr int R = D / 8;               // chunks per row
   static constexpr int BYTES = TILE * D * 2;
-  static constexpr int NDMA = BYTES / 1024;     // DMA instructions per tile
-  static constexpr int TOKENS = 64 / R;         // of an instruction
+  static constexpr int N = BYTES / 1024;        // loads and stores, 64 chunks each
+  static constexpr int TOKENS = 64 / R;         // of a load
   __device__ static int rot(int row) {
     return R == 16 ? 2 * (row & 3) + 8 * (row >> 3 & 1) : 2 * (row >> 1 & 1) + 4 * (row >> 3 & 1);
   }
@@ -61,18 +62,17 @@ struct Values {
 
 // C: columns of 16 rows that a workgroup takes
 template <class T, int D, int C>
-__global__ __launch_bounds__(64 * NW, 2) void kv16_tokens_kernel(Kv16AttnArgs a) {
+__global__ __launch_bounds__(64 * NW, C == 1 ? 3 : 2) void kv16_tokens_kernel(Kv16AttnArgs a) {
   typedef typename Mfma16<T>::x8 x8;
   typedef T Tx4 __attribute__((ext_vector_type(4)));
   using V = Values<D>;
   constexpr int ROWS = 16 * C;
   constexpr int KS = D / 32;   // 32-dimension steps of q . k
   constexpr int DB = D / 16;   // 16-dimension blocks of the output
-  constexpr int NK = 2 * KS;   // loads of a tile's keys
-  constexpr int SETS = C * D <= 128 ? 2 : 1;   // tiles of keys in registers: two beside 32 rows of 128 spill 54 of them
+  constexpr int SETS = C * D == 64 ? 2 : 1;   // tiles on their way
   constexpr float TOP = std::is_same_v<T, f16> ? 15.0f : 0.0f;   // log2 of the largest weight
-  constexpr int RING = NW * 2 * V::BYTES, PARTS = NW * ROWS * D * 4;
-  __shared__ __attribute__((aligned(1024))) char smem[RING > PARTS ? RING : PARTS];   // values, then the waves' sums
+  constexpr int STAGE = NW * V::BYTES, PARTS = NW * ROWS * D * 4;
+  __shared__ __attribute__((aligned(1024))) char smem[STAGE > PARTS ? STAGE : PARTS];   // values, then the waves' sums
   __shared__ float m_part[NW][ROWS], l_part[NW][ROWS];
 
   unsigned b = blockIdx.x;
@@ -82,7 +82,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kv16_tokens_kernel(Kv16AttnArgs a)
   const Seq s = find_seq(a, r);
   const int group = a.heads / a.c.kv_heads, rows = s.nq * group;
   if (!takes_few(a, s) || rows == 0) return;
-  const int runs = few_runs(s.len, s.nq, a.heads, a.c.kv_heads);
+  const int runs = few_runs(s.len, a.c.kv_heads);
   if (run >= runs) return;
   const int each = few_run_tokens(s.len, runs);
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
@@ -95,10 +95,6 @@ __global__ __launch_bounds__(64 * NW, 2) void kv16_tokens_kernel(Kv16AttnArgs a)
   const int w0 = (int)min(w_begin, (long)t_end), w1 = (int)min((long)t_end, w_begin + each / NW), last = w1 - 1;
   const int tiles = (w1 - w0 + TILE - 1) / TILE;
   const int* table = a.pages + (long)r * a.max_pages;
-  // lane p: page of the tokens 16 p .. of the 32 tiles from tile t on
-  const auto pages_of = [&](int t) { return table[min(w0 + t * TILE + 16 * lane, last) >> a.c.page_shift]; };
-  int pages = 0;   // renewed by whichever of a tile's keys and values is asked for first
-  if (tiles > 0) pages = pages_of(0);
 
   // this lane's rows, and how many tokens they see
   int sees[C];
@@ -159,51 +155,53 @@ __global__ __launch_bounds__(64 * NW, 2) void kv16_tokens_kernel(Kv16AttnArgs a)
   // .. + 8, of its rows: as the products with the values want them.
   const int ktok = 8 * (c >> 2) + (c & 3);   // + 4 i: the token whose key the lane loads for block i
   x8 kf[SETS][2][KS];
+  x8 vf[SETS][V::N];
   int parts[SETS];   // which halves of a tile lie in pages that are held
-  const auto block_of = [&](int t, int half) {   // elements before the head's block in the half's page
-    const int page = __builtin_amdgcn_readlane(pages, (2 * t + half) & 63);
-    return ((long)(held_page(a, page) ? page : 0) * a.c.kv_heads + kvh) * D << a.c.page_shift;
+  // The pages of a tile's halves, behind the last token the last one's, by scalar loads: they count apart from the others
+  struct Pages { int half[2]; };
+  const auto pages_of = [&](int t) {
+    const auto* scalar = (const __attribute__((address_space(4))) int*)(uintptr_t)table;
+    return Pages{{scalar[min(w0 + t * TILE, last) >> a.c.page_shift], scalar[min(w0 + t * TILE + 16, last) >> a.c.page_shift]}};
   };
-  const auto load_k = [&](int t, int set) {
-    if (SETS == 2 && t > 0 && (t & 31) == 0) pages = pages_of(t);
-    const unsigned long long held = __ballot(held_page(a, pages));
-    parts[set] = (int)(held >> (2 * t & 63) & 3);
-    const long block = c < 8 ? block_of(t, 0) : block_of(t, 1);
+  Pages next;   // of the tile that is asked for next
+  const int vrow = lane / V::R, vcol = lane % V::R;
+  const auto load = [&](int t, int set) {
+    const Pages now = next;
+    next = pages_of(t + 1);
+    parts[set] = (held_page(a, now.half[0]) ? 1 : 0) | (held_page(a, now.half[1]) ? 2 : 0);
+    long block[2];   // elements before the head's block
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      block[h] = ((long)(held_page(a, now.half[h]) ? now.half[h] : 0) * a.c.kv_heads + kvh) * D << a.c.page_shift;
+    const T* kp = keys + (c < 8 ? block[0] : block[1]) + 8 * g;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int at = min(w0 + t * TILE + ktok + 4 * i, last) & page_mask;   // behind the last token it again
-      const T* kp = keys + block + at * D + 8 * g;
 #pragma unroll
-      for (int k = 0; k < KS; ++k) kf[set][i][k] = *reinterpret_cast<const x8*>(kp + 32 * k);
+      for (int k = 0; k < KS; ++k) kf[set][i][k] = *reinterpret_cast<const x8*>(kp + at * D + 32 * k);
     }
-  };
-  const unsigned ring = (unsigned)(size_t)(__attribute__((address_space(3))) char*)smem + wave * 2 * V::BYTES;
-  const int vrow = lane / V::R, vcol = lane % V::R;
-  const auto fetch_v = [&](int t) {
-    if (SETS == 1 && t > 0 && (t & 31) == 0) pages = pages_of(t);   // asked for before its keys
 #pragma unroll
-    for (int n = 0; n < V::NDMA; ++n) {
-      const int row = n * V::TOKENS, first = min(w0 + t * TILE + row, last);
-      const long at = block_of(t, row / 16) + (long)(first & page_mask) * D;
-      const int chunk = vcol ^ V::rot(row + vrow);
-      dma16(ring + (t & 1) * V::BYTES + n * 1024, (unsigned)min(vrow, last - first) * (D * 2) + chunk * 16, values + at);
+    for (int n = 0; n < V::N; ++n) {
+      const int first = min(w0 + t * TILE + n * V::TOKENS, last);
+      const T* vp = values + block[n * V::TOKENS / 16] + (first & page_mask) * D;
+      vf[set][n] = *reinterpret_cast<const x8*>(vp + (unsigned)(min(vrow, last - first) * D + 8 * vcol));
     }
   };
   // V^T operand: lane 16 g + 4 e + i reads token 8 g + 4 half + e, dimensions 16 d + 4 i .. + 4
+  const unsigned stage = (unsigned)(size_t)(__attribute__((address_space(3))) char*)smem + wave * V::BYTES;
   const int vtok = 8 * g + (lane >> 2 & 3);
   const unsigned vat = vtok * D * 2 + (V::rot(vtok) + (lane >> 1 & 1)) * 16 + (lane & 1) * 8;   // rot is even, at most R - 2
-  const auto read_v = [&](int t, int d) {
+  const auto read_v = [&](int d) {
     union { x8 v; v4i16 h[2]; } u;
-    const unsigned at = ring + (t & 1) * V::BYTES + (vat ^ d * 32);
 #pragma unroll
     for (int half = 0; half < 2; ++half)
-      u.h[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(size_t)(at + half * 4 * D * 2));
+      u.h[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (lds_v4i16*)(size_t)(stage + (vat ^ d * 32) + half * 4 * D * 2));
     return u.v;
   };
-  // Tile t, whose keys are in kf[set]; MORE: how many tiles follow, 2 or more as 2.  Memory operations complete in order:
-  // when the values of tile t are waited for, what was asked for after them may be on its way.
-  const auto tile = [&](int t, int set, auto more) {
-    constexpr int MORE = decltype(more)::value;
+  // Tile t, whose keys and values are in kf[set] and vf[set]; MORE: tile t + SETS follows.
+  const auto tile = [&](int t, auto set_, auto more) {
+    constexpr int set = decltype(set_)::value;
     f32x4 sc[C][2];
 #pragma unroll
     for (int j = 0; j < C; ++j)
@@ -214,7 +212,12 @@ __global__ __launch_bounds__(64 * NW, 2) void kv16_tokens_kernel(Kv16AttnArgs a)
         for (int k = 0; k < KS; ++k) sc[j][i] = Mfma16<T>::go(kf[set][i][k], qf[j][k], sc[j][i]);
       }
     const bool there = parts[set] >> (g >> 1) & 1;
-    if constexpr (MORE >= SETS) load_k(t + SETS, set);
+#pragma unroll
+    for (int n = 0; n < V::N; ++n) {
+      const int row = n * V::TOKENS + vrow;
+      *reinterpret_cast<x8*>(smem + wave * V::BYTES + row * D * 2 + (vcol ^ V::rot(row)) * 16) = vf[set][n];
+    }
+    if constexpr (decltype(more)::value) load(t + SETS, set);
     float x[C][8];
     weigh(sc, w0 + t * TILE, there, x);
     x8 p[C];
@@ -222,43 +225,36 @@ __global__ __launch_bounds__(64 * NW, 2) void kv16_tokens_kernel(Kv16AttnArgs a)
     for (int j = 0; j < C; ++j)
 #pragma unroll
       for (int i = 0; i < 8; ++i) p[j][i] = (T)x[j][i];
-    // keys t + 1, values t + 1 and keys t + 2; values t + 1 and keys t + 1
-    constexpr int AFTER = MORE == 0 ? 0 : V::NDMA + NK * (SETS == 2 ? MORE : 1);
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(AFTER) : "memory");
+    asm volatile("" ::: "memory");   // the wave's stores come before its reads, which LDS keeps in order
+    x8 v[4];   // read ahead
+#pragma unroll
+    for (int d = 0; d < 4; ++d) v[d] = read_v(d);
 #pragma unroll
     for (int d = 0; d < DB; ++d) {
-      const x8 v = read_v(t, d);
 #pragma unroll
-      for (int j = 0; j < C; ++j) o[j][d] = Mfma16<T>::go(v, p[j], o[j][d]);
+      for (int j = 0; j < C; ++j) o[j][d] = Mfma16<T>::go(v[d & 3], p[j], o[j][d]);
+      if (d + 4 < DB) v[d & 3] = read_v(d + 4);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    if constexpr (MORE == 2) {
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the tile's reads are done
-      fetch_v(t + 2);
-    }
+    asm volatile("" ::: "memory");   // and those before the next tile's stores
   };
   clear();
   if (tiles > 0) {
-    load_k(0, 0);
-    fetch_v(0);
-    if (tiles > 1) {
-      if constexpr (SETS == 2) load_k(1, 1);
-      fetch_v(1);
-    }
+    constexpr std::integral_constant<bool, true> yes{};
+    constexpr std::integral_constant<bool, false> no{};
+    next = pages_of(0);
+    // tiles behind the last are asked for too, the last token again and again: no branch stands around a load
+    const auto sets = [&](auto&& f) {
+      f(std::integral_constant<int, 0>{});
+      if constexpr (SETS > 1) f(std::integral_constant<int, 1>{});
+      if constexpr (SETS > 2) f(std::integral_constant<int, 2>{}), f(std::integral_constant<int, 3>{});
+    };
+    sets([&](auto set) { load(set, set); });
     int t = 0;
-    for (; t + 3 < tiles; t += 2) {
-      tile(t, 0, std::integral_constant<int, 2>{});
-      tile(t + 1, SETS - 1, std::integral_constant<int, 2>{});
-    }
-    if (t + 2 < tiles) {
-      tile(t, 0, std::integral_constant<int, 2>{});
-      tile(t + 1, SETS - 1, std::integral_constant<int, 1>{});
-      tile(t + 2, 0, std::integral_constant<int, 0>{});
-    } else if (t + 1 < tiles) {
-      tile(t, 0, std::integral_constant<int, 1>{});
-      tile(t + 1, SETS - 1, std::integral_constant<int, 0>{});
-    } else {
-      tile(t, 0, std::integral_constant<int, 0>{});
-    }
+    for (; t + SETS < tiles; t += SETS) sets([&](auto set) { tile(t + set, set, yes); });
+    sets([&](auto set) {
+      if (t + set < tiles) tile(t + set, set, no);
+    });
   }
   // A hidden value went into the products with weight 0: where it is infinite or NaN it shows, and the wave's tokens are
   // walked again, value by value, by the rows that see them.
@@ -360,47 +356,82 @@ __global__ __launch_bounds__(64 * NW, 2) void kv16_tokens_kernel(Kv16AttnArgs a)
   }
 }
 
-// Joins the runs of the sequences that were split, in order: D / 4 threads for each row.
-template <class T, int D>
-__global__ __launch_bounds__(256) void kv16_join_kernel(Kv16AttnArgs a, int join_q) {
-  constexpr int EACH = 256 / (D / 4);
-  const unsigned row = blockIdx.x * EACH + threadIdx.x / (D / 4);   // (sequence, query, head), below 2^31
-  const int d = threadIdx.x % (D / 4) * 4;
-  const int h = row % (unsigned)a.heads, i = row / (unsigned)a.heads % (unsigned)join_q;
-  const int r = row / (unsigned)a.heads / (unsigned)join_q;
-  if (r >= a.n_seqs) return;
-  const Seq s = find_seq(a, r);
-  if (i >= s.nq) return;
-  const int runs = runs_of(a, s);
-  if (runs == 1) return;
-  const int group = a.heads / a.c.kv_heads, kvh = h / group;
-  const long rows = (long)s.nq * group, step = rows * a.c.kv_heads;   // from run to run
-  const long slot = first_slot(a, s, r) + kvh * rows + (long)i * group + (h - kvh * group);
-  float M = -INFINITY;
-  for (int k = 0; k < runs; ++k) M = fmaxf(M, a.part_lse[slot + k * step]);
-  const float base = M == -INFINITY ? 0.0f : M;
-  float W = 0.0f;
-  f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-  for (int k = 0; k < runs; ++k) {
-    const f32x4 x = *reinterpret_cast<const f32x4*>(a.part + (slot + k * step) * D + d);
-    const float wk = __builtin_amdgcn_exp2f(a.part_lse[slot + k * step] - base);
-    W += wk;
+// Joins the runs of the sequences that were split, a row by D / 4 threads, or, where rows are few and runs are many, by
+// four times as many, each for every fourth run, and their four sums in order.  DIRECT: a.items workgroups for each
+// sequence; else they go over the split rows of the batch in strides, as only the sequences' lengths say how many there
+// are, which takes 2 - 3 us more but no workgroup for rows that are not split.
+template <class T, int D, bool DIRECT>
+__global__ __launch_bounds__(256) void kv16_join_kernel(Kv16AttnArgs a) {
+  constexpr int L = D / 4, GROUPS = 256 / L;
+  __shared__ f32x4 sums[2][GROUPS][L];
+  const int sub = threadIdx.x / L, in = threadIdx.x % L;
+  const int group = a.heads / a.c.kv_heads;
+  const auto slices_of = [&](const Seq& s) { return takes_few(a, s) ? 4 : 1; };
+  const auto count = [&](const Seq& s) {
+    const int each = GROUPS / slices_of(s);
+    return runs_of(a, s) > 1 ? (int)(((long)s.nq * a.heads + each - 1) / each) : 0;
+  };
+  Items<decltype(count)> items(a, count, !DIRECT);
+  for (int first = blockIdx.x, turn = 0;; first += gridDim.x, turn ^= 1) {
+    int item = first, r;
+    Seq s;
+    if constexpr (DIRECT) {
+      r = (unsigned)item / (unsigned)a.items, item -= r * a.items;
+      if (r >= a.n_seqs) return;
+      s = find_seq(a, r);
+      if (item >= count(s)) return;
+    } else {
+      r = items.find(&item, &s);
+      if (r < 0) return;
+    }
+    const int runs = runs_of(a, s), slices = slices_of(s), slice = sub % slices;
+    const int row = item * (GROUPS / slices) + sub / slices;     // [key / value head, query and head of the group]
+    const int rows = s.nq * group, all = rows * a.c.kv_heads;    // all: from run to run, too
+    const long slot = first_slot(a, s, r) + min(row, all - 1);
+    float M = -INFINITY, W = 0.0f;
+    float lse[64 / L];   // of runs in + L e
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sum[e] = fmaf(wk, x[e], sum[e]);
+    for (int e = 0; e < 64 / L; ++e) {
+      lse[e] = a.part_lse[slot + (long)min(in + L * e, runs - 1) * all];
+      M = fmaxf(M, lse[e]);
+    }
+#pragma unroll
+    for (int o = L / 2; o; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
+    const float base = M == -INFINITY ? 0.0f : M;
+#pragma unroll
+    for (int e = 0; e < 64 / L; ++e) W += in + L * e < runs ? __builtin_amdgcn_exp2f(lse[e] - base) : 0.0f;
+#pragma unroll
+    for (int o = L / 2; o; o >>= 1) W += __shfl_xor(W, o, 64);
+    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 8
+    for (int k = slice; k < runs; k += slices) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(a.part + (slot + (long)k * all) * D + in * 4);
+      const float wk = __builtin_amdgcn_exp2f(a.part_lse[slot + (long)k * all] - base);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] = fmaf(wk, x[e], sum[e]);
+    }
+    sums[turn][sub][in] = sum;
+    __syncthreads();   // what is read here is written again two turns on, behind the next barrier
+    if (slices > 1) {
+#pragma unroll
+      for (int k = 1; k < 4; ++k) sum += sums[turn][(sub + k) % GROUPS][in];   // slice 0's: of slices 1, 2, 3
+    }
+    if (slice || row >= all) continue;
+    const float inv = W == 0.0f ? 0.0f : 1.0f / W;
+    typedef T Tx4 __attribute__((ext_vector_type(4)));
+    Tx4 y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = (T)(sum[e] * inv);
+    const int kvh = (unsigned)row / (unsigned)rows, i = (row - kvh * rows) / group, h = kvh * group + row - kvh * rows - i * group;
+    *reinterpret_cast<Tx4*>(static_cast<T*>(a.out) + (s.row0 + i) * a.os.row + h * a.os.head + in * 4) = y;
+    if (in == 0 && a.lse)
+      a.lse[(s.row0 + i) * a.heads + h] = W == 0.0f ? -INFINITY : ((M == -INFINITY ? 0.0f : M) + __log2f(W)) * kLn2;
   }
-  const float inv = W == 0.0f ? 0.0f : 1.0f / W;
-  typedef T Tx4 __attribute__((ext_vector_type(4)));
-  Tx4 y;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) y[e] = (T)(sum[e] * inv);
-  *reinterpret_cast<Tx4*>(static_cast<T*>(a.out) + (s.row0 + i) * a.os.row + h * a.os.head + d) = y;
-  if (d == 0 && a.lse) a.lse[(s.row0 + i) * a.heads + h] = W == 0.0f ? -INFINITY : (M + __log2f(W)) * kLn2;
 }
 
 // The most runs of a sequence within the bounds, and the slots of one that is split: runs * queries * heads.
 int most_runs(int max_q, int max_len, int heads, int kv_heads) {
-  const int group = heads / kv_heads, few = few_runs(max_len, 1, heads, kv_heads);
+  const int group = heads / kv_heads, few = few_runs(max_len, kv_heads);
   if (few_rows(max_q, group)) return few;
   const int many = many_runs(max_len, 1, kv_heads);   // fewer rows, more runs
   return many > few ? many : few;
@@ -424,11 +455,7 @@ eas_status launch(Kv16AttnArgs& a, hipStream_t s) {
   const int group = a.heads / a.c.kv_heads;
   const int64_t pairs = (int64_t)a.n_seqs * a.c.kv_heads;
   const bool many = !few_rows(a.most_q, group), few = a.cu_q || !many;
-  constexpr int each = 256 / (D / 4);
-  const int64_t join_q = split_queries(a.most_q, a.heads), joined = a.n_seqs * join_q;
   if (pairs > 0x7fffffff || (few && !fits_launch(a.most_runs * pairs, 64 * NW))) return EAS_ERR_UNSUPPORTED;
-  if (a.most_runs > 1 && (joined * a.heads > 0x7fffffff || !fits_launch((joined * a.heads + each - 1) / each, 256)))
-    return EAS_ERR_UNSUPPORTED;
   if (many) {
     const eas_status st = launch_kv16_many(a, std::is_same_v<T, bf16> ? EAS_BF16 : EAS_FP16, D, s);
     if (st != EAS_OK) return st;
@@ -442,8 +469,18 @@ eas_status launch(Kv16AttnArgs& a, hipStream_t s) {
     if (hipGetLastError() != hipSuccess) return EAS_ERR_HIP;
   }
   if (a.most_runs == 1) return EAS_OK;
-  hipLaunchKernelGGL((kv16_join_kernel<T, D>), dim3((unsigned)((joined * a.heads + each - 1) / each)), dim3(256), 0, s, a,
-                     (int)join_q);
+  constexpr int64_t each = 256 / (D / 4);   // rows of a workgroup; of one for a sequence's few rows a quarter
+  const int64_t every = (int64_t)a.n_rows * a.heads / each + a.n_seqs;
+  const int64_t of_many = many ? split_queries(a.most_q, a.heads) * a.heads / each + 1 : 0;
+  const int64_t of_few = few ? 4 * ((int64_t)FEW_ROWS * a.c.kv_heads / each + 1) : 0, seq = of_many > of_few ? of_many : of_few;
+  if (a.n_seqs * seq <= 8192) {
+    a.items = (int)seq;
+    hipLaunchKernelGGL((kv16_join_kernel<T, D, true>), dim3((unsigned)(a.n_seqs * seq)), dim3(256), 0, s, a);
+    return hipGetLastError() == hipSuccess ? EAS_OK : EAS_ERR_HIP;
+  }
+  const int64_t blocks = 4 * every;
+  constexpr int64_t most = 4096;
+  hipLaunchKernelGGL((kv16_join_kernel<T, D, false>), dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, s, a);
   return hipGetLastError() == hipSuccess ? EAS_OK : EAS_ERR_HIP;
 }
 
@@ -497,9 +534,12 @@ extern "C" eas_status eas_kv16_attention(const eas_kv16_cache* cache, const eas_
   a.max_pages = max_pages, a.n_seqs = n_seqs;
   const int64_t there = (int64_t)max_pages * cache->page_tokens;
   a.max_len = max_len < there ? max_len : (int)there;
-  a.most_runs = most_runs(a.most_q, a.max_len, a.heads, a.c.kv_heads);
+  // where all sequences have the same number of queries it is known here
+  a.most_runs = !cu_q && (int64_t)max_q * n_seqs == n_rows && !few_rows(max_q, a.heads / a.c.kv_heads)
+                    ? many_runs(a.max_len, (long)max_q * (a.heads / a.c.kv_heads), a.c.kv_heads)
+                    : most_runs(a.most_q, a.max_len, a.heads, a.c.kv_heads);
   if (a.most_runs > 1) {
-    a.slots = seq_slots(a.most_q, a.max_len, a.heads, a.c.kv_heads);
+    a.slots = split_queries(a.most_q, a.heads) * a.heads * a.most_runs;
     const int64_t slots = all_slots(n_rows, n_seqs, a.slots, a.heads, a.most_runs);
     if (slots < (int64_t)n_seqs * a.slots) a.slots = 0;
     if (!workspace || !aligned16(workspace)) return EAS_ERR_INVALID_ARG;

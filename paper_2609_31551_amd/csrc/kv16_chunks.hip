@@ -13,38 +13,6 @@
 namespace eas {
 namespace {
 
-// The sequence and its item of the launch's `item`th: row tiles and runs of all sequences with many rows, in order.
-// Each wave goes over the sequences by itself, 64 at a time.  False where there is none.
-template <int QT>
-__device__ __forceinline__ bool find_item(const Kv16AttnArgs& a, int* item, int* r) {
-  const int lane = threadIdx.x & 63, group = a.heads / a.c.kv_heads;
-  for (int first = 0; first < a.n_seqs; first += 64) {
-    int own = 0;
-    if (first + lane < a.n_seqs) {
-      const Seq s = find_seq(a, first + lane);
-      if (!takes_few(a, s)) {
-        const long rows = (long)s.nq * group;
-        own = (int)((rows + QT - 1) / QT) * many_runs(s.len, rows, a.c.kv_heads);
-      }
-    }
-    int upto = own;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int x = __shfl_up(upto, o, 64);
-      upto += lane >= o ? x : 0;
-    }
-    const unsigned long long behind = __ballot(upto > *item);
-    if (behind) {
-      const int at = __ffsll(behind) - 1;
-      *item -= __builtin_amdgcn_readlane(upto - own, at);
-      *r = first + at;
-      return true;
-    }
-    *item -= __builtin_amdgcn_readlane(upto, 63);
-  }
-  return false;
-}
-
 template <class T, int HD, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void kv16_chunks_kernel(Kv16AttnArgs a) {
   using C = Cfg<HD, NW>;
@@ -52,12 +20,18 @@ __global__ __launch_bounds__(64 * NW, 2) void kv16_chunks_kernel(Kv16AttnArgs a)
   extern __shared__ __attribute__((aligned(1024))) char smem[];   // keys x 2, values x 2
   const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) char*)smem;
 
-  int kvh, item, r;
+  const int group = a.heads / a.c.kv_heads;
+  int kvh, item;
   place(a.c.kv_heads, a.c.kv_heads, &kvh, &item);
-  if (item >= a.items || !find_item<C::QT>(a, &item, &r)) return;
-  item = __builtin_amdgcn_readfirstlane(item), r = __builtin_amdgcn_readfirstlane(r);
-  const Seq s = find_seq(a, r);
-  const int group = a.heads / a.c.kv_heads, rows = s.nq * group;
+  if (item >= a.items) return;
+  const auto count = [&](const Seq& s) {
+    const long rows = (long)s.nq * group;
+    return takes_few(a, s) ? 0 : (int)((rows + C::QT - 1) / C::QT) * many_runs(s.len, rows, a.c.kv_heads);
+  };
+  Seq s;
+  const int r = Items<decltype(count)>(a, count).find(&item, &s);
+  if (r < 0) return;
+  const int rows = s.nq * group;
   const int runs = many_runs(s.len, rows, a.c.kv_heads), run = item % runs;
   const int tile = (rows + C::QT - 1) / C::QT - 1 - item / runs;   // the last rows, which see most, first
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, l32 = lane & 31;
@@ -81,26 +55,38 @@ __global__ __launch_bounds__(64 * NW, 2) void kv16_chunks_kernel(Kv16AttnArgs a)
     for (int ks = 0; ks < C::KS; ++ks) qf[ks] = *reinterpret_cast<const x8*>(qp + ks * 16 + g * 8);
   }
 
-  // A tile's DMA: instruction n = wave + NW j fills LDS slots 64 n + lane; slot i is chunk i % R of row i / R
-  constexpr int ROWS = 64 / C::R;   // of an instruction
-  const int lrow = lane / C::R;
-  const int dcol = C::logical(wave * ROWS + lrow, lane % C::R) * 16;   // the same for all j: a row's place goes by row % 16
+  // A tile's DMA: instruction n = wave + NW j fills LDS slots 64 n + lane; slot i is chunk i % R of row i / R.  Its rows
+  // lie in one part of 16 tokens, part part0 + j * PARTS, from row part_row on.
+  constexpr int ROWS = 64 / C::R, PARTS = NW * ROWS / 16;
+  const int part0 = wave * ROWS / 16, part_row = wave * ROWS % 16 + lane / C::R;
+  const int dcol = C::logical(wave * ROWS + lane / C::R, lane % C::R) * 16;   // the same for all j: a row's place goes by row % 16
   const int last = s.len - 1;
   const int* table = a.pages + (long)r * a.max_pages;
-  // in lane p (of every four), the page of tokens 16 p .. of tile t; behind the last token, the last one's
-  const auto pages_of = [&](int t) { return table[min((tb + t) * KT + 16 * (lane & 3), last) >> a.c.page_shift]; };
+  // lane p has part p % 4 of a tile: its first token -- the last one where it lies behind it -- and that one's page
+  const auto token_of = [&](int t) { return min((tb + t) * KT + 16 * (lane & 3), last); };
+  const auto pages_of = [&](int t) { return table[token_of(t) >> a.c.page_shift]; };
   const auto held_parts = [&](int pages) { return (int)(__ballot(held_page(a, pages)) & 15); };
-  const auto fetch = [&](const void* base, int t, int pages, int lds_off) {
+  // bytes before the part's first token in the cache
+  const auto offset_of = [&](int t, int pages) { return token_offset(a, pages, kvh, token_of(t), HD) * 2; };
+  const auto fetch = [&](const void* base, int t, long offset, int lds_off) {
+    const uint64_t from = (uint64_t)(uintptr_t)base + offset;
+    const int lo = (int)from, hi = (int)(from >> 32);
+    const auto go = [&](int j, unsigned voff) {
+      const int part = part0 + j * PARTS;
+      const uint32_t at[2] = {(uint32_t)__builtin_amdgcn_readlane(lo, part), (uint32_t)__builtin_amdgcn_readlane(hi, part)};
+      dma16(lds0 + lds_off + (wave + NW * j) * 1024, voff, (const void*)(uintptr_t)(at[0] | (uint64_t)at[1] << 32));
+    };
+    if ((tb + t + 1) * KT <= s.len) {
 #pragma unroll
-    for (int j = 0; j < C::NDMA; ++j) {
-      const int n = wave + NW * j, row = n * ROWS, first = min((tb + t) * KT + row, last);
-      const long at = token_offset(a, __builtin_amdgcn_readlane(pages, row / 16), kvh, first, HD);
-      // rows behind the last token read it again
-      dma16(lds0 + lds_off + n * 1024, (unsigned)min(lrow, last - first) * (HD * 2) + dcol, static_cast<const T*>(base) + at);
+      for (int j = 0; j < C::NDMA; ++j) go(j, part_row * (HD * 2) + dcol);
+    } else {   // rows behind the last token read it again
+#pragma unroll
+      for (int j = 0; j < C::NDMA; ++j)
+        go(j, min(part_row, max(last - ((tb + t) * KT + 16 * (part0 + j * PARTS)), 0)) * (HD * 2) + dcol);
     }
   };
-  const auto fetch_k = [&](int t, int pages) { fetch(a.c.k, t, pages, (t & 1) * C::TILE); };
-  const auto fetch_v = [&](int t, int pages) { fetch(a.c.v, t, pages, (2 + (t & 1)) * C::TILE); };
+  const auto fetch_k = [&](int t, long offset) { fetch(a.c.k, t, offset, (t & 1) * C::TILE); };
+  const auto fetch_v = [&](int t, long offset) { fetch(a.c.v, t, offset, (2 + (t & 1)) * C::TILE); };
 
   TileWalk<T, HD, NW> walk(smem, qf, a.scale_log2);
   constexpr std::integral_constant<bool, true> yes{};
@@ -109,15 +95,18 @@ __global__ __launch_bounds__(64 * NW, 2) void kv16_chunks_kernel(Kv16AttnArgs a)
   // asm: no read may move up between the wait and the barrier.  Every wave passes it once a tile, from whichever of
   // the loops below it is in.
   const auto meet = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
-  int pages_v = 0, pages_k = 0;        // of tiles t + 1 and t + 2
+  int pages = 0;                           // of tile t + 2
+  long offset = 0;                         // of tile t + 1
   int parts = 0, parts1 = 0, parts2 = 0;   // which of the parts of tiles t, t + 1 and t + 2 are held
   const auto arrive = [&](int t) {
     meet();   // keys t + 1 and values t are there, keys t and values t - 1 read by all
-    if (t + 2 < nt) fetch_k(t + 2, pages_k);
-    if (t + 1 < nt) fetch_v(t + 1, pages_v);
-    parts = parts1, parts1 = parts2, parts2 = held_parts(pages_k);
-    pages_v = pages_k;
-    pages_k = pages_of(t + 3);
+    asm volatile("" : "+v"(pages));   // so are the page numbers: taken here, as a wait behind the DMA would be for it, too
+    const long next = offset_of(t + 2, pages);
+    parts = parts1, parts1 = parts2, parts2 = held_parts(pages);
+    if (t + 1 < nt) fetch_v(t + 1, offset);
+    if (t + 2 < nt) fetch_k(t + 2, next);
+    offset = next;
+    pages = pages_of(t + 3);
   };
   const auto hidden = [&](int t) {   // of tile t's weights
     int upto[4];
@@ -127,12 +116,14 @@ __global__ __launch_bounds__(64 * NW, 2) void kv16_chunks_kernel(Kv16AttnArgs a)
   };
   if (nt > 0) {
     f32x16 sa[2], sb[2];
-    const int pages0 = pages_of(0);
-    pages_v = pages_of(1), pages_k = pages_of(2);
-    parts1 = held_parts(pages0), parts2 = held_parts(pages_v);   // of tiles 0 and 1
-    fetch_k(0, pages0);
-    fetch_v(0, pages0);
-    if (nt > 1) fetch_k(1, pages_v);
+    const int pages0 = pages_of(0), pages1 = pages_of(1);
+    pages = pages_of(2);
+    parts1 = held_parts(pages0), parts2 = held_parts(pages1);   // of tiles 0 and 1
+    const long offset0 = offset_of(0, pages0);
+    offset = offset_of(1, pages1);
+    fetch_k(0, offset0);
+    fetch_v(0, offset0);
+    if (nt > 1) fetch_k(1, offset);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     // the queries are taken here, so that no wait for them is left to the loop, where it would wait for a tile
 #pragma unroll
@@ -240,8 +231,16 @@ eas_status launch(Kv16AttnArgs a, hipStream_t s) {
 }  // namespace
 
 eas_status launch_kv16_many(const Kv16AttnArgs& a, int32_t dtype, int dim, hipStream_t s) {
-  if (dtype == EAS_BF16) return dim == 128 ? launch<bf16, 128, 4>(a, s) : launch<bf16, 64, 4>(a, s);
-  return dim == 128 ? launch<f16, 128, 4>(a, s) : launch<f16, 64, 4>(a, s);
+  // 256 rows a workgroup share what is fetched among twice the rows; where they leave each CU a workgroup, and little of
+  // one idle behind a sequence's last row.  A row's arithmetic is the same.
+  const int64_t group = a.heads / a.c.kv_heads;
+  const bool wide = (int64_t)a.n_rows * a.heads >= 256ll * device_cus() && a.n_rows * group >= 1024ll * a.n_seqs;
+#define EAS_KV16_MANY(T, D) return wide ? launch<T, D, 8>(a, s) : launch<T, D, 4>(a, s)
+  if (dtype == EAS_BF16 && dim == 128) EAS_KV16_MANY(bf16, 128);
+  if (dtype == EAS_BF16) EAS_KV16_MANY(bf16, 64);
+  if (dim == 128) EAS_KV16_MANY(f16, 128);
+  EAS_KV16_MANY(f16, 64);
+#undef EAS_KV16_MANY
 }
 
 }  // namespace eas

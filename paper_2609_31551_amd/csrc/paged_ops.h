@@ -52,7 +52,7 @@ struct Kv16AttnArgs {
   int max_q, most_q;    // the caller's, and a bound of the queries of a sequence that are computed
   long slots;           // of a sequence; 0: most_runs for each row and head instead
   int most_runs;        // of any sequence within the bounds
-  int items;            // of the launch: row tiles and runs of all sequences with many rows
+  int items;            // of the launch: row tiles and runs of all sequences with many rows; what is joined of each sequence
 };
 
 // ---- which kernel takes a sequence, and in how many runs of its tokens: by the sequence's own sizes alone, as runs
@@ -63,12 +63,14 @@ struct Kv16AttnArgs {
 constexpr int FEW_ROWS = 32;
 __host__ __device__ inline bool few_rows(int lq, int group) { return (long)lq * group <= FEW_ROWS; }
 
-// Few rows: runs of 1,024 tokens at least
+// Few rows: beyond 1,024 tokens, runs of 1,024 or, up to 128 workgroups of a sequence, of 512.
 constexpr int FEW_STEP = 128;    // tokens that a run's length is a multiple of
-__host__ __device__ inline int few_runs(int len, int nq, int heads, int kv_heads) {
-  const int by_len = (int)(((unsigned)len + 1023) / 1024);   // len <= 2^30: 32 bits hold all sums here
+__host__ __device__ inline int few_runs(int len, int kv_heads) {
+  if (len <= 1024) return 1;
+  const int whole = (len + 1023) / 1024, halves = (len + 511) / 512, fill = (128 + kv_heads - 1) / kv_heads;
+  const int by_len = halves < fill ? halves : whole > fill ? whole : fill;
   const int most = kv_heads >= 512 ? 1 : 512 / kv_heads < 64 ? 512 / kv_heads : 64;
-  return by_len < 1 ? 1 : by_len < most ? by_len : most;
+  return by_len < most ? by_len : most;
 }
 __host__ __device__ inline int few_run_tokens(int len, int runs) {
   const unsigned all = (unsigned)runs * FEW_STEP;
@@ -80,8 +82,7 @@ constexpr int MANY_ALONE = 256, MANY_RUNS = 16;
 __host__ __device__ inline int many_runs(int len, long rows, int kv_heads) {
   const long alone = (rows + 127) / 128 * kv_heads;   // workgroups of one run
   if (alone > MANY_ALONE) return 1;
-  const int shortest = alone <= 32 ? 1024 : alone >= 128 ? 4096 : 32 * (int)alone;
-  const int runs = len / shortest;
+  const int by_len = len / (alone <= 64 ? 1024 : 2048), fill = 512 / (int)alone, runs = by_len < fill ? by_len : fill;
   return runs < 1 ? 1 : runs < MANY_RUNS ? runs : MANY_RUNS;
 }
 __host__ __device__ inline int many_run_tiles(int len, int runs) { return ((len + 63) / 64 + runs - 1) / runs; }
@@ -93,7 +94,7 @@ __device__ __forceinline__ bool takes_few(const Kv16AttnArgs& a, const Seq& s) {
 // Runs of a sequence, whichever kernel takes it
 __device__ __forceinline__ int runs_of(const Kv16AttnArgs& a, const Seq& s) {
   const int group = a.heads / a.c.kv_heads;
-  return takes_few(a, s) ? few_runs(s.len, s.nq, a.heads, a.c.kv_heads)
+  return takes_few(a, s) ? few_runs(s.len, a.c.kv_heads)
                                : many_runs(s.len, (long)s.nq * group, a.c.kv_heads);
 }
 // First of a sequence's slots in the workspace: [run, key / value head, row]
@@ -106,6 +107,54 @@ __device__ __forceinline__ long token_offset(const Kv16AttnArgs& a, int page, in
   const long block = (long)(held_page(a, page) ? page : 0) * a.c.kv_heads + kvh;
   return ((block << a.c.page_shift) + (t & ((1 << a.c.page_shift) - 1))) * dim;
 }
+
+// Sum of v over the lanes up to and with this one, by DPP: within rows of 16 lanes, then of the rows before.
+__device__ __forceinline__ int sum_upto(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);   // row_shr:1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);   // row_bcast:15, to the odd rows
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);   // row_bcast:31, to the upper two
+  return v;
+}
+
+// Pieces of work of a launch that sequence r has count(its Seq) of, in the sequences' order.  Each wave goes over the
+// sequences by itself, 64 at a time, the first 64 once.
+template <class Count>
+struct Items {
+  const Kv16AttnArgs& a;
+  const Count count;
+  Seq seq;         // of sequence `lane`
+  int own, upto;   // its pieces, and those of it and of the ones before
+
+  __device__ __forceinline__ Items(const Kv16AttnArgs& a_, const Count& count_, bool used = true) : a(a_), count(count_) {
+    if (used) load(0);
+  }
+  __device__ __forceinline__ void load(int first) {
+    const int r = first + (threadIdx.x & 63);
+    seq = find_seq(a, min(r, a.n_seqs - 1));
+    own = r < a.n_seqs ? count(seq) : 0;
+    upto = sum_upto(own);
+  }
+  // The sequence of the `*item`th piece, which becomes its number among the sequence's own; -1 where there are fewer.
+  __device__ __forceinline__ int find(int* item, Seq* s) {
+    for (int first = 0; first < a.n_seqs; first += 64) {
+      if (a.n_seqs > 64) load(first);
+      const unsigned long long behind = __ballot(upto > *item);
+      if (behind) {
+        const int at = __builtin_amdgcn_readfirstlane(__ffsll(behind) - 1);
+        const auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
+        *item = __builtin_amdgcn_readfirstlane(*item - of(upto - own));
+        *s = {(long)((uint64_t)(uint32_t)of((int)seq.row0) | (uint64_t)of((int)(seq.row0 >> 32)) << 32), of(seq.before),
+              of(seq.nq), of(seq.len), of(seq.lq)};
+        return __builtin_amdgcn_readfirstlane(first + at);
+      }
+      *item -= __builtin_amdgcn_readlane(upto, 63);
+    }
+    return -1;
+  }
+};
 
 // Launches the kernel of the sequences with many rows.
 eas_status launch_kv16_many(const Kv16AttnArgs& a, int32_t dtype, int dim, hipStream_t s);
