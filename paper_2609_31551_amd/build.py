@@ -22,8 +22,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-u
 # are finite or -inf there, never NaN; the language side's calls say what a NaN does)
 _ATTENTION = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
 FILE_FLAGS = {"attention_dma.hip": _ATTENTION + ["-fno-honor-nans"], "prompt_attention.hip": _ATTENTION,
-              "kv8_attention.hip": _ATTENTION, "kv16_attention.hip": _ATTENTION,
-              "kv16_chunks.hip": _ATTENTION}
+              "kv8_attention.hip": _ATTENTION, "kv16_attention.hip": _ATTENTION}
 
 
 # Host-code sanitizers (AddressSanitizer + UndefinedBehaviorSanitizer) for a

@@ -157,11 +157,11 @@ struct Cfg {
 };
 
 
-// The head and tile of a workgroup.  Workgroups go to the 8 XCDs in turn, each with an L2 of its own, so the heads of one
+// The head and tile of workgroup b.  Workgroups go to the 8 XCDs in turn, each with an L2 of its own, so the heads of one
 // key / value head, which read the same keys, are kept on one XCD (of 8 or more key / value heads a whole number each; 1,
 // 2 or 4 get 8, 4 or 2 XCDs each); other numbers are dealt out as they come.  All heads of a tile, then those of the next.
-__device__ __forceinline__ void place(int heads, int kv_heads, int* h, int* tile) {
-  const int b = blockIdx.x, xcd = b & 7, i = b >> 3;
+__device__ __forceinline__ void place(int b, int heads, int kv_heads, int* h, int* tile) {
+  const int xcd = b & 7, i = b >> 3;
   if (kv_heads % 8 == 0) {
     const int each = heads / 8;
     *h = xcd * each + i % each;

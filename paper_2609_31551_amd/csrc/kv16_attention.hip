@@ -1,5 +1,5 @@
 // Attention of new tokens over the paged 16-bit cache (include/eas_paged.h): the call, sequences with few rows, and the
-// join of runs.  Sequences with many rows go to kv16_chunks.hip.
+// join of runs.  Sequences with many rows are kv16_chunks.h's.
 //
 // A row is one query of one head; the rows of a sequence that share a key / value head (its queries times the
 // group's heads) are the columns, 16 or 32 of them, of MFMA products whose rows are the cache's tokens and dimensions:
@@ -10,8 +10,7 @@
 // Keys and values are on their way some tiles ahead, into registers, in loads that no branch stands around, so that
 // each is waited for alone.  Keys are taken by the products as they come; values have to be turned: a wave stores its tile
 // to LDS of its own and reads it back by transposing reads.
-#include "attention_tiles.h"
-#include "paged_ops.h"
+#include "kv16_chunks.h"
 
 namespace eas {
 namespace {
@@ -60,9 +59,16 @@ struct Values {
   }
 };
 
-// C: columns of 16 rows that a workgroup takes
+// Bytes of LDS of a workgroup: the waves' tiles of values, and, when they are read, the waves' sums
+template <int D, int C>
+constexpr int few_lds() {
+  return NW * (Values<D>::BYTES > 16 * C * D * 4 ? Values<D>::BYTES : 16 * C * D * 4);
+}
+
+// One workgroup's work, number `block` of kv_heads times the runs of sequences with few rows; C: columns of 16 rows that
+// it takes; smem: few_lds()
 template <class T, int D, int C>
-__global__ __launch_bounds__(64 * NW, C == 1 ? 3 : 2) void kv16_tokens_kernel(Kv16AttnArgs a) {
+__device__ __forceinline__ void few_rows_run(const Kv16AttnArgs& a, unsigned block, char* smem) {
   typedef typename Mfma16<T>::x8 x8;
   typedef T Tx4 __attribute__((ext_vector_type(4)));
   using V = Values<D>;
@@ -71,19 +77,15 @@ __global__ __launch_bounds__(64 * NW, C == 1 ? 3 : 2) void kv16_tokens_kernel(Kv
   constexpr int DB = D / 16;   // 16-dimension blocks of the output
   constexpr int SETS = C * D == 64 ? 2 : 1;   // tiles on their way
   constexpr float TOP = std::is_same_v<T, f16> ? 15.0f : 0.0f;   // log2 of the largest weight
-  constexpr int STAGE = NW * V::BYTES, PARTS = NW * ROWS * D * 4;
-  __shared__ __attribute__((aligned(1024))) char smem[STAGE > PARTS ? STAGE : PARTS];   // values, then the waves' sums
   __shared__ float m_part[NW][ROWS], l_part[NW][ROWS];
 
-  unsigned b = blockIdx.x;
-  const int run = b % (unsigned)a.most_runs;
-  b /= (unsigned)a.most_runs;
-  const int kvh = b % (unsigned)a.c.kv_heads, r = b / (unsigned)a.c.kv_heads;
-  const Seq s = find_seq(a, r);
-  const int group = a.heads / a.c.kv_heads, rows = s.nq * group;
-  if (!takes_few(a, s) || rows == 0) return;
-  const int runs = few_runs(s.len, a.c.kv_heads);
-  if (run >= runs) return;
+  const int group = a.heads / a.c.kv_heads, kvh = block % (unsigned)a.c.kv_heads;
+  int run = block / (unsigned)a.c.kv_heads;
+  const auto count = [&](const Seq& s) { return takes_few(a, s) && s.nq > 0 ? few_runs(s.len, a.c.kv_heads) : 0; };
+  Seq s;
+  const int r = Items<decltype(count)>(a, count).find(&run, &s);
+  if (r < 0) return;
+  const int rows = s.nq * group, runs = count(s);
   const int each = few_run_tokens(s.len, runs);
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -356,6 +358,29 @@ __global__ __launch_bounds__(64 * NW, C == 1 ? 3 : 2) void kv16_tokens_kernel(Kv
   }
 }
 
+template <class T, int D, int C>
+__global__ __launch_bounds__(64 * NW, 2) void kv16_tokens_kernel(Kv16AttnArgs a) {
+  __shared__ __attribute__((aligned(1024))) char smem[few_lds<D, C>()];
+  few_rows_run<T, D, C>(a, blockIdx.x, smem);
+}
+
+template <class T, int D, int W>
+__global__ __launch_bounds__(64 * W, 2) void kv16_chunks_kernel(Kv16AttnArgs a) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  many_rows<T, D, W>(a, blockIdx.x, smem);
+}
+
+// Both: single tokens' loads beside chunks' products (1,024, 777 and 512 tokens beside five: 129 us, in two launches 144)
+template <class T, int D>
+__global__ __launch_bounds__(64 * NW, 2) void kv16_mixed_kernel(Kv16AttnArgs a) {
+  constexpr int MANY = 4 * KT * D * 2, FEW = few_lds<D, 2>();
+  __shared__ __attribute__((aligned(1024))) char smem[MANY > FEW ? MANY : FEW];
+  if ((int)blockIdx.x < a.few_blocks)
+    few_rows_run<T, D, 2>(a, blockIdx.x, smem);
+  else
+    many_rows<T, D, NW>(a, blockIdx.x - a.few_blocks, smem);
+}
+
 // Joins the runs of the sequences that were split, a row by D / 4 threads, or, where rows are few and runs are many, by
 // four times as many, each for every fourth run, and their four sums in order.  DIRECT: a.items workgroups for each
 // sequence; else they go over the split rows of the batch in strides, as only the sequences' lengths say how many there
@@ -455,24 +480,37 @@ eas_status launch(Kv16AttnArgs& a, hipStream_t s) {
   const int group = a.heads / a.c.kv_heads;
   const int64_t pairs = (int64_t)a.n_seqs * a.c.kv_heads;
   const bool many = !few_rows(a.most_q, group), few = a.cu_q || !many;
-  if (pairs > 0x7fffffff || (few && !fits_launch(a.most_runs * pairs, 64 * NW))) return EAS_ERR_UNSUPPORTED;
-  if (many) {
-    const eas_status st = launch_kv16_many(a, std::is_same_v<T, bf16> ? EAS_BF16 : EAS_FP16, D, s);
-    if (st != EAS_OK) return st;
+  // 256 rows a workgroup share what is fetched among twice the rows of 128; where they leave each CU a workgroup, and
+  // little of one idle behind a sequence's last row.  A row's arithmetic is the same.
+  const bool wide = (int64_t)a.n_rows * a.heads >= 256ll * device_cus() && (int64_t)a.n_rows * group >= 1024ll * a.n_seqs;
+  const int64_t items = !many ? 0 : wide ? many_items<D, 8>(a) : many_items<D, 4>(a);
+  const int64_t many_blocks = tile_workgroups(items, a.c.kv_heads, a.c.kv_heads), few_blocks = few ? a.most_runs * pairs : 0;
+  if (pairs > 0x7fffffff || items > 0x7fffffff || !fits_launch(many_blocks, 512) || !fits_launch(few_blocks, 64 * NW) ||
+      !fits_launch(many_blocks + few_blocks, 64 * NW))
+    return EAS_ERR_UNSUPPORTED;
+  a.items = (int)items;
+  constexpr int lds = 4 * KT * D * 2;   // of many_rows
+  const dim3 few_grid((unsigned)few_blocks), many_grid((unsigned)many_blocks);
+  if (few && many && !wide) {
+    a.few_blocks = (int)((few_blocks + 7) / 8 * 8);   // the others' numbers still tell their XCD
+    hipLaunchKernelGGL((kv16_mixed_kernel<T, D>), dim3((unsigned)(a.few_blocks + many_blocks)), dim3(64 * NW), 0, s, a);
+  } else {
+    if (wide && many)
+      hipLaunchKernelGGL((kv16_chunks_kernel<T, D, 8>), many_grid, dim3(512), lds, s, a);
+    else if (many)
+      hipLaunchKernelGGL((kv16_chunks_kernel<T, D, 4>), many_grid, dim3(256), lds, s, a);
+    if (few && (int64_t)a.most_q * group <= 16)
+      hipLaunchKernelGGL((kv16_tokens_kernel<T, D, 1>), few_grid, dim3(64 * NW), 0, s, a);
+    else if (few)
+      hipLaunchKernelGGL((kv16_tokens_kernel<T, D, 2>), few_grid, dim3(64 * NW), 0, s, a);
   }
-  if (few) {
-    const dim3 blocks((unsigned)(a.most_runs * pairs));
-    if ((int64_t)a.most_q * group <= 16)
-      hipLaunchKernelGGL((kv16_tokens_kernel<T, D, 1>), blocks, dim3(64 * NW), 0, s, a);
-    else
-      hipLaunchKernelGGL((kv16_tokens_kernel<T, D, 2>), blocks, dim3(64 * NW), 0, s, a);
-    if (hipGetLastError() != hipSuccess) return EAS_ERR_HIP;
-  }
+  if (hipGetLastError() != hipSuccess) return EAS_ERR_HIP;
   if (a.most_runs == 1) return EAS_OK;
   constexpr int64_t each = 256 / (D / 4);   // rows of a workgroup; of one for a sequence's few rows a quarter
   const int64_t every = (int64_t)a.n_rows * a.heads / each + a.n_seqs;
   const int64_t of_many = many ? split_queries(a.most_q, a.heads) * a.heads / each + 1 : 0;
-  const int64_t of_few = few ? 4 * ((int64_t)FEW_ROWS * a.c.kv_heads / each + 1) : 0, seq = of_many > of_few ? of_many : of_few;
+  const int64_t few_most = (int64_t)a.most_q * group < FEW_ROWS ? (int64_t)a.most_q * group : FEW_ROWS;
+  const int64_t of_few = few ? (4 * few_most * a.c.kv_heads + each - 1) / each : 0, seq = of_many > of_few ? of_many : of_few;
   if (a.n_seqs * seq <= 8192) {
     a.items = (int)seq;
     hipLaunchKernelGGL((kv16_join_kernel<T, D, true>), dim3((unsigned)(a.n_seqs * seq)), dim3(256), 0, s, a);

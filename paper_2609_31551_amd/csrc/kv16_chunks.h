@@ -7,22 +7,23 @@
 // its 64 tokens lie in one to four pages.  A DMA instruction moves 4 or 8 tokens, which no page's border parts, so its
 // page is one scalar; the page numbers of a tile are one load, a tile ahead of the DMA that goes by them.  Tiles of pages
 // that are not held are masked like tokens behind a query's own (their DMA reads page 0).
+#pragma once
+
 #include "attention_tiles.h"
 #include "paged_ops.h"
 
 namespace eas {
-namespace {
 
+// One workgroup's work, number `block` of tile_workgroups(a.items, kv_heads, kv_heads); smem: keys x 2, values x 2
 template <class T, int HD, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void kv16_chunks_kernel(Kv16AttnArgs a) {
+__device__ __forceinline__ void many_rows(const Kv16AttnArgs& a, int block, char* smem) {
   using C = Cfg<HD, NW>;
   typedef typename Mfma<T>::x8 x8;
-  extern __shared__ __attribute__((aligned(1024))) char smem[];   // keys x 2, values x 2
   const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) char*)smem;
 
   const int group = a.heads / a.c.kv_heads;
   int kvh, item;
-  place(a.c.kv_heads, a.c.kv_heads, &kvh, &item);
+  place(block, a.c.kv_heads, a.c.kv_heads, &kvh, &item);
   if (item >= a.items) return;
   const auto count = [&](const Seq& s) {
     const long rows = (long)s.nq * group;
@@ -214,33 +215,12 @@ __global__ __launch_bounds__(64 * NW, 2) void kv16_chunks_kernel(Kv16AttnArgs a)
   }
 }
 
-template <class T, int HD, int NW>
-eas_status launch(Kv16AttnArgs a, hipStream_t s) {
-  using C = Cfg<HD, NW>;
-  const int group = a.heads / a.c.kv_heads;
-  // row tiles of all sequences, and their runs: of each either by its length's bound or what is split at most
-  const int64_t tiles = ((int64_t)a.n_rows * group + C::QT - 1) / C::QT + (a.n_seqs < a.n_rows ? a.n_seqs : a.n_rows);
-  const int runs = many_runs(a.max_len, 1, a.c.kv_heads);
-  const int64_t items = tiles * runs, blocks = tile_workgroups(items, a.c.kv_heads, a.c.kv_heads);
-  if (items > 0x7fffffff || !fits_launch(blocks, 64 * NW)) return EAS_ERR_UNSUPPORTED;
-  a.items = (int)items;
-  hipLaunchKernelGGL((kv16_chunks_kernel<T, HD, NW>), dim3((unsigned)blocks), dim3(64 * NW), 4 * C::TILE, s, a);
-  return hipGetLastError() == hipSuccess ? EAS_OK : EAS_ERR_HIP;
-}
-
-}  // namespace
-
-eas_status launch_kv16_many(const Kv16AttnArgs& a, int32_t dtype, int dim, hipStream_t s) {
-  // 256 rows a workgroup share what is fetched among twice the rows; where they leave each CU a workgroup, and little of
-  // one idle behind a sequence's last row.  A row's arithmetic is the same.
-  const int64_t group = a.heads / a.c.kv_heads;
-  const bool wide = (int64_t)a.n_rows * a.heads >= 256ll * device_cus() && a.n_rows * group >= 1024ll * a.n_seqs;
-#define EAS_KV16_MANY(T, D) return wide ? launch<T, D, 8>(a, s) : launch<T, D, 4>(a, s)
-  if (dtype == EAS_BF16 && dim == 128) EAS_KV16_MANY(bf16, 128);
-  if (dtype == EAS_BF16) EAS_KV16_MANY(bf16, 64);
-  if (dim == 128) EAS_KV16_MANY(f16, 128);
-  EAS_KV16_MANY(f16, 64);
-#undef EAS_KV16_MANY
+// Row tiles of all sequences, and their runs: a bound of what many_rows() has to do
+template <int HD, int NW>
+inline int64_t many_items(const Kv16AttnArgs& a) {
+  constexpr int QT = Cfg<HD, NW>::QT;
+  const int64_t rows = (int64_t)a.n_rows * (a.heads / a.c.kv_heads);
+  return ((rows + QT - 1) / QT + (a.n_seqs < a.n_rows ? a.n_seqs : a.n_rows)) * many_runs(a.max_len, 1, a.c.kv_heads);
 }
 
 }  // namespace eas

@@ -52,7 +52,8 @@ struct Kv16AttnArgs {
   int max_q, most_q;    // the caller's, and a bound of the queries of a sequence that are computed
   long slots;           // of a sequence; 0: most_runs for each row and head instead
   int most_runs;        // of any sequence within the bounds
-  int items;            // of the launch: row tiles and runs of all sequences with many rows; what is joined of each sequence
+  int items, few_blocks;   // of the launch: row tiles and runs of sequences with many rows, or rows joined of each
+                           // sequence; workgroups for those with few, which come first
 };
 
 // ---- which kernel takes a sequence, and in how many runs of its tokens: by the sequence's own sizes alone, as runs
@@ -155,8 +156,5 @@ struct Items {
     return -1;
   }
 };
-
-// Launches the kernel of the sequences with many rows.
-eas_status launch_kv16_many(const Kv16AttnArgs& a, int32_t dtype, int dim, hipStream_t s);
 
 }  // namespace eas

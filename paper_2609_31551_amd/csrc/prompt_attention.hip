@@ -77,7 +77,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
   const unsigned lds0 = (unsigned)(size_t)lds;
 
   int h, tile;
-  place(a.heads, a.heads / a.group, &h, &tile);
+  place(blockIdx.x, a.heads, a.heads / a.group, &h, &tile);
   if (tile >= a.tiles) return;
   int r = 0, item;
   if (w.listed) {
