@@ -467,7 +467,12 @@ int64_t split_queries(int max_q, int heads) {
   return max_q < most ? max_q : most;
 }
 int64_t seq_slots(int max_q, int max_len, int heads, int kv_heads) {
-  return split_queries(max_q, heads) * heads * most_runs(max_q, max_len, heads, kv_heads);
+  const int64_t rows = (int64_t)max_q * heads, few = few_runs(max_len, kv_heads), most_few = FEW_ROWS * kv_heads;
+  const int64_t of_few = (rows < most_few ? rows : most_few) * few;
+  if (few_rows(max_q, heads / kv_heads)) return of_few;
+  const int64_t many = split_queries(max_q, heads) * heads * many_runs(max_len, 1, kv_heads), most = MANY_FILL * 128;
+  const int64_t of_many = many < most ? many : most;
+  return of_few > of_many ? of_few : of_many;
 }
 // Slots of a call: for each sequence, or for each row, whichever are fewer
 int64_t all_slots(int64_t n_rows, int64_t n_seqs, int64_t each, int heads, int runs) {
@@ -577,7 +582,7 @@ extern "C" eas_status eas_kv16_attention(const eas_kv16_cache* cache, const eas_
                     ? many_runs(a.max_len, (long)max_q * (a.heads / a.c.kv_heads), a.c.kv_heads)
                     : most_runs(a.most_q, a.max_len, a.heads, a.c.kv_heads);
   if (a.most_runs > 1) {
-    a.slots = split_queries(a.most_q, a.heads) * a.heads * a.most_runs;
+    a.slots = seq_slots(a.most_q, a.max_len, a.heads, a.c.kv_heads);
     const int64_t slots = all_slots(n_rows, n_seqs, a.slots, a.heads, a.most_runs);
     if (slots < (int64_t)n_seqs * a.slots) a.slots = 0;
     if (!workspace || !aligned16(workspace)) return EAS_ERR_INVALID_ARG;

@@ -78,13 +78,15 @@ __host__ __device__ inline int few_run_tokens(int len, int runs) {
   return (int)(((unsigned)len + all - 1) / all) * FEW_STEP;
 }
 
-// Many: where the sequence alone leaves CUs without a workgroup
-constexpr int MANY_ALONE = 256, MANY_RUNS = 16;
+// Many: where the sequence alone leaves CUs without a workgroup, runs of 2,048 tokens, down to 512 where it has few
+// workgroups without, up to 512 workgroups.
+constexpr int MANY_ALONE = 256, MANY_FILL = 512;
 __host__ __device__ inline int many_runs(int len, long rows, int kv_heads) {
   const long alone = (rows + 127) / 128 * kv_heads;   // workgroups of one run
-  if (alone > MANY_ALONE) return 1;
-  const int by_len = len / (alone <= 64 ? 1024 : 2048), fill = 512 / (int)alone, runs = by_len < fill ? by_len : fill;
-  return runs < 1 ? 1 : runs < MANY_RUNS ? runs : MANY_RUNS;
+  if (len <= 1024 || alone > MANY_ALONE) return 1;
+  const int by_len = len / (alone <= 8 ? 512 : alone <= 64 ? 1024 : 2048), fill = MANY_FILL / (int)alone;
+  const int runs = by_len < fill ? by_len : fill;
+  return runs < 1 ? 1 : runs < 64 ? runs : 64;
 }
 __host__ __device__ inline int many_run_tiles(int len, int runs) { return ((len + 63) / 64 + runs - 1) / runs; }
 
