@@ -7,8 +7,8 @@ import struct
 
 import torch
 
-from .attention import (AttnShape, I32, I64, P, Strides, VP, _check, _count, _current_stream, _device, _dtype, _ints, _on,
-                        _outputs, _rows, _shape, _workspace)
+from .attention import (AttnShape, I32, I64, P, Strides, VP, _DTYPE, _check, _count, _current_stream, _device, _dtype,
+                        _ints, _on, _outputs, _rows, _shape, _workspace)
 from .eas import LIB
 
 MAX_PAIRS, MAX_AXES = 128, 4
@@ -44,12 +44,14 @@ _NO_STRIDES = Strides(0, 0)
 
 
 def _turned(x, name, out, heads, dim, dtype, index, stream):
-    """The tensor that rotated rows go to -- the caller's or a new one -- and its strides."""
+    """The tensor that rotated rows go to -- the caller's or a new one --, its address and strides."""
     if out is None:
-        out = _on(stream, lambda: torch.empty_like(x))
-    elif out.shape[0] != x.shape[0]:
+        out = torch.empty_like(x) if stream is None else _on(stream, lambda: torch.empty_like(x))
+        row, head, _ = out.stride()   # empty_like keeps x's order
+        return out, out.data_ptr(), Strides(row if x.shape[0] > 1 else 0, head if heads > 1 else 0)
+    if out.shape[0] != x.shape[0]:
         raise ValueError("%s has %d rows, wanted %d" % (name, out.shape[0], x.shape[0]))
-    return out, _rows(out, name, heads, dim, dtype, index)
+    return out, out.data_ptr(), Strides(*_rows(out, name, heads, dim, dtype, index))
 
 
 class Rotary:
@@ -86,7 +88,7 @@ class Rotary:
     def _positions(self, positions, rows, index):
         """Address and axis stride of int32 [axes, rows], or [rows] for all axes."""
         shape, strides = positions.shape, positions.stride()
-        if positions.dtype == torch.int32 and positions.get_device() == index and shape[-1:] == (rows,) \
+        if positions.dtype == torch.int32 and positions.get_device() == index and strides and shape[-1] == rows \
                 and (strides[-1] == 1 or rows <= 1):
             if len(shape) == 1:
                 return positions.data_ptr(), 0
@@ -106,22 +108,21 @@ class Rotary:
         if q.dim() != 3 or (k is not None and k.dim() != 3):
             raise ValueError("q and k must be [rows, heads, head_dim]")
         rows, heads, dim = q.shape
-        qs = _rows(q, "q", None, dim, dtype, index)
+        qs = Strides(*_rows(q, "q", None, dim, dtype, index))
         at, axis_stride = self._positions(positions, rows, index)
-        q_out, qos = _turned(q, "q_out", q_out, heads, dim, dtype, index, stream)
-        ks, kos, kv_heads, k_ptr, k_out_ptr = (0, 0), (0, 0), 0, None, None
-        if k is not None:
+        q_out, q_ptr, qos = _turned(q, "q_out", q_out, heads, dim, dtype, index, stream)
+        if k is None:
+            if k_out is not None:
+                raise ValueError("k_out without k")
+            kv_heads, k_in, k_ptr, ks, kos = 0, None, None, _NO_STRIDES, _NO_STRIDES
+        else:
             if k.shape[0] != rows:
                 raise ValueError("q has %d rows, k %d" % (rows, k.shape[0]))
-            kv_heads = k.shape[1]
-            ks = _rows(k, "k", None, dim, dtype, index)
-            k_out, kos = _turned(k, "k_out", k_out, kv_heads, dim, dtype, index, stream)
-            k_ptr, k_out_ptr = k.data_ptr(), k_out.data_ptr()
-        elif k_out is not None:
-            raise ValueError("k_out without k")
+            kv_heads, k_in = k.shape[1], k.data_ptr()
+            ks = Strides(*_rows(k, "k", None, dim, dtype, index))
+            k_out, k_ptr, kos = _turned(k, "k_out", k_out, kv_heads, dim, dtype, index, stream)
         _check(LIB.eas_rotary_rows(self._c, code, dim, 1 if inverse else 0, at, axis_stride, _count(None, rows, "rows"),
-                                   q.data_ptr(), Strides(*qs), heads, q_out.data_ptr(), Strides(*qos), k_ptr, Strides(*ks),
-                                   kv_heads, k_out_ptr, Strides(*kos),
+                                   q.data_ptr(), qs, heads, q_ptr, qos, k_in, ks, kv_heads, k_ptr, kos,
                                    _current_stream(index) if stream is None else stream.cuda_stream), "Rotary.rows")
         return q_out, k_out
 
@@ -132,17 +133,22 @@ class Kv16Cache:
     max_pages]; an entry that is no page (-1) is not held."""
 
     def __init__(self, k, v):
-        index = k.get_device()
-        if not (k.dim() == 4 and k.dtype in (torch.bfloat16, torch.float16) and v.shape == k.shape and v.dtype == k.dtype and v.get_device() == index
-                and k.is_contiguous() and v.is_contiguous()):
+        index, shape, dtype = k.get_device(), k.shape, k.dtype
+        if not (len(shape) == 4 and (dtype == torch.bfloat16 or dtype == torch.float16) and v.shape == shape
+                and v.dtype == dtype and v.get_device() == index and k.is_contiguous() and v.is_contiguous()):
             raise ValueError("wanted contiguous k and v [pages, kv_heads, page_tokens, head_dim], bfloat16 or "
-                             "float16, on one device: got " + ", ".join("%s %s on %s" % (tuple(t.shape), t.dtype, t.device) for t in (k, v)))
-        n, h, p, d = k.shape
-        code = _dtype(k.dtype)
-        self.k, self.v, self.dtype = k, v, k.dtype
+                             "float16, on one device: got " +
+                             ", ".join("%s %s on %s" % (tuple(t.shape), t.dtype, t.device) for t in (k, v)))
+        n, h, p, d = shape
+        code = _DTYPE[dtype]
+        self.k, self.v, self.dtype = k, v, dtype
         self.n_pages, self.kv_heads, self.page_tokens, self.head_dim = n, h, p, d
-        self.device, self._index, self._code = k.device, index, code
+        self._index, self._code = index, code
         self._c = Kv16CacheStruct.from_buffer_copy(_pack_cache(code, h, d, p, n, k.data_ptr(), v.data_ptr()))
+
+    @property
+    def device(self):
+        return self.k.device
 
     @classmethod
     def empty(cls, n_pages, kv_heads, head_dim, page_tokens=64, dtype=torch.bfloat16, device="cuda"):
@@ -198,9 +204,8 @@ class Kv16Cache:
             if q.dim() != 3 or q.shape[0] != rows:
                 raise ValueError("q must be [%d, heads, %d], got %s" % (rows, dim, tuple(q.shape)))
             heads = q.shape[1]
-            qs = Strides(*_rows(q, "q", None, dim, dtype, index))
-            q_out, strides = _turned(q, "q_out", q_out, heads, dim, dtype, index, stream)
-            q_ptr, out_ptr, qos = q.data_ptr(), q_out.data_ptr(), Strides(*strides)
+            q_ptr, qs = q.data_ptr(), Strides(*_rows(q, "q", None, dim, dtype, index))
+            q_out, out_ptr, qos = _turned(q, "q_out", q_out, heads, dim, dtype, index, stream)
         elif q_out is not None:
             raise ValueError("q_out without q")
         _check(LIB.eas_kv16_append(self._c, plan, at, axis_stride, q_ptr, qs, heads, out_ptr, qos, k.data_ptr(),
