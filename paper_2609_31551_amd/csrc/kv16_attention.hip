@@ -76,7 +76,9 @@ __device__ __forceinline__ void few_rows_run(const Kv16AttnArgs& a, unsigned blo
   constexpr int KS = D / 32;   // 32-dimension steps of q . k
   constexpr int DB = D / 16;   // 16-dimension blocks of the output
   constexpr int SETS = C * D == 64 ? 2 : 1;   // tiles on their way
-  constexpr float TOP = std::is_same_v<T, f16> ? 15.0f : 0.0f;   // log2 of the largest weight
+  // log2 of the largest weight: fp16's small weights do not vanish (below 2^-24, 2^-39 of the largest); bf16's sums over
+  // all tokens that there may be do not overflow where a softmax's do not
+  constexpr float TOP = std::is_same_v<T, f16> ? 15.0f : -30.0f;
   __shared__ float m_part[NW][ROWS], l_part[NW][ROWS];
 
   const int group = a.heads / a.c.kv_heads, kvh = block % (unsigned)a.c.kv_heads;
@@ -490,7 +492,7 @@ eas_status launch(Kv16AttnArgs& a, hipStream_t s) {
   const bool wide = (int64_t)a.n_rows * a.heads >= 256ll * device_cus() && (int64_t)a.n_rows * group >= 1024ll * a.n_seqs;
   const int64_t items = !many ? 0 : wide ? many_items<D, 8>(a) : many_items<D, 4>(a);
   const int64_t many_blocks = tile_workgroups(items, a.c.kv_heads, a.c.kv_heads), few_blocks = few ? a.most_runs * pairs : 0;
-  if (pairs > 0x7fffffff || items > 0x7fffffff || !fits_launch(many_blocks, 512) || !fits_launch(few_blocks, 64 * NW) ||
+  if (pairs > 0x7fffffff || items > 0x7fffffff || (int64_t)a.n_rows * group > 0x7fffff00 || !fits_launch(many_blocks, 512) || !fits_launch(few_blocks, 64 * NW) ||
       !fits_launch(many_blocks + few_blocks, 64 * NW))
     return EAS_ERR_UNSUPPORTED;
   a.items = (int)items;
