@@ -85,8 +85,15 @@ __device__ __forceinline__ void few_rows_run(const Kv16AttnArgs& a, unsigned blo
   int run = block / (unsigned)a.c.kv_heads;
   const auto count = [&](const Seq& s) { return takes_few(a, s) && s.nq > 0 ? few_runs(s.len, a.c.kv_heads) : 0; };
   Seq s;
-  const int r = Items<decltype(count)>(a, count).find(&run, &s);
-  if (r < 0) return;
+  int r;
+  if (a.direct) {
+    r = run % (unsigned)a.n_seqs, run = run / (unsigned)a.n_seqs;
+    s = find_seq(a, r);
+    if (run >= count(s)) return;
+  } else {
+    r = Items<decltype(count)>(a, count).find(&run, &s);
+    if (r < 0) return;
+  }
   const int rows = s.nq * group, runs = count(s);
   const int each = few_run_tokens(s.len, runs);
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
@@ -496,6 +503,10 @@ eas_status launch(Kv16AttnArgs& a, hipStream_t s) {
       !fits_launch(many_blocks + few_blocks, 64 * NW))
     return EAS_ERR_UNSUPPORTED;
   a.items = (int)items;
+  // Runs of short and long sequences are packed, so that workgroups without work leave no XCD or CU with less than others
+  // (eight of 333 to 9,000 tokens 16 us, 21 with places for all); where none is split, or there are more sequences than a
+  // wave looks at at once, a place each takes less time (2,048 of 128 tokens 229 us and 422)
+  a.direct = a.most_runs == 1 || a.n_seqs > 64;
   constexpr int lds = 4 * KT * D * 2;   // of many_rows
   const dim3 few_grid((unsigned)few_blocks), many_grid((unsigned)many_blocks);
   if (few && many && !wide) {

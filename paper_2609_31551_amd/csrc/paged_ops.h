@@ -54,6 +54,7 @@ struct Kv16AttnArgs {
   int most_runs;        // of any sequence within the bounds
   int items, few_blocks;   // of the launch: row tiles and runs of sequences with many rows, or rows joined of each
                            // sequence; workgroups for those with few, which come first
+  int direct;              // few rows: whether each sequence has workgroups for the most runs
 };
 
 // ---- which kernel takes a sequence, and in how many runs of its tokens: by the sequence's own sizes alone, as runs
