@@ -129,10 +129,17 @@ __device__ __forceinline__ bool any_not_finite(const f32x16* o) {
 }
 
 #pragma clang diagnostic ignored "-Winline-asm"
-// 64 lanes' 16-byte pieces at base + voff, to 1 KB of LDS in lane order
+// 64 lanes' 16-byte pieces at base + voff, to 1 KB of LDS in lane order.  A base that comes from a vector instruction
+// (READLANE) may be read by a memory instruction five wait states after it was written; the compiler, which keeps that
+// for its own instructions, does not see one in here.
+template <bool READLANE = false>
 __device__ __forceinline__ void dma16(unsigned lds_addr, unsigned voff, const void* base) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n"
-               :: "s"(lds_addr), "v"(voff), "s"(base) : "memory", "m0");
+  if constexpr (READLANE)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2\n"
+                 :: "s"(lds_addr), "v"(voff), "s"(base) : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n"
+                 :: "s"(lds_addr), "v"(voff), "s"(base) : "memory", "m0");
 }
 
 typedef short v4i16 __attribute__((ext_vector_type(4)));

@@ -75,7 +75,7 @@ __device__ __forceinline__ void many_rows(const Kv16AttnArgs& a, int block, char
     const auto go = [&](int j, unsigned voff) {
       const int part = part0 + j * PARTS;
       const uint32_t at[2] = {(uint32_t)__builtin_amdgcn_readlane(lo, part), (uint32_t)__builtin_amdgcn_readlane(hi, part)};
-      dma16(lds0 + lds_off + (wave + NW * j) * 1024, voff, (const void*)(uintptr_t)(at[0] | (uint64_t)at[1] << 32));
+      dma16<true>(lds0 + lds_off + (wave + NW * j) * 1024, voff, (const void*)(uintptr_t)(at[0] | (uint64_t)at[1] << 32));
     };
     if ((tb + t + 1) * KT <= s.len) {
 #pragma unroll
