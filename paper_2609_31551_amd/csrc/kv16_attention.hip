@@ -7,9 +7,15 @@
 // with one pass over the tokens, the running maximum and sum of the softmax in fp32, and P rounded to the element type
 // (2^-8 or 2^-11 of each weight at most, as the result itself).
 // The four waves of a workgroup take a quarter of its run's tokens each, 32 at a time, without a barrier between them.
-// Keys and values are on their way some tiles ahead, into registers, in loads that no branch stands around, so that
-// each is waited for alone.  Keys are taken by the products as they come; values have to be turned: a wave stores its tile
-// to LDS of its own and reads it back by transposing reads.
+// Keys and values are on their way a tile ahead (two for 16 rows of 64), into registers, in loads that no branch stands
+// around, so that each is waited for alone.  Keys are taken by the products as they come; values have to be turned: a wave
+// stores its tile to LDS of its own and reads it back by transposing reads.
+//
+// Bound by HBM, 4 * head_dim bytes a cached token and key / value head: 16 sequences of 32,768 tokens, 8 heads of 128,
+// 2,136 MB, take 379 us, 5.6 TB/s (a copy of 1 GiB runs at 5.2).  Short ones are bound by what comes before and behind:
+// lengths, pages and first tokens one after the other, 4 us; a workgroup draws 60 GB/ms at most, however far ahead its
+// loads are (1,023 tokens of one head 13 us, 127 5.3); the join of runs is a launch of 5 us.  32 sequences of 1 to 8,192
+// tokens, 4 heads, 141 MB, 41 us.
 #include "kv16_chunks.h"
 
 namespace eas {
@@ -172,7 +178,8 @@ __device__ __forceinline__ void few_rows_run(const Kv16AttnArgs& a, unsigned blo
   struct Pages { int half[2]; };
   const auto pages_of = [&](int t) {
     const auto* scalar = (const __attribute__((address_space(4))) int*)(uintptr_t)table;
-    return Pages{{scalar[min(w0 + t * TILE, last) >> a.c.page_shift], scalar[min(w0 + t * TILE + 16, last) >> a.c.page_shift]}};
+    const int first = w0 + t * TILE;
+    return Pages{{scalar[min(first, last) >> a.c.page_shift], scalar[min(first + 16, last) >> a.c.page_shift]}};
   };
   Pages next;   // of the tile that is asked for next
   const int vrow = lane / V::R, vcol = lane % V::R;
@@ -257,8 +264,7 @@ __device__ __forceinline__ void few_rows_run(const Kv16AttnArgs& a, unsigned blo
     // tiles behind the last are asked for too, the last token again and again: no branch stands around a load
     const auto sets = [&](auto&& f) {
       f(std::integral_constant<int, 0>{});
-      if constexpr (SETS > 1) f(std::integral_constant<int, 1>{});
-      if constexpr (SETS > 2) f(std::integral_constant<int, 2>{}), f(std::integral_constant<int, 3>{});
+      if constexpr (SETS == 2) f(std::integral_constant<int, 1>{});
     };
     sets([&](auto set) { load(set, set); });
     int t = 0;
@@ -379,7 +385,7 @@ __global__ __launch_bounds__(64 * W, 2) void kv16_chunks_kernel(Kv16AttnArgs a) 
   many_rows<T, D, W>(a, blockIdx.x, smem);
 }
 
-// Both: single tokens' loads beside chunks' products (1,024, 777 and 512 tokens beside five: 129 us, in two launches 144)
+// Both: single tokens' loads beside chunks' products (1,024, 777 and 512 tokens beside five: 132 us, in two launches 144)
 template <class T, int D>
 __global__ __launch_bounds__(64 * NW, 2) void kv16_mixed_kernel(Kv16AttnArgs a) {
   constexpr int MANY = 4 * KT * D * 2, FEW = few_lds<D, 2>();
@@ -391,9 +397,10 @@ __global__ __launch_bounds__(64 * NW, 2) void kv16_mixed_kernel(Kv16AttnArgs a) 
 }
 
 // Joins the runs of the sequences that were split, a row by D / 4 threads, or, where rows are few and runs are many, by
-// four times as many, each for every fourth run, and their four sums in order.  DIRECT: a.items workgroups for each
-// sequence; else they go over the split rows of the batch in strides, as only the sequences' lengths say how many there
-// are, which takes 2 - 3 us more but no workgroup for rows that are not split.
+// four times as many, each for every fourth run, and their four sums in order (a sequence of 16,384 tokens in 64 runs
+// 20 us, joined one run after the other 55).  DIRECT: a.items workgroups for each sequence; else they go over the split
+// rows of the batch in strides, as only the sequences' lengths say how many there are, which takes 2 - 3 us more but no
+// workgroup for rows that are not split.
 template <class T, int D, bool DIRECT>
 __global__ __launch_bounds__(256) void kv16_join_kernel(Kv16AttnArgs a) {
   constexpr int L = D / 4, GROUPS = 256 / L;
@@ -456,7 +463,8 @@ __global__ __launch_bounds__(256) void kv16_join_kernel(Kv16AttnArgs a) {
     Tx4 y;
 #pragma unroll
     for (int e = 0; e < 4; ++e) y[e] = (T)(sum[e] * inv);
-    const int kvh = (unsigned)row / (unsigned)rows, i = (row - kvh * rows) / group, h = kvh * group + row - kvh * rows - i * group;
+    const int kvh = (unsigned)row / (unsigned)rows, in_head = row - kvh * rows, i = (unsigned)in_head / (unsigned)group;
+    const int h = kvh * group + in_head - i * group;
     *reinterpret_cast<Tx4*>(static_cast<T*>(a.out) + (s.row0 + i) * a.os.row + h * a.os.head + in * 4) = y;
     if (in == 0 && a.lse)
       a.lse[(s.row0 + i) * a.heads + h] = W == 0.0f ? -INFINITY : ((M == -INFINITY ? 0.0f : M) + __log2f(W)) * kLn2;
@@ -495,12 +503,16 @@ eas_status launch(Kv16AttnArgs& a, hipStream_t s) {
   const int64_t pairs = (int64_t)a.n_seqs * a.c.kv_heads;
   const bool many = !few_rows(a.most_q, group), few = a.cu_q || !many;
   // 256 rows a workgroup share what is fetched among twice the rows of 128; where they leave each CU a workgroup, and
-  // little of one idle behind a sequence's last row.  A row's arithmetic is the same.
+  // little of one idle behind a sequence's last row: 4,096 tokens of 28 heads over 4 behind 32,768 1,830 us and 1,982, but
+  // 2,048 of 20 over 20 behind 8,192 175 and 163, and chunks of 512 to 1,024 beside single tokens 155 and 143.  A row's
+  // arithmetic is the same.
   const bool wide = (int64_t)a.n_rows * a.heads >= 256ll * device_cus() && (int64_t)a.n_rows * group >= 1024ll * a.n_seqs;
   const int64_t items = !many ? 0 : wide ? many_items<D, 8>(a) : many_items<D, 4>(a);
-  const int64_t many_blocks = tile_workgroups(items, a.c.kv_heads, a.c.kv_heads), few_blocks = few ? a.most_runs * pairs : 0;
-  if (pairs > 0x7fffffff || items > 0x7fffffff || (int64_t)a.n_rows * group > 0x7fffff00 || !fits_launch(many_blocks, 512) || !fits_launch(few_blocks, 64 * NW) ||
-      !fits_launch(many_blocks + few_blocks, 64 * NW))
+  const int64_t many_blocks = tile_workgroups(items, a.c.kv_heads, a.c.kv_heads);
+  const int64_t few_blocks = few ? a.most_runs * pairs : 0;
+  if (pairs > 0x7fffffff || items > 0x7fffffff || (int64_t)a.n_rows * group > 0x7fffff00 ||
+      !fits_launch(many_blocks, 512) || !fits_launch(few_blocks, 64 * NW) ||
+      !fits_launch(many_blocks + few_blocks + 8, 64 * NW))
     return EAS_ERR_UNSUPPORTED;
   a.items = (int)items;
   // Runs of short and long sequences are packed, so that workgroups without work leave no XCD or CU with less than others
@@ -528,7 +540,8 @@ eas_status launch(Kv16AttnArgs& a, hipStream_t s) {
   const int64_t every = (int64_t)a.n_rows * a.heads / each + a.n_seqs;
   const int64_t of_many = many ? split_queries(a.most_q, a.heads) * a.heads / each + 1 : 0;
   const int64_t few_most = (int64_t)a.most_q * group < FEW_ROWS ? (int64_t)a.most_q * group : FEW_ROWS;
-  const int64_t of_few = few ? (4 * few_most * a.c.kv_heads + each - 1) / each : 0, seq = of_many > of_few ? of_many : of_few;
+  const int64_t of_few = few ? (4 * few_most * a.c.kv_heads + each - 1) / each : 0;
+  const int64_t seq = of_many > of_few ? of_many : of_few;
   if (a.n_seqs * seq <= 8192) {
     a.items = (int)seq;
     hipLaunchKernelGGL((kv16_join_kernel<T, D, true>), dim3((unsigned)(a.n_seqs * seq)), dim3(256), 0, s, a);

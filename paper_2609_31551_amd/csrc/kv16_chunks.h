@@ -5,8 +5,14 @@
 // their group side by side, so that a chunk of few tokens fills a wave, and tokens that stand in LDS serve the whole
 // group.  The walk over the tokens is prompt attention's (attention_tiles.h); what differs is where a tile comes from:
 // its 64 tokens lie in one to four pages.  A DMA instruction moves 4 or 8 tokens, which no page's border parts, so its
-// page is one scalar; the page numbers of a tile are one load, a tile ahead of the DMA that goes by them.  Tiles of pages
-// that are not held are masked like tokens behind a query's own (their DMA reads page 0).
+// page is one scalar; the page numbers of a tile are one load, a tile ahead of the DMA that goes by them, and their
+// addresses one vector computation (each by itself in scalars: 4,096 tokens over 32,768 2,105 us, so 1,982).  Tiles of
+// pages that are not held are masked like tokens behind a query's own (their DMA reads page 0).
+//
+// Bound by the matrix units, 4 * head_dim flops for each visible (row, token) pair: 4,096 tokens of 28 heads over 4 behind
+// 32,768, 2,044 GFLOP, take 1,830 - 1,880 us, 1,087 - 1,117 TFLOP/s (prompt attention over the same rows 1,914), the units
+// 51% busy at 2.0 GHz: 448 workgroups on 256 CUs leave an eighth of the time to half of them.  Chunks of 512 to 1,024
+// tokens over up to 6,001 beside single tokens, 88 GFLOP, 132 us: the longest walk, 48 tiles, and the join.
 #pragma once
 
 #include "attention_tiles.h"
@@ -42,7 +48,8 @@ __device__ __forceinline__ void many_rows(const Kv16AttnArgs& a, int block, char
   // this lane's row, and tokens that rows see: the lane's, the wave's fewest and most, the workgroup's most
   const auto query = [&](int row) { return (int)((unsigned)min(row, rows - 1) / (unsigned)group); };
   const auto head_of = [&](int row, int i) { return kvh * group + min(row, rows - 1) - i * group; };
-  const int sees = seen_by(a, s, query(rw + l32)), fewest = seen_by(a, s, query(rw)), most = rw < rows ? seen_by(a, s, query(rw + 31)) : 0;
+  const int sees = seen_by(a, s, query(rw + l32)), fewest = seen_by(a, s, query(rw));
+  const int most = rw < rows ? seen_by(a, s, query(rw + 31)) : 0;
   // token tiles of the workgroup, from tb on those of the run, and of these the wave's
   const int all = (seen_by(a, s, query((tile + 1) * C::QT - 1)) + KT - 1) / KT, each = many_run_tiles(s.len, runs);
   const int tb = run * each;
@@ -60,7 +67,7 @@ __device__ __forceinline__ void many_rows(const Kv16AttnArgs& a, int block, char
   // lie in one part of 16 tokens, part part0 + j * PARTS, from row part_row on.
   constexpr int ROWS = 64 / C::R, PARTS = NW * ROWS / 16;
   const int part0 = wave * ROWS / 16, part_row = wave * ROWS % 16 + lane / C::R;
-  const int dcol = C::logical(wave * ROWS + lane / C::R, lane % C::R) * 16;   // the same for all j: a row's place goes by row % 16
+  const int dcol = C::logical(wave * ROWS + lane / C::R, lane % C::R) * 16;   // of all j: it goes by row % 16
   const int last = s.len - 1;
   const int* table = a.pages + (long)r * a.max_pages;
   // lane p has part p % 4 of a tile: its first token -- the last one where it lies behind it -- and that one's page

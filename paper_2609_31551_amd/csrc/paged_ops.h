@@ -60,12 +60,15 @@ struct Kv16AttnArgs {
 // ---- which kernel takes a sequence, and in how many runs of its tokens: by the sequence's own sizes alone, as runs
 // are joined with other roundings than one walk's, and a result must not depend on the batch ------------------------
 
-// A sequence's rows of a key / value head, its queries times the group's heads: up to this many are taken 16 at a time
-// by waves that share the tokens, more 32 to a wave, all tokens each.
+// A sequence's rows of a key / value head, its queries times the group's heads: up to this many are taken whole by each
+// wave, which share the tokens out; more are taken 32 to a wave, all tokens each.  (Up to 64 as two workgroups that read the
+// same tokens: four sequences of 4,096, five queries of 28 heads over 4 22 us and 23, sixteen 53 and 42.)
 constexpr int FEW_ROWS = 32;
 __host__ __device__ inline bool few_rows(int lq, int group) { return (long)lq * group <= FEW_ROWS; }
 
-// Few rows: beyond 1,024 tokens, runs of 1,024 or, up to 128 workgroups of a sequence, of 512.
+// Few rows: beyond 1,024 tokens, runs of 1,024 or, up to 128 workgroups of a sequence, of 512.  A run costs its first loads
+// and its share of the join, and one alone draws no more than one CU's loads: one sequence of 4,096 tokens, 8 heads, 14 us
+// in runs of 512 and 18 in runs of 1,024; 32 of them 103 and 99; 64 of 1,024 51 whole and 57 in two.
 constexpr int FEW_STEP = 128;    // tokens that a run's length is a multiple of
 __host__ __device__ inline int few_runs(int len, int kv_heads) {
   if (len <= 1024) return 1;
@@ -80,7 +83,9 @@ __host__ __device__ inline int few_run_tokens(int len, int runs) {
 }
 
 // Many: where the sequence alone leaves CUs without a workgroup, runs of 2,048 tokens, down to 512 where it has few
-// workgroups without, up to 512 workgroups.
+// workgroups without, up to 512 workgroups.  A call waits for its longest walk, and a batch that fills the chip anyway
+// pays for the runs' sums: 512 queries of 28 heads over 4 over 8,192 tokens 79 us, in runs of 4,096 111, eight of them 542
+// and 543; 512 of 32 over 8 over 4,096 56 and, whole, 96; 64 over 4,096 31 and, in runs of 512, 25, sixteen 99 and 126.
 constexpr int MANY_ALONE = 256, MANY_FILL = 512;
 __host__ __device__ inline int many_runs(int len, long rows, int kv_heads) {
   const long alone = (rows + 127) / 128 * kv_heads;   // workgroups of one run
