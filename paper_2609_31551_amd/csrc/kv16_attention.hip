@@ -71,10 +71,11 @@ constexpr int few_lds() {
   return NW * (Values<D>::BYTES > 16 * C * D * 4 ? Values<D>::BYTES : 16 * C * D * 4);
 }
 
-// One workgroup's work, number `block` of kv_heads times the runs of sequences with few rows; C: columns of 16 rows that
-// it takes; smem: few_lds()
+// Run `run` of sequence r, whose rows of key / value head kvh are few; C: columns of 16 rows that the workgroup takes;
+// smem: few_lds()
 template <class T, int D, int C>
-__device__ __forceinline__ void few_rows_run(const Kv16AttnArgs& a, unsigned block, char* smem) {
+__device__ __forceinline__ void few_rows_run(const Kv16AttnArgs& a, int kvh, int r, const Seq& s, int run, char* smem,
+                                             int tid) {
   typedef typename Mfma16<T>::x8 x8;
   typedef T Tx4 __attribute__((ext_vector_type(4)));
   using V = Values<D>;
@@ -87,23 +88,10 @@ __device__ __forceinline__ void few_rows_run(const Kv16AttnArgs& a, unsigned blo
   constexpr float TOP = std::is_same_v<T, f16> ? 15.0f : -30.0f;
   __shared__ float m_part[NW][ROWS], l_part[NW][ROWS];
 
-  const int group = a.heads / a.c.kv_heads, kvh = block % (unsigned)a.c.kv_heads;
-  int run = block / (unsigned)a.c.kv_heads;
-  const auto count = [&](const Seq& s) { return takes_few(a, s) && s.nq > 0 ? few_runs(s.len, a.c.kv_heads) : 0; };
-  Seq s;
-  int r;
-  if (a.direct) {
-    r = run % (unsigned)a.n_seqs, run = run / (unsigned)a.n_seqs;
-    s = find_seq(a, r);
-    if (run >= count(s)) return;
-  } else {
-    r = Items<decltype(count)>(a, count).find(&run, &s);
-    if (r < 0) return;
-  }
-  const int rows = s.nq * group, runs = count(s);
+  const int group = a.heads / a.c.kv_heads, rows = s.nq * group, runs = few_runs(s.len, a.c.kv_heads);
   const int each = few_run_tokens(s.len, runs);
-  const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = tid & 63, c = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
   // the last query sees most; the run's tokens, and of these the wave's
   const long t_begin = (long)run * each;
@@ -340,7 +328,7 @@ __device__ __forceinline__ void few_rows_run(const Kv16AttnArgs& a, unsigned blo
     for (int i = 0; i < DB; ++i) *reinterpret_cast<f32x4*>(&o_part[wave][16 * j + c][16 * i + 4 * g]) = o[j][i];
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < ROWS * (D / 4); i += 64 * NW) {
+  for (int i = tid; i < ROWS * (D / 4); i += 64 * NW) {
     const int row = i / (D / 4), d = i % (D / 4) * 4;
     if (row >= rows) break;
     float M = m_part[0][row];
@@ -373,10 +361,38 @@ __device__ __forceinline__ void few_rows_run(const Kv16AttnArgs& a, unsigned blo
   }
 }
 
-template <class T, int D, int C>
+// One workgroup's work, number `block` of a.few_blocks: of the runs of all sequences with few rows and key / value heads
+// the block-th, and where there may be more (MORE) every a.few_blocks-th from it on (as a loop, one run takes 0.3 - 1 us
+// longer).
+template <class T, int D, int C, bool MORE>
+__device__ __forceinline__ void few_rows_runs(const Kv16AttnArgs& a, int block, char* smem) {
+  for (;; block += a.few_blocks) {
+    int run = (unsigned)block / (unsigned)a.c.kv_heads;
+    const auto count = [&](const Seq& s) { return takes_few(a, s) && s.nq > 0 ? few_runs(s.len, a.c.kv_heads) : 0; };
+    Seq s;
+    int r, all;
+    if (a.most_runs == 1) {   // no look at the others' lengths
+      r = run, run = 0, all = a.n_seqs;
+      if (r >= all) return;
+      s = find_seq(a, r);
+    } else {
+      Items<decltype(count)> items(a, count);
+      all = items.all();
+      if (run >= all) return;
+      r = items.find(&run, &s);
+    }
+    int tid = threadIdx.x;
+    if constexpr (MORE) asm volatile("" : "+v"(tid));   // what follows from it is not kept in registers from run to run
+    if (a.most_runs > 1 || count(s)) few_rows_run<T, D, C>(a, block % (unsigned)a.c.kv_heads, r, s, run, smem, tid);
+    if (!MORE || (long)block + a.few_blocks >= (long)all * a.c.kv_heads) return;
+    __syncthreads();   // the sums are read
+  }
+}
+
+template <class T, int D, int C, bool MORE>
 __global__ __launch_bounds__(64 * NW, 2) void kv16_tokens_kernel(Kv16AttnArgs a) {
   __shared__ __attribute__((aligned(1024))) char smem[few_lds<D, C>()];
-  few_rows_run<T, D, C>(a, blockIdx.x, smem);
+  few_rows_runs<T, D, C, MORE>(a, blockIdx.x, smem);
 }
 
 template <class T, int D, int W>
@@ -386,12 +402,12 @@ __global__ __launch_bounds__(64 * W, 2) void kv16_chunks_kernel(Kv16AttnArgs a) 
 }
 
 // Both: single tokens' loads beside chunks' products (1,024, 777 and 512 tokens beside five: 132 us, in two launches 144)
-template <class T, int D>
+template <class T, int D, bool MORE>
 __global__ __launch_bounds__(64 * NW, 2) void kv16_mixed_kernel(Kv16AttnArgs a) {
   constexpr int MANY = 4 * KT * D * 2, FEW = few_lds<D, 2>();
   __shared__ __attribute__((aligned(1024))) char smem[MANY > FEW ? MANY : FEW];
   if ((int)blockIdx.x < a.few_blocks)
-    few_rows_run<T, D, 2>(a, blockIdx.x, smem);
+    few_rows_runs<T, D, 2, MORE>(a, blockIdx.x, smem);
   else
     many_rows<T, D, NW>(a, blockIdx.x - a.few_blocks, smem);
 }
@@ -412,19 +428,23 @@ __global__ __launch_bounds__(256) void kv16_join_kernel(Kv16AttnArgs a) {
     const int each = GROUPS / slices_of(s);
     return runs_of(a, s) > 1 ? (int)(((long)s.nq * a.heads + each - 1) / each) : 0;
   };
-  Items<decltype(count)> items(a, count, !DIRECT);
-  for (int first = blockIdx.x, turn = 0;; first += gridDim.x, turn ^= 1) {
-    int item = first, r;
-    Seq s;
+  const auto find = [&](int* item, Seq* s) {
     if constexpr (DIRECT) {
-      r = (unsigned)item / (unsigned)a.items, item -= r * a.items;
-      if (r >= a.n_seqs) return;
-      s = find_seq(a, r);
-      if (item >= count(s)) return;
+      const int r = (unsigned)*item / (unsigned)a.items;
+      if (r >= a.n_seqs) return -1;
+      *item -= r * a.items;
+      *s = find_seq(a, r);
+      return *item < count(*s) ? r : -1;
     } else {
-      r = items.find(&item, &s);
-      if (r < 0) return;
+      Items<decltype(count)> items(a, count);
+      return *item < items.all() ? items.find(item, s) : -1;
     }
+  };
+  for (int first = blockIdx.x, turn = 0;; first += gridDim.x, turn ^= 1) {
+    int item = first;
+    Seq s;
+    const int r = find(&item, &s);
+    if (r < 0) return;
     const int runs = runs_of(a, s), slices = slices_of(s), slice = sub % slices;
     const int row = item * (GROUPS / slices) + sub / slices;     // [key / value head, query and head of the group]
     const int rows = s.nq * group, all = rows * a.c.kv_heads;    // all: from run to run, too
@@ -509,30 +529,33 @@ eas_status launch(Kv16AttnArgs& a, hipStream_t s) {
   const bool wide = (int64_t)a.n_rows * a.heads >= 256ll * device_cus() && (int64_t)a.n_rows * group >= 1024ll * a.n_seqs;
   const int64_t items = !many ? 0 : wide ? many_items<D, 8>(a) : many_items<D, 4>(a);
   const int64_t many_blocks = tile_workgroups(items, a.c.kv_heads, a.c.kv_heads);
-  const int64_t few_blocks = few ? a.most_runs * pairs : 0;
-  if (pairs > 0x7fffffff || items > 0x7fffffff || (int64_t)a.n_rows * group > 0x7fffff00 ||
+  // Runs of short and long sequences are packed, so that workgroups without work leave no XCD or CU with less than others
+  // (eight of 333 to 9,000 tokens 16 us, 21 with a place for each that there may be), and as many workgroups are launched
+  // as have work where sequences are split in two: only the device knows, and one without work costs a look at the lengths
+  // (128 sequences of 1,024 tokens, 131,072 allowed: 101 us, with places for all 155)
+  const int64_t two_each = 2 * pairs < 4096 ? 4096 : 2 * pairs;
+  const int64_t few_blocks = !few ? 0 : a.most_runs * pairs < two_each ? a.most_runs * pairs : two_each;
+  if (pairs * a.most_runs > 0x7fffffff || items > 0x7fffffff || (int64_t)a.n_rows * group > 0x7fffff00 ||
       !fits_launch(many_blocks, 512) || !fits_launch(few_blocks, 64 * NW) ||
       !fits_launch(many_blocks + few_blocks + 8, 64 * NW))
     return EAS_ERR_UNSUPPORTED;
-  a.items = (int)items;
-  // Runs of short and long sequences are packed, so that workgroups without work leave no XCD or CU with less than others
-  // (eight of 333 to 9,000 tokens 16 us, 21 with places for all); where none is split, or there are more sequences than a
-  // wave looks at at once, a place each takes less time (2,048 of 128 tokens 229 us and 422)
-  a.direct = a.most_runs == 1 || a.n_seqs > 64;
+  a.items = (int)items, a.few_blocks = (int)few_blocks;
   constexpr int lds = 4 * KT * D * 2;   // of many_rows
   const dim3 few_grid((unsigned)few_blocks), many_grid((unsigned)many_blocks);
+  const bool more = few_blocks < a.most_runs * pairs;
+  const auto run = [&](auto kernel, dim3 grid, int threads, int shared) {
+    hipLaunchKernelGGL(kernel, grid, dim3(threads), shared, s, a);
+  };
   if (few && many && !wide) {
     a.few_blocks = (int)((few_blocks + 7) / 8 * 8);   // the others' numbers still tell their XCD
-    hipLaunchKernelGGL((kv16_mixed_kernel<T, D>), dim3((unsigned)(a.few_blocks + many_blocks)), dim3(64 * NW), 0, s, a);
+    const dim3 grid((unsigned)(a.few_blocks + many_blocks));
+    run(more ? kv16_mixed_kernel<T, D, true> : kv16_mixed_kernel<T, D, false>, grid, 64 * NW, 0);
   } else {
-    if (wide && many)
-      hipLaunchKernelGGL((kv16_chunks_kernel<T, D, 8>), many_grid, dim3(512), lds, s, a);
-    else if (many)
-      hipLaunchKernelGGL((kv16_chunks_kernel<T, D, 4>), many_grid, dim3(256), lds, s, a);
+    if (many) run(wide ? kv16_chunks_kernel<T, D, 8> : kv16_chunks_kernel<T, D, 4>, many_grid, wide ? 512 : 256, lds);
     if (few && (int64_t)a.most_q * group <= 16)
-      hipLaunchKernelGGL((kv16_tokens_kernel<T, D, 1>), few_grid, dim3(64 * NW), 0, s, a);
+      run(more ? kv16_tokens_kernel<T, D, 1, true> : kv16_tokens_kernel<T, D, 1, false>, few_grid, 64 * NW, 0);
     else if (few)
-      hipLaunchKernelGGL((kv16_tokens_kernel<T, D, 2>), few_grid, dim3(64 * NW), 0, s, a);
+      run(more ? kv16_tokens_kernel<T, D, 2, true> : kv16_tokens_kernel<T, D, 2, false>, few_grid, 64 * NW, 0);
   }
   if (hipGetLastError() != hipSuccess) return EAS_ERR_HIP;
   if (a.most_runs == 1) return EAS_OK;

@@ -35,9 +35,10 @@ __device__ __forceinline__ void many_rows(const Kv16AttnArgs& a, int block, char
     const long rows = (long)s.nq * group;
     return takes_few(a, s) ? 0 : (int)((rows + C::QT - 1) / C::QT) * many_runs(s.len, rows, a.c.kv_heads);
   };
+  Items<decltype(count)> items(a, count);
+  if (item >= items.all()) return;
   Seq s;
-  const int r = Items<decltype(count)>(a, count).find(&item, &s);
-  if (r < 0) return;
+  const int r = items.find(&item, &s);
   const int rows = s.nq * group;
   const int runs = many_runs(s.len, rows, a.c.kv_heads), run = item % runs;
   const int tile = (rows + C::QT - 1) / C::QT - 1 - item / runs;   // the last rows, which see most, first

@@ -54,7 +54,6 @@ struct Kv16AttnArgs {
   int most_runs;        // of any sequence within the bounds
   int items, few_blocks;   // of the launch: row tiles and runs of sequences with many rows, or rows joined of each
                            // sequence; workgroups for those with few, which come first
-  int direct;              // few rows: whether each sequence has workgroups for the most runs
 };
 
 // ---- which kernel takes a sequence, and in how many runs of its tokens: by the sequence's own sizes alone, as runs
@@ -128,40 +127,53 @@ __device__ __forceinline__ int sum_upto(int v) {
   return v;
 }
 
-// Pieces of work of a launch that sequence r has count(its Seq) of, in the sequences' order.  Each wave goes over the
-// sequences by itself, 64 at a time, the first 64 once.
+// Pieces of work of a launch that sequence r has count(its Seq) of, in an order of the sequences.  Each wave goes over
+// the sequences by itself: lane i over i, i + 64, .. one after the other, and, to find one, the wave over a lane's.
 template <class Count>
 struct Items {
   const Kv16AttnArgs& a;
   const Count count;
-  Seq seq;         // of sequence `lane`
-  int own, upto;   // its pieces, and those of it and of the ones before
+  int each;         // sequences of a lane
+  Seq seq;          // of the last one that the lane looked at: its only one where there are 64 at most
+  int own, upto;    // the lane's pieces, and those of it and of the lanes before
 
-  __device__ __forceinline__ Items(const Kv16AttnArgs& a_, const Count& count_, bool used = true) : a(a_), count(count_) {
-    if (used) load(0);
-  }
-  __device__ __forceinline__ void load(int first) {
-    const int r = first + (threadIdx.x & 63);
-    seq = find_seq(a, min(r, a.n_seqs - 1));
-    own = r < a.n_seqs ? count(seq) : 0;
+  __device__ __forceinline__ Items(const Kv16AttnArgs& a_, const Count& count_) : a(a_), count(count_) {
+    each = (unsigned)(a.n_seqs + 63) / 64;
+    own = 0;
+#pragma unroll 4
+    for (int i = 0; i < each; ++i) own += look(i * 64 + (threadIdx.x & 63));
     upto = sum_upto(own);
   }
-  // The sequence of the `*item`th piece, which becomes its number among the sequence's own; -1 where there are fewer.
+  __device__ __forceinline__ int look(int r) {
+    seq = find_seq(a, min(r, a.n_seqs - 1));
+    return r < a.n_seqs ? count(seq) : 0;
+  }
+  __device__ __forceinline__ int all() const { return __builtin_amdgcn_readlane(upto, 63); }
+  // The sequence of the `*item`th piece, below all(), which becomes its number among the sequence's own.
   __device__ __forceinline__ int find(int* item, Seq* s) {
-    for (int first = 0; first < a.n_seqs; first += 64) {
-      if (a.n_seqs > 64) load(first);
-      const unsigned long long behind = __ballot(upto > *item);
-      if (behind) {
-        const int at = __builtin_amdgcn_readfirstlane(__ffsll(behind) - 1);
-        const auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
-        *item = __builtin_amdgcn_readfirstlane(*item - of(upto - own));
-        *s = {(long)((uint64_t)(uint32_t)of((int)seq.row0) | (uint64_t)of((int)(seq.row0 >> 32)) << 32), of(seq.before),
-              of(seq.nq), of(seq.len), of(seq.lq)};
-        return __builtin_amdgcn_readfirstlane(first + at);
+    int at = first_above(upto, *item), r = at, left = *item - __builtin_amdgcn_readlane(upto - own, at);
+    if (each > 1) {
+      const int first = at, lane = threadIdx.x & 63;
+      for (int i = 0;; i += 64) {
+        const int mine = i + lane < each ? look((i + lane) * 64 + first) : 0, so_far = sum_upto(mine);
+        if (left < __builtin_amdgcn_readlane(so_far, 63)) {
+          at = first_above(so_far, left);
+          left -= __builtin_amdgcn_readlane(so_far - mine, at);
+          r = (i + at) * 64 + first;
+          break;
+        }
+        left -= __builtin_amdgcn_readlane(so_far, 63);
       }
-      *item -= __builtin_amdgcn_readlane(upto, 63);
     }
-    return -1;
+    const auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
+    *item = __builtin_amdgcn_readfirstlane(left);
+    *s = {(long)((uint64_t)(uint32_t)of((int)seq.row0) | (uint64_t)of((int)(seq.row0 >> 32)) << 32), of(seq.before),
+          of(seq.nq), of(seq.len), of(seq.lq)};
+    return __builtin_amdgcn_readfirstlane(r);
+  }
+  // The first lane whose v is above x, where some lane's is
+  __device__ __forceinline__ static int first_above(int v, int x) {
+    return __builtin_amdgcn_readfirstlane(__ffsll(__ballot(v > x)) - 1);
   }
 };
 

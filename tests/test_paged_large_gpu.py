@@ -163,3 +163,35 @@ def test_a_page_table_that_changes_between_replays():
         rows = sum(news[i])
         assert torch.equal(out[:rows], want[:rows]) and torch.equal(lse[:rows], want_lse[:rows])
         check_on_gpu(cache, q, lens[i], t.cpu().numpy(), news[i], out, lse, range(3))
+
+
+@pytest.mark.parametrize("mixed", [False, True])
+def test_bounds_far_above_the_lengths(mixed):
+    """A page table and max_len for 65,536 tokens: as with bounds that fit, bit for bit; fewer workgroups than places."""
+    torch, B = lib()
+    rng = np.random.default_rng(360)
+    new = [int(x) for x in rng.choice([1, 1, 3, 80] if mixed else [1, 2], 150)]
+    lens = [n + int(x) for n, x in zip(new, rng.choice([0, 60, 900, 1500, 2600], 150))]
+    cache, table = random_cache("bfloat16", lens, 16, 2, 64, 361)
+    far = np.full((150, 4096), -1)
+    far[:, :table.shape[1]] = table
+    q = make(torch, (sum(new), 8, 64), torch.bfloat16, 362)
+    n, c = i32(torch, lens), i32(torch, cu(new))
+    want = cache.attention(q, n, i32(torch, table), c, max(new), max(lens), with_lse=True)
+    got = cache.attention(q, n, i32(torch, far), c, max(new), with_lse=True)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    check_on_gpu(cache, q, lens, table, new, *got, range(0, 150, 9))
+
+
+def test_more_runs_than_workgroups():
+    """300 sequences of 8 key heads in three runs each: workgroups take several."""
+    torch, B = lib()
+    lens = [1100 + 3 * i % 400 for i in range(300)]
+    cache, table = random_cache("float16", lens, 64, 8, 64, 370)
+    q = make(torch, (300, 16, 64), torch.float16, 371)
+    n, t = i32(torch, lens), i32(torch, table)
+    out, lse = cache.attention(q, n, t, with_lse=True)
+    check_on_gpu(cache, q, lens, table, [1] * 300, out, lse, range(0, 300, 23))
+    for r in (0, 150, 299):
+        one, one_lse = cache.attention(q[r:r + 1], n[r:r + 1], t[r:r + 1].contiguous(), with_lse=True)
+        assert torch.equal(one, out[r:r + 1]) and torch.equal(one_lse, lse[r:r + 1])
