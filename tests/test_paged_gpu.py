@@ -247,6 +247,34 @@ def test_append_at_the_places_of_tokens():
         assert all(torch.equal(a, b) for a, b in zip(want[0], other))
 
 
+@pytest.mark.parametrize("n,most", [(1, 9), (63, 2), (64, 1), (65, 3), (130, 1), (4096, 1), (4097, 4), (9000, 2)])
+def test_append_finds_the_sequence_of_a_row(n, most):
+    """Batches of few and of many sequences, runs of empty ones among them, at the ends too: every row in its place."""
+    torch, B = lib()
+    rot, _ = plan_of(B, (32,), 1e4)
+    rng = np.random.default_rng(n)
+    for case, new in enumerate((rng.integers(0, most + 1, n), np.where(rng.random(n) < 0.02, most, 0),
+                                np.where(np.arange(n) == n // 2, most, 0))):
+        rows = int(new.sum())
+        if rows == 0:
+            continue
+        print("[sequence of a row] %d sequences, case %d, %d rows" % (n, case, rows), flush=True)
+        held, pages = rng.integers(0, 16 - most, n), rng.permutation(n)
+        cache = B.Kv16Cache.empty(n, 1, 64, 16)
+        cache.k.zero_(), cache.v.zero_()
+        k, v, q = (make(torch, (rows, 1, 64), torch.bfloat16, 50 + i) for i in range(3))
+        out = cache.append(k, v, i32(torch, held), i32(torch, pages[:, None]), cu_new=i32(torch, cu(new)), max_new=most,
+                           rotary=rot, q=q)
+        seq = np.repeat(np.arange(n), new)
+        place = np.concatenate([np.arange(a, a + b) for a, b in zip(held, new)])
+        turned_q, turned_k = rot.rows(q, i32(torch, place), k)
+        assert torch.equal(out, turned_q)
+        want_k, want_v = torch.zeros_like(cache.k), torch.zeros_like(cache.v)
+        at = i32(torch, pages[seq]).long(), i32(torch, place).long()
+        want_k[at[0], 0, at[1]], want_v[at[0], 0, at[1]] = turned_k[:, 0], v[:, 0]
+        assert torch.equal(cache.k, want_k) and torch.equal(cache.v, want_v)
+
+
 def test_append_drops_what_has_no_place():
     torch, B = lib()
     rot, _ = plan_of(B, (32,), 1e4)
