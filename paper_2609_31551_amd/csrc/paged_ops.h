@@ -127,8 +127,10 @@ __device__ __forceinline__ int sum_upto(int v) {
   return v;
 }
 
-// Pieces of work of a launch that sequence r has count(its Seq) of, in an order of the sequences.  Each wave goes over
-// the sequences by itself: lane i over i, i + 64, .. one after the other, and, to find one, the wave over a lane's.
+// Pieces of work of a launch that sequence r has count(its Seq) of, in an order of the sequences: lane i of a wave goes
+// over i, i + 64, .. one after the other, and, to find one, the wave over a lane's.  Of more than 64 sequences the waves
+// of the workgroup, all of which come here together, take a share each (1,024 of 2,048 tokens, 4 heads, 4,096 allowed:
+// 914 us, each wave over all 1,060; 4,096 of them 4.3 and 7.4 ms; a chunk of 512 beside 255 single tokens 159 and 197 us).
 template <class Count>
 struct Items {
   const Kv16AttnArgs& a;
@@ -139,9 +141,19 @@ struct Items {
 
   __device__ __forceinline__ Items(const Kv16AttnArgs& a_, const Count& count_) : a(a_), count(count_) {
     each = (unsigned)(a.n_seqs + 63) / 64;
-    own = 0;
-#pragma unroll 4
-    for (int i = 0; i < each; ++i) own += look(i * 64 + (threadIdx.x & 63));
+    if (each == 1) {
+      own = look(threadIdx.x & 63);
+    } else {
+      __shared__ int shares[8][64];   // a later one's are written behind a barrier of the caller's
+      const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+      own = 0;
+#pragma unroll 2
+      for (int i = wave; i < each; i += waves) own += look(i * 64 + lane);
+      shares[wave][lane] = own;
+      __syncthreads();
+      own = 0;
+      for (int w = 0; w < waves; ++w) own += shares[w][lane];
+    }
     upto = sum_upto(own);
   }
   __device__ __forceinline__ int look(int r) {

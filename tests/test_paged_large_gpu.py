@@ -195,3 +195,34 @@ def test_more_runs_than_workgroups():
     for r in (0, 150, 299):
         one, one_lse = cache.attention(q[r:r + 1], n[r:r + 1], t[r:r + 1].contiguous(), with_lse=True)
         assert torch.equal(one, out[r:r + 1]) and torch.equal(one_lse, lse[r:r + 1])
+
+
+@pytest.mark.parametrize("kind,n", [("wide", 65), ("wide", 130)] + [(k, n) for k in ("tokens", "guesses", "mixed")
+                                                                    for n in (65, 129, 577, 1100)])
+def test_waves_share_the_lengths_of_many_sequences(kind, n):
+    """More sequences than a wave has lanes, split ones at the ends and between, in each kind of launch: the last lane's
+    share, lanes without any, and results that are those of the sequence alone, bit for bit."""
+    torch, B = lib()
+    rng = np.random.default_rng(n)
+    new = [int(x) for x in {"tokens": rng.choice([1], n), "guesses": rng.choice([0, 1, 3], n),
+                            "mixed": rng.choice([0, 1, 1, 30], n), "wide": rng.choice([0, 1, 1, 3], n)}[kind]]
+    lens = [x + int(y) for x, y in zip(new, rng.choice([0, 5, 90], n))]
+    split = [0, 1, 63, 64, n // 2, n - 2, n - 1]
+    for i, r in enumerate(split):
+        new[r] = {"tokens": 1, "guesses": 1 + i % 3, "mixed": (1, 40, 200)[i % 3], "wide": 1 if i % 2 else 50 * n}[kind]
+        lens[r] = new[r] + 1500 + 100 * i
+    cache, table = random_cache("bfloat16", lens, 64, 2, 64, 380)
+    q = make(torch, (sum(new), 16, 64), torch.bfloat16, 381)
+    if kind == "wide":
+        assert sum(new) * 16 >= 256 * 256 and sum(new) * 8 >= 1024 * n
+    print("[shares] %s, %d sequences" % (kind, n), flush=True)
+    t, c = i32(torch, table), cu(new)
+    bounds = (None, None) if kind == "tokens" else (i32(torch, c), max(new))
+    out, lse = cache.attention(q, i32(torch, lens), t, *bounds, max(lens), with_lse=True)
+    some = sorted(set(split) | set(range(0, n, n // 12)))
+    for r in some:
+        a = slice(c[r], c[r + 1])
+        if new[r]:
+            one, one_lse = cache.attention(q[a], i32(torch, lens[r:r + 1]), t[r:r + 1].contiguous(), with_lse=True)
+            assert torch.equal(one, out[a]) and torch.equal(one_lse, lse[a]), r
+    check_on_gpu(cache, q, lens, table, new, out, lse, [r for r in some if 0 < new[r] <= 200])
