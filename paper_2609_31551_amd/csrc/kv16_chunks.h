@@ -10,7 +10,7 @@
 // pages that are not held are masked like tokens behind a query's own (their DMA reads page 0).
 //
 // Bound by the matrix units, 4 * head_dim flops for each visible (row, token) pair: 4,096 tokens of 28 heads over 4 behind
-// 32,768, 2,044 GFLOP, take 1,830 - 1,880 us, 1,087 - 1,117 TFLOP/s (prompt attention over the same rows 1,914), the units
+// 32,768, 2,044 GFLOP, take 1,830 - 1,920 us, 1,064 - 1,117 TFLOP/s (prompt attention over the same rows 1,914), the units
 // 51% busy at 2.0 GHz: 448 workgroups on 256 CUs leave an eighth of the time to half of them.  Chunks of 512 to 1,024
 // tokens over up to 6,001 beside single tokens, 88 GFLOP, 132 us: the longest walk, 48 tiles, and the join.
 #pragma once
