@@ -64,10 +64,18 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 // M0 carries the LDS base of each DMA; nothing else in these kernels uses M0
 // (checked in the generated code), so setting it here cannot disturb the
 // compiler's own code even though it treats M0 as reserved.
+// A base that the compiler takes back from a lane that it had put it aside in (RESTORED)
+// may be read by a memory instruction five wait states later; it keeps that for its own
+// instructions and does not see this one.
 #pragma clang diagnostic ignored "-Winline-asm"
+template <bool RESTORED = false>
 __device__ __forceinline__ void dma16(unsigned lds_addr, unsigned voff, const void* gbase) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n"
-               :: "s"(lds_addr), "v"(voff), "s"(gbase) : "memory", "m0");
+  if constexpr (RESTORED)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2\n"
+                 :: "s"(lds_addr), "v"(voff), "s"(gbase) : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n"
+                 :: "s"(lds_addr), "v"(voff), "s"(gbase) : "memory", "m0");
 }
 template <int N> __device__ __forceinline__ void wait_vm() {
   static_assert(N >= 0 && N < 64, "vmcnt range");
@@ -747,8 +755,9 @@ __global__ __launch_bounds__(64 * WGM * WGN) void gemm_bf16_async_kernel(GemmArg
   // with the rotary epilogue, the (t, h, w) positions of the wave's 64 rows -> slab bytes [1024, 2048)
   auto issue_bias = [&](int n0, int m0) {
     const int n = a.bias ? min(n0 + wn * C::WN + (lane % (C::WN / 8)) * 8, a.N - 8) : 0;
-    dma16(slab_lds, (unsigned)(n * 2), bias);
-    if constexpr (ROPE) dma16(slab_lds + 1024, (unsigned)(min(m0 + wm * C::WM + lane, a.M - 1) * 16), a.rope_pos);
+    // once a tile, and the bases of the rotary forms are put aside over the k-loop
+    dma16<true>(slab_lds, (unsigned)(n * 2), bias);
+    if constexpr (ROPE) dma16<true>(slab_lds + 1024, (unsigned)(min(m0 + wm * C::WM + lane, a.M - 1) * 16), a.rope_pos);
   };
 
   const int lrow = lane & 31, g = lane >> 5, swz = C::sw(lrow);
