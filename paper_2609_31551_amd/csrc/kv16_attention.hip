@@ -416,7 +416,8 @@ __global__ __launch_bounds__(64 * NW, 2) void kv16_mixed_kernel(Kv16AttnArgs a) 
 // four times as many, each for every fourth run, and their four sums in order (a sequence of 16,384 tokens in 64 runs
 // 20 us, joined one run after the other 55).  DIRECT: a.items workgroups for each sequence; else they go over the split
 // rows of the batch in strides, as only the sequences' lengths say how many there are, which takes 2 - 3 us more but no
-// workgroup for rows that are not split.
+// workgroup for rows that are not split.  The runs' results are means of values that may be as large as bf16's largest, so
+// their weights, which sum to 64 at most, are taken by 2^-6: the sum stays in fp32's range, and its bits are the same.
 template <class T, int D, bool DIRECT>
 __global__ __launch_bounds__(256) void kv16_join_kernel(Kv16AttnArgs a) {
   constexpr int L = D / 4, GROUPS = 256 / L;
@@ -467,7 +468,7 @@ __global__ __launch_bounds__(256) void kv16_join_kernel(Kv16AttnArgs a) {
 #pragma unroll 8
     for (int k = slice; k < runs; k += slices) {
       const f32x4 x = *reinterpret_cast<const f32x4*>(a.part + (slot + (long)k * all) * D + in * 4);
-      const float wk = __builtin_amdgcn_exp2f(a.part_lse[slot + (long)k * all] - base);
+      const float wk = __builtin_amdgcn_exp2f(a.part_lse[slot + (long)k * all] - base) * 0x1p-6f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum[e] = fmaf(wk, x[e], sum[e]);
     }
@@ -478,7 +479,7 @@ __global__ __launch_bounds__(256) void kv16_join_kernel(Kv16AttnArgs a) {
       for (int k = 1; k < 4; ++k) sum += sums[turn][(sub + k) % GROUPS][in];   // slice 0's: of slices 1, 2, 3
     }
     if (slice || row >= all) continue;
-    const float inv = W == 0.0f ? 0.0f : 1.0f / W;
+    const float inv = W == 0.0f ? 0.0f : 1.0f / W * 0x1p6f;
     typedef T Tx4 __attribute__((ext_vector_type(4)));
     Tx4 y;
 #pragma unroll
