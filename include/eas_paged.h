@@ -117,8 +117,8 @@ eas_status eas_kv16_append(const eas_kv16_cache* cache, const eas_rotary* rotary
  * stand.
  * A key's score of -inf, +inf or NaN and a value's infinities do what they do in
  * eas_prompt_attention, and what a query does not see never reaches its result.
- * Sums and the softmax are held in fp32, probabilities are rounded to the element
- * type for the product with v.
+ * Sums and the softmax are held in fp32, in whose range they stay for all finite
+ * values; probabilities are rounded to the element type for the product with v.
  * A sequence's result does not depend on the other sequences, on max_q and
  * max_len that hold for it, or on which pages hold its tokens, to the bit.
  * workspace: device, 16-byte aligned, at least the bytes that

@@ -171,8 +171,9 @@ __device__ __forceinline__ void many_rows(const Kv16AttnArgs& a, int block, char
   const int ri = row0 + l32, qi = query(ri);
   char* stage = smem + wave * 32 * HD * 2;
   f32x16* o = walk.o;
-  float m = walk.m, l = walk.l;
+  float m = walk.m, l = walk.l, lift = 1.0f;
   if (any_not_finite<C::HB>(o)) {
+    lift = careful_lift<T>;
     const auto page_of = [&](int i) { return table[i >> a.c.page_shift]; };
     careful_rows<T, HD>(
         qf, [&](long i) { return static_cast<const T*>(a.c.k) + token_offset(a, page_of((int)i), kvh, (int)i, HD); },
@@ -186,7 +187,7 @@ __device__ __forceinline__ void many_rows(const Kv16AttnArgs& a, int block, char
         s.len, tb, tb + nt_w, a.scale_log2, stage, o, &m, &l);
   }
   l += __shfl_xor(l, 32, 64);
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l, lse2 = l == 0.0f ? -INFINITY : m + __log2f(l);
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l, lse2 = l == 0.0f ? -INFINITY : m + __log2f(l * lift);
   if (runs > 1) {
     const long slot = first_slot(a, s, r) + ((long)run * a.c.kv_heads + kvh) * rows + ri;   // a wave's are consecutive
     if (ri < rows) {

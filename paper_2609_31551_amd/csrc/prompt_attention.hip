@@ -184,14 +184,16 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
   if (qw >= lq) return;
   char* stage = smem + wave * 32 * HD * 2;
   f32x16* o = walk.o;
-  float m = walk.m, l = walk.l;
-  if (a.causal && any_not_finite<C::HB>(o))
+  float m = walk.m, l = walk.l, lift = 1.0f;
+  if (a.causal && any_not_finite<C::HB>(o)) {
+    lift = careful_lift<T>;
     careful_rows<T, HD>(
         qf, [&](long i) { return kp + i * a.ks.row; }, [&](long i) { return vp + i * a.vs.row; },
         [&](int i) { return i >= sees; }, [&](int t) { return (t + 1) * KT <= fewest; }, lk, tb, tb + nt_w, a.scale_log2,
         stage, o, &m, &l);
+  }
   l += __shfl_xor(l, 32, 64);
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l, lse2 = l == 0.0f ? -INFINITY : m + __log2f(l);
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l, lse2 = l == 0.0f ? -INFINITY : m + __log2f(l * lift);
   if (runs > 1) {
     const long slot = w.slot0[r] + ((long)run * a.heads + h) * lq + qi;   // [run, head, query]: a wave's are consecutive
     if (qi < lq) {

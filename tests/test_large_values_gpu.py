@@ -1,5 +1,5 @@
-"""Values near the largest that bf16 holds: a result is a mean of values, so it is finite wherever they are in however
-many runs.  What is held on the way are sums of weighted values, over all tokens of a run
+"""Values near the largest that bf16 holds: a result is a mean of values, so it is finite wherever they are, whichever kernel
+takes the sequence and in however many runs.  What is held on the way are sums of weighted values, over all tokens of a run
 and over all runs.
 
 Tolerances.  Equal values c of a dimension: the weights are rounded to the element type, their sum is not, so the result is
@@ -23,12 +23,13 @@ def columns(torch, dim, size=2.0 ** 127):
     return want
 
 
-# (new tokens, tokens): whole and in runs
+# (new tokens, tokens): whole and in runs, of the kernel for few rows of a key head and of that for many
 FEW = [(1, 1023), (1, 32768), (3, 70000), (5, 3000)]
+MANY = [(40, 70), (70, 70), (300, 700), (1024, 5000), (64, 4096), (300, 33000)]
 
 
 @pytest.mark.parametrize("dim", [64, 128])
-@pytest.mark.parametrize("new,length", FEW)
+@pytest.mark.parametrize("new,length", FEW + MANY)
 def test_paged_attention_of_equal_values(new, length, dim):
     torch, _ = lib()
     cache, table = random_cache("bfloat16", [length], 128, 1, dim, 400)
@@ -41,7 +42,7 @@ def test_paged_attention_of_equal_values(new, length, dim):
             assert ((out.double() / want.double() - 1).abs() <= TOL).all(), (size, causal)
 
 
-@pytest.mark.parametrize("new,length", FEW)
+@pytest.mark.parametrize("new,length", FEW + MANY)
 def test_paged_attention_of_large_values(new, length):
     """Random ones, of up to 2^128 (5.6 deviations), and what is hidden among them."""
     torch, _ = lib()
@@ -53,7 +54,7 @@ def test_paged_attention_of_large_values(new, length):
     check_on_gpu(cache, q, [length], table, [new], out, lse, [0])
 
 
-@pytest.mark.parametrize("new", [1, 8])
+@pytest.mark.parametrize("new", [1, 40, 300])
 def test_the_size_of_values_does_not_change_what_is_made_of_them(new):
     """Powers of two apart, results are powers of two apart, bit for bit, as long as no sum leaves fp32's range."""
     torch, _ = lib()
