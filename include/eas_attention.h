@@ -62,7 +62,8 @@ typedef struct {
  * last Lq of the Lk tokens) or every key (full):
  *   out[i, h] = sum_j p_j v[j, h'],  p = softmax_j(scale * q[i, h] . k[j, h']).
  * A query that sees no key gets zeros.  Sums and the softmax are held in fp32,
- * probabilities are rounded to the element type for the product with v.
+ * probabilities are rounded to the element type for the product with v.  (Full:
+ * sums of bf16 values from 2^119 on may leave fp32's range; causal ones stay in it.)
  * cu_q, cu_k: host, [n_seqs + 1] prefix sums from 0, not decreasing, equal
  * neighbours allowed; cu_k NULL = cu_q.  0 <= n_seqs <= EAS_MAX_SEQS.
  * lse: device fp32 [cu_q[n_seqs], heads] or NULL: the natural logarithm of each

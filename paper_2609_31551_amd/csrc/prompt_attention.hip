@@ -22,7 +22,7 @@ namespace eas {
 namespace {
 
 constexpr int kMaxRows = 1 << 30;    // queries or keys of a call
-constexpr int MAX_RUNS = 16;         // runs that a sequence's keys are split into
+constexpr int MAX_RUNS = 16;         // runs that a sequence's keys are split into, a power of two
 
 // Runs of keys that each query tile of a sequence is split into, a workgroup each, where the sequence alone leaves CUs
 // without one: of 4,096 keys at least, or fewer where it has less than 128 workgroups without, down to 1,024 with 32.
@@ -229,7 +229,8 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a, Prompt
   }
 }
 
-// Joins the runs of the split sequences, in order.
+// Joins the runs of the split sequences, in order.  Their weights, which sum to MAX_RUNS at most, are taken by 1 / MAX_RUNS:
+// the sum of results as large as bf16's largest stays in fp32's range, and its bits are the same.
 struct JoinWork {
   int n;
   int seq[kMaxSeqs], row0[kMaxSeqs + 1];   // split sequences, prefix sums of their queries
@@ -252,7 +253,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, PromptWo
 #pragma unroll 4
   for (int k = 0; k < runs; ++k) {
     const f32x4 x = *reinterpret_cast<const f32x4*>(a.part + (slot + k * step) * HD + d);
-    const float wk = __builtin_amdgcn_exp2f(a.part_lse[slot + k * step] - base);
+    const float wk = __builtin_amdgcn_exp2f(a.part_lse[slot + k * step] - base) * (1.0f / MAX_RUNS);
     W += wk;
 #pragma unroll
     for (int e = 0; e < 4; ++e) sum[e] = fmaf(wk, x[e], sum[e]);
@@ -263,7 +264,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a, PromptWo
 #pragma unroll
   for (int e = 0; e < 4; ++e) y[e] = (T)(sum[e] * inv);
   *reinterpret_cast<Tx4*>(static_cast<T*>(a.out) + (w.cu_q[r] + i) * a.os.row + h * a.os.head + d) = y;
-  if (d == 0 && a.lse) a.lse[(long)(w.cu_q[r] + i) * a.heads + h] = W == 0.0f ? -INFINITY : (M + __log2f(W)) * kLn2;
+  if (d == 0 && a.lse) a.lse[(long)(w.cu_q[r] + i) * a.heads + h] = W == 0.0f ? -INFINITY : (M + __log2f(W * MAX_RUNS)) * kLn2;
 }
 
 template <class T, int HD, int NW>

@@ -67,3 +67,17 @@ def test_the_size_of_values_does_not_change_what_is_made_of_them(new):
         out, lse = cache.attention(q, n, t, with_lse=True)
         cache.v.mul_(2.0 ** -power)
         assert torch.equal(out.double(), want.double() * 2.0 ** power) and torch.equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("queries,keys", [(1, 500), (300, 300), (700, 700), (64, 5000), (1, 70000), (300, 33000), (2000, 2000)])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_causal_prompt_attention_of_equal_values(queries, keys, dim):
+    torch, _ = lib()
+    from paper_2609_31551_amd import attention as A
+    want = columns(torch, dim)
+    k = make(torch, (keys, 1, dim), torch.bfloat16, 430)
+    v = want.to(torch.bfloat16).expand(keys, 1, dim).contiguous()
+    for size in (0.0, 1.0):
+        q = make(torch, (queries, 4, dim), torch.bfloat16, 431, size)
+        out, _ = A.prompt_attention(q, k, v, [0, queries], [0, keys])
+        assert ((out.double() / want.double() - 1).abs() <= TOL).all(), size
