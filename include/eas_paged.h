@@ -120,7 +120,8 @@ eas_status eas_kv16_append(const eas_kv16_cache* cache, const eas_rotary* rotary
  * Sums and the softmax are held in fp32, in whose range they stay for all finite
  * values; probabilities are rounded to the element type for the product with v.
  * A sequence's result does not depend on the other sequences, on max_q and
- * max_len that hold for it, or on which pages hold its tokens, to the bit.
+ * max_len that hold for it, on which pages hold its tokens, or on what is in
+ * places of the cache that hold none of them, to the bit.
  * workspace: device, 16-byte aligned, at least the bytes that
  * eas_kv16_attention_workspace gives for the same arguments (0: NULL is fine);
  * calls that may overlap, captured ones included, need one each.  Nothing in it

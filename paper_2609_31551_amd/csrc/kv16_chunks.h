@@ -6,8 +6,9 @@
 // group.  The walk over the tokens is prompt attention's (attention_tiles.h); what differs is where a tile comes from:
 // its 64 tokens lie in one to four pages.  A DMA instruction moves 4 or 8 tokens, which no page's border parts, so its
 // page is one scalar; the page numbers of a tile are one load, a tile ahead of the DMA that goes by them, and their
-// addresses one vector computation (each by itself in scalars: 4,096 tokens over 32,768 2,105 us, so 1,982).  Tiles of
-// pages that are not held are masked like tokens behind a query's own (their DMA reads page 0).
+// addresses one vector computation (each by itself in scalars: 4,096 tokens over 32,768 2,105 us, so 1,982).  Tokens of
+// pages that are not held are masked like those behind a query's own; their DMA reads zeros, as a weight of 0 does not hide
+// an infinity or a NaN, and a page of the cache would be another sequence's.
 //
 // Bound by the matrix units, 4 * head_dim flops for each visible (row, token) pair: 4,096 tokens of 28 heads over 4 behind
 // 32,768, 2,044 GFLOP, take 1,830 - 1,920 us, 1,064 - 1,117 TFLOP/s (prompt attention over the same rows 1,914), the units
@@ -77,25 +78,28 @@ __device__ __forceinline__ void many_rows(const Kv16AttnArgs& a, int block, char
   const auto held_parts = [&](int pages) { return (int)(__ballot(held_page(a, pages)) & 15); };
   // bytes before the part's first token in the cache
   const auto offset_of = [&](int t, int pages) { return token_offset(a, pages, kvh, token_of(t), HD) * 2; };
-  const auto fetch = [&](const void* base, int t, long offset, int lds_off) {
+  const auto fetch = [&](const void* base, int t, long offset, int held, int lds_off) {
     const uint64_t from = (uint64_t)(uintptr_t)base + offset;
     const int lo = (int)from, hi = (int)(from >> 32);
-    const auto go = [&](int j, unsigned voff) {
+    const auto go = [&](int j, unsigned voff, auto whole) {
       const int part = part0 + j * PARTS;
       const uint32_t at[2] = {(uint32_t)__builtin_amdgcn_readlane(lo, part), (uint32_t)__builtin_amdgcn_readlane(hi, part)};
-      dma16<true>(lds0 + lds_off + (wave + NW * j) * 1024, voff, (const void*)(uintptr_t)(at[0] | (uint64_t)at[1] << 32));
+      const void* tokens = (const void*)(uintptr_t)(at[0] | (uint64_t)at[1] << 32);
+      if (!decltype(whole)::value && !(held >> part & 1)) tokens = absent_tokens;
+      dma16<true>(lds0 + lds_off + (wave + NW * j) * 1024, voff, tokens);
     };
-    if ((tb + t + 1) * KT <= s.len) {
+    if ((tb + t + 1) * KT <= s.len && held == 15) {
 #pragma unroll
-      for (int j = 0; j < C::NDMA; ++j) go(j, part_row * (HD * 2) + dcol);
+      for (int j = 0; j < C::NDMA; ++j) go(j, part_row * (HD * 2) + dcol, std::integral_constant<bool, true>{});
     } else {   // rows behind the last token read it again
 #pragma unroll
       for (int j = 0; j < C::NDMA; ++j)
-        go(j, min(part_row, max(last - ((tb + t) * KT + 16 * (part0 + j * PARTS)), 0)) * (HD * 2) + dcol);
+        go(j, min(part_row, max(last - ((tb + t) * KT + 16 * (part0 + j * PARTS)), 0)) * (HD * 2) + dcol,
+           std::integral_constant<bool, false>{});
     }
   };
-  const auto fetch_k = [&](int t, long offset) { fetch(a.c.k, t, offset, (t & 1) * C::TILE); };
-  const auto fetch_v = [&](int t, long offset) { fetch(a.c.v, t, offset, (2 + (t & 1)) * C::TILE); };
+  const auto fetch_k = [&](int t, long offset, int held) { fetch(a.c.k, t, offset, held, (t & 1) * C::TILE); };
+  const auto fetch_v = [&](int t, long offset, int held) { fetch(a.c.v, t, offset, held, (2 + (t & 1)) * C::TILE); };
 
   TileWalk<T, HD, NW> walk(smem, qf, a.scale_log2);
   constexpr std::integral_constant<bool, true> yes{};
@@ -112,8 +116,8 @@ __device__ __forceinline__ void many_rows(const Kv16AttnArgs& a, int block, char
     asm volatile("" : "+v"(pages));   // so are the page numbers: taken here, as a wait behind the DMA would be for it, too
     const long next = offset_of(t + 2, pages);
     parts = parts1, parts1 = parts2, parts2 = held_parts(pages);
-    if (t + 1 < nt) fetch_v(t + 1, offset);
-    if (t + 2 < nt) fetch_k(t + 2, next);
+    if (t + 1 < nt) fetch_v(t + 1, offset, parts1);
+    if (t + 2 < nt) fetch_k(t + 2, next, parts2);
     offset = next;
     pages = pages_of(t + 3);
   };
@@ -130,9 +134,9 @@ __device__ __forceinline__ void many_rows(const Kv16AttnArgs& a, int block, char
     parts1 = held_parts(pages0), parts2 = held_parts(pages1);   // of tiles 0 and 1
     const long offset0 = offset_of(0, pages0);
     offset = offset_of(1, pages1);
-    fetch_k(0, offset0);
-    fetch_v(0, offset0);
-    if (nt > 1) fetch_k(1, offset);
+    fetch_k(0, offset0, parts1);
+    fetch_v(0, offset0, parts1);
+    if (nt > 1) fetch_k(1, offset, parts2);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     // the queries are taken here, so that no wait for them is left to the loop, where it would wait for a tile
 #pragma unroll

@@ -109,6 +109,8 @@ __device__ __forceinline__ int runs_of(const Kv16AttnArgs& a, const Seq& s) {
 __device__ __forceinline__ long first_slot(const Kv16AttnArgs& a, const Seq& s, int r) {
   return a.slots ? r * a.slots : s.row0 * a.heads * a.most_runs;
 }
+// 16 tokens of a page that is not held
+__device__ const uint4 absent_tokens[16 * 128 * 2 / 16] = {};
 __device__ __forceinline__ bool held_page(const Kv16AttnArgs& a, int page) { return page >= 0 && page < a.c.n_pages; }
 // Offset of token t of a key / value head in the cache, `page` its page's number (one that is not held: page 0's)
 __device__ __forceinline__ long token_offset(const Kv16AttnArgs& a, int page, int kvh, int t, int dim) {
