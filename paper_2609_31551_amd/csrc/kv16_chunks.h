@@ -228,12 +228,14 @@ __device__ __forceinline__ void many_rows(const Kv16AttnArgs& a, int block, char
   }
 }
 
-// Row tiles of all sequences, and their runs: a bound of what many_rows() has to do.  A sequence that is split has at
-// most MANY_FILL workgroups, whatever its heads.
+// Row tiles of all sequences, and their runs: a bound of what many_rows() has to do.  A sequence that comes here has more
+// than FEW_ROWS rows, but for one that the rows' beginning cuts, and one that their end does; one that is split has at most
+// MANY_FILL workgroups, whatever its heads.
 template <int HD, int NW>
 inline int64_t many_items(const Kv16AttnArgs& a) {
   constexpr int QT = Cfg<HD, NW>::QT;
-  const int64_t rows = (int64_t)a.n_rows * (a.heads / a.c.kv_heads), seqs = a.n_seqs < a.n_rows ? a.n_seqs : a.n_rows;
+  const int64_t rows = (int64_t)a.n_rows * (a.heads / a.c.kv_heads), by_rows = rows / (FEW_ROWS + 1) + 2;
+  const int64_t some = a.n_seqs < a.n_rows ? a.n_seqs : a.n_rows, seqs = some < by_rows ? some : by_rows;
   const int64_t tiles = (rows + QT - 1) / QT + seqs, runs = many_runs(a.max_len, 1, a.c.kv_heads);
   const int64_t split = tiles + seqs * (MANY_FILL / a.c.kv_heads);
   return runs == 1 ? tiles : tiles * runs < split ? tiles * runs : split;
