@@ -46,11 +46,12 @@ typedef struct {
   uint8_t axis[EAS_MAX_ROTARY_PAIRS];
 } eas_rotary;
 
-/* freqs: [pairs] radians for one position, finite; axis: [pairs], each in
- * [0, axes), or NULL (0 for all).  A turn is kept to 2^-64 of a whole one, so
- * that positions multiply it exactly, modulo whole turns: angles are good to
- * about 2^-24 at any position of 32 bits.  Host only.
- * Errors: INVALID_ARG, UNSUPPORTED (pairs, axes). */
+/* freqs: [pairs] radians for one position, finite, less than 2^60 either way;
+ * axis: [pairs], each in [0, axes), or NULL (0 for all).  A turn is kept to the
+ * nearest 2^-64 of a whole one, so that positions multiply it exactly, modulo
+ * whole turns: angles are good to about 2^-23 radians at any position of 32
+ * bits.  Host only.
+ * Errors: INVALID_ARG, UNSUPPORTED (pairs, axes, frequencies from 2^60 on). */
 eas_status eas_rotary_make(const double* freqs, const int32_t* axis, int32_t pairs, int32_t axes, int32_t adjacent,
                            eas_rotary* rotary);
 

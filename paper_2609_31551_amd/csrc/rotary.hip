@@ -217,6 +217,23 @@ eas_status check_rotary(const eas_rotary* r, int32_t head_dim) {
   return 2 * r->pairs <= head_dim ? EAS_OK : EAS_ERR_INVALID_ARG;
 }
 
+// The turns of f radians, |f| < 2^60, modulo whole ones and to the nearest 2^-64: f is m 2^e with a whole m below 2^53, and
+// m / (2 pi) is a whole number of 2^-128ths, m times those of 1 / (2 pi).  What these leave out is below 2^-68 of a turn.
+uint64_t step_of(double f) {
+  typedef unsigned __int128 u128;
+  int e;
+  const uint64_t m = (uint64_t)ldexp(frexp(fabs(f), &e), 53);
+  const u128 low = (u128)m * 0x7f09d5f47d4d3770u, high = (u128)m * 0x28be60db9391054au + (low >> 64);
+  const uint64_t rest = (uint64_t)low;
+  const int n = 64 - (e - 53);   // bits below 2^-64 of a turn, 57 at least
+  uint64_t step = 0;
+  if (n < 64)
+    step = ((uint64_t)(high << (64 - n)) | rest >> n) + (rest >> (n - 1) & 1);
+  else if (n < 192)
+    step = (uint64_t)(high >> (n - 64)) + (n == 64 ? rest >> 63 : (uint64_t)(high >> (n - 65)) & 1);
+  return f < 0 ? 0 - step : step;
+}
+
 // What is rotated from x to out: rows of `heads` heads; out may be x
 eas_status check_rows(const void* x, const eas_strides& xs, const void* out, const eas_strides& os, int64_t rows,
                       int32_t heads, int32_t dim) {
@@ -239,11 +256,8 @@ extern "C" eas_status eas_rotary_make(const double* freqs, const int32_t* axis, 
   for (int i = 0; i < pairs; ++i) {
     const int a = axis ? axis[i] : 0;
     if (a < 0 || a >= axes || !std::isfinite(freqs[i])) return EAS_ERR_INVALID_ARG;
-    // 64 bits of a fraction need long double's 64: turns modulo whole ones, to the nearest 2^-64
-    const long double turns = (long double)freqs[i] / 6.283185307179586476925286766559L;
-    const long double part = turns - floorl(turns);   // [0, 1]
-    const long double steps = roundl(part * 18446744073709551616.0L);
-    r.step[i] = steps >= 18446744073709551616.0L ? 0 : (uint64_t)steps;
+    if (fabs(freqs[i]) >= 0x1p60) return EAS_ERR_UNSUPPORTED;
+    r.step[i] = step_of(freqs[i]);
     r.axis[i] = (uint8_t)a;
   }
   *rotary = r;
