@@ -114,8 +114,7 @@ eas_status eas_kv16_append(const eas_kv16_cache* cache, const eas_rotary* rotary
  * what is seen, what is left out, and rows that see nothing as in
  * eas_kv8_attention (shape: its k and v strides are not read; dtype, kv_heads
  * and head_dim as the cache's), but that the prefix sums in cu_q must not
- * decrease: of a sequence's rows that others' overlap, either's result may
- * stand.
+ * decrease: with sums that do, any row within [0, n_rows) may get anything.
  * A key's score of -inf, +inf or NaN and a value's infinities do what they do in
  * eas_prompt_attention, and what a query does not see never reaches its result.
  * Sums and the softmax are held in fp32, in whose range they stay for all finite

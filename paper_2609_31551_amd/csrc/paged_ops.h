@@ -133,6 +133,8 @@ __device__ __forceinline__ int sum_upto(int v) {
 // over i, i + 64, .. one after the other, and, to find one, the wave over a lane's.  Of more than 64 sequences the waves
 // of the workgroup, all of which come here together, take a share each (1,024 of 2,048 tokens, 4 heads, 4,096 allowed:
 // 914 us, each wave over all 1,060; 4,096 of them 4.3 and 7.4 ms; a chunk of 512 beside 255 single tokens 159 and 197 us).
+// Prefix sums that decrease would let rows, and pieces, be counted again and again: a lane counts MOST at most, more than a
+// launch has workgroups for, so that no sum wraps and a piece that is found is one of its sequence's.
 template <class Count>
 struct Items {
   const Kv16AttnArgs& a;
@@ -140,6 +142,7 @@ struct Items {
   int each;         // sequences of a lane
   Seq seq;          // of the last one that the lane looked at: its only one where there are 64 at most
   int own, upto;    // the lane's pieces, and those of it and of the lanes before
+  static constexpr int MOST = (1 << 25) - 1;   // a sequence has 2^24 at most
 
   __device__ __forceinline__ Items(const Kv16AttnArgs& a_, const Count& count_) : a(a_), count(count_) {
     each = (unsigned)(a.n_seqs + 63) / 64;
@@ -150,11 +153,11 @@ struct Items {
       const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
       own = 0;
 #pragma unroll 2
-      for (int i = wave; i < each; i += waves) own += look(i * 64 + lane);
+      for (int i = wave; i < each; i += waves) own = min(own + look(i * 64 + lane), MOST);
       shares[wave][lane] = own;
       __syncthreads();
       own = 0;
-      for (int w = 0; w < waves; ++w) own += shares[w][lane];
+      for (int w = 0; w < waves; ++w) own = min(own + shares[w][lane], MOST);
     }
     upto = sum_upto(own);
   }

@@ -69,3 +69,28 @@ def test_a_batch_of_8200_sequences_of_1024_heads():
     for a, b in ((0, 3000), (3000, 6000), (6000, n)):
         part, _ = cache.attention(q[c[a]:c[b]], lens[a:b], table[a:b], i32(torch, cu(new[a:b])), 40)
         assert torch.equal(part, out[c[a]:c[b]])
+
+
+def test_prefix_sums_that_decrease_end():
+    """What the rows get is open then; nothing else is written, and no sum of the pieces of work wraps, of which these 27,000
+    sequences of 20,000 queries and of less than none count 2 * 10^9."""
+    torch, B = lib()
+    n, rows, heads = 27000, 20000, 1024
+    assert (n // 2) * (rows * heads // 128) > 1 << 31
+    cache = B.Kv16Cache.empty(4, 1, 64, 16)
+    cache.k.fill_(1.0)
+    cache.v.fill_(2.0)
+    out = torch.full((rows + 8, heads, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((rows + 8, heads), 7.0, device="cuda")
+    q = make(torch, (1, 1, 64), torch.bfloat16, 630).expand(rows, heads, 64)
+    lens, table = i32(torch, np.full(n, 40)), i32(torch, np.tile([0, 1, 2, 3], (n, 1)))
+    print("[decreasing] %d sequences" % n, flush=True)
+    cache.attention(q, lens, table, i32(torch, np.arange(n + 1) % 2 * rows), rows, causal=False, out=out[4:-4], lse=lse[4:-4])
+    torch.cuda.synchronize()
+    for x in (out, lse):
+        assert (x[:4] == 7.0).all() and (x[-4:] == 7.0).all()
+    assert ((out[4:-4] == 2.0) | (out[4:-4] == 7.0)).all()           # all values are 2: what is computed is
+    # a batch as it should be, behind it
+    c = i32(torch, [0, 5, 5, 45])
+    one, _ = cache.attention(q[:45, :8], lens[:3], table[:3], c, 40, causal=False)
+    assert (one == 2.0).all()
