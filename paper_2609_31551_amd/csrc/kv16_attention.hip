@@ -13,7 +13,7 @@
 //
 // Bound by HBM, 4 * head_dim bytes a cached token and key / value head: 16 sequences of 32,768 tokens, 8 heads of 128,
 // 2,136 MB, take 379 us, 5.6 TB/s (a copy of 1 GiB runs at 5.2).  Short ones are bound by what comes before and behind:
-// lengths, pages and first tokens one after the other, 4 us; a workgroup draws 60 GB/ms at most, however far ahead its
+// lengths, pages and first tokens one after the other, 4 us; a workgroup draws 60 GB/s at most, however far ahead its
 // loads are (1,023 tokens of one head 13 us, 127 5.3); the join of runs is a launch of 5 us.  32 sequences of 1 to 8,192
 // tokens, 4 heads, 141 MB, 41 us.
 #include "kv16_chunks.h"

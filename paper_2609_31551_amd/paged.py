@@ -56,8 +56,8 @@ def _turned(x, name, out, heads, dim, dtype, index, stream):
 
 class Rotary:
     """What a model's positions do to a head (include/eas_paged.h, eas_rotary): pair i of its dimensions turns by
-    positions[axis[i]] * freqs[i] radians.  Pair i is dimensions (i, i + pairs) or, adjacent, (2 i, 2 i + 1); dimensions
-    behind the pairs pass.  Made once for a model; holds no device memory."""
+    positions[axis[i]] * freqs[i] radians (|freqs[i]| < 2 ** 60).  Pair i is dimensions (i, i + pairs) or, adjacent,
+    (2 i, 2 i + 1); dimensions behind the pairs pass.  Made once for a model; holds no device memory."""
 
     def __init__(self, freqs, axis=None, axes=None, adjacent=False):
         freqs = [float(f) for f in freqs]
